@@ -284,6 +284,116 @@ int tri_transition_bwd(int dtype, int64_t m, int64_t c, int64_t f, const void* x
                        float* dw1, float* dw2, float* dgamma, float* dbeta, void* workspace,
                        size_t workspace_bytes, void* stream);
 
+/* Layer norm by itself (the fused calls above normalise 128 features only):
+ * for every row of x [m][c]
+ *   xhat = (x - mean) * rstd,  rstd = 1 / sqrt(var + eps),
+ *   out = xhat * gamma + beta,
+ *   mean and var (biased) over the row's c features.
+ * out [m][c] (dtype); mean and rstd [m] (fp32) are saved for the backward.
+ *   gamma and beta [c] (dtype) may each be NULL (ones and zeros).
+ *   dtype: TRIATTN_F32 or TRIATTN_BF16; fp32 statistics and arithmetic, out
+ *          rounded once.
+ *   1 <= m <= 2^31, 1 <= c <= 8192 (TRIATTN_ERR_UNSUPPORTED above), any
+ *   parity; eps finite and >= 0.  out may be x itself.  No workspace.  Same
+ *   stream, pointer and error rules as above. */
+int tri_layer_norm_fwd(int dtype, int64_t m, int64_t c, float eps, const void* x,
+                       const void* gamma, const void* beta, void* out, float* mean, float* rstd,
+                       void* stream);
+
+/* Bytes of device workspace tri_layer_norm_bwd needs for these sizes. */
+int tri_layer_norm_bwd_workspace_bytes(int dtype, int64_t m, int64_t c, size_t* bytes);
+
+/* Backward of the layer norm for L = sum(dout * out): takes the forward's x,
+ * gamma (NULL = ones) and its saved mean and rstd, and dout [m][c].  With
+ * w = dout * gamma and c1, c2 the row means of w * xhat and of w:
+ *   dx = rstd (w - c1 xhat - c2)                       [m][c] (dtype)
+ *   dgamma = sum over rows of dout * xhat              [c] (fp32)
+ *   dbeta  = sum over rows of dout                     [c] (fp32)
+ * the sums taken in a fixed order (bitwise reproducible).  dgamma and dbeta
+ * may each be NULL (not wanted; the workspace may be NULL if both are).  dx
+ * may be dout itself. */
+int tri_layer_norm_bwd(int dtype, int64_t m, int64_t c, const void* x, const void* gamma,
+                       const float* mean, const float* rstd, const void* dout, void* dx,
+                       float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
+/* Linear projection with bias, activation and residual in one pass (after
+ * the attention: the projection of its output back to the pair channels,
+ * added to the pair representation):
+ *   z = x W + bias,   out = act(z) + residual,
+ * x [m][k], W [k][n], bias [n] (NULL = zeros), residual [m][n] (NULL = none),
+ * out [m][n], all in dtype.  z [m][n] (dtype) is written if it is not NULL:
+ * the backward of an activation takes it.
+ *   act: a triattn_act; gelu is z Phi(z) with the error function, silu is
+ *        z sigmoid(z).
+ *   dtype: TRIATTN_BF16 (bf16 products, fp32 sums, each output rounded once)
+ *          or TRIATTN_F32 (fp32 throughout).
+ *   1 <= m <= 2^31, 1 <= k, n <= 8192 (TRIATTN_ERR_UNSUPPORTED above), any
+ *   parity, and fewer than 2^24 tiles of 64 x 64 outputs
+ *   (TRIATTN_ERR_UNSUPPORTED).  out may be residual itself.  No workspace.
+ *   Same stream, pointer and error rules as above. */
+typedef enum {
+  TRIATTN_ACT_NONE = 0,
+  TRIATTN_ACT_RELU = 1,
+  TRIATTN_ACT_GELU = 2,
+  TRIATTN_ACT_SILU = 3
+} triattn_act;
+int tri_linear_fwd(int dtype, int64_t m, int64_t k, int64_t n, int act, const void* x,
+                   const void* w, const void* bias, const void* residual, void* out, void* z,
+                   void* stream);
+
+/* Bytes of device workspace tri_linear_bwd needs for these sizes. */
+int tri_linear_bwd_workspace_bytes(int dtype, int64_t m, int64_t k, int64_t n, int act,
+                                   size_t* bytes);
+
+/* Backward of the projection for L = sum(dout * out): takes the forward's x
+ * and W, z as the forward wrote it (NULL for TRIATTN_ACT_NONE) and dout
+ * [m][n].  With dz = dout * act'(z), act' evaluated at the z given and dz
+ * held in 24 bits (fp32 dw, dbias) or 16 bits (bf16 dx) in the products:
+ *   dx = dz W^T [m][k] (dtype),  dw = x^T dz [k][n] (fp32),
+ *   dbias = sum over rows of dz [n] (fp32);
+ * the residual's gradient is dout.  Sums over rows are taken in a fixed order
+ * (bitwise reproducible).  dx, dw and dbias may each be NULL (not wanted; at
+ * least one is not).  Sizes as the forward's, with [m][k] outputs too. */
+int tri_linear_bwd(int dtype, int64_t m, int64_t k, int64_t n, int act, const void* x,
+                   const void* w, const void* z, const void* dout, void* dx, float* dw,
+                   float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Learned relative position bias by buckets, in the layout of the attention's
+ * bias (or, with h the pair channels, a term of the pair representation):
+ *   bucket(q, k) = number of edges e with e <= pos[q] - pos[k],
+ *   out[b][q][k][:] = table[bucket(q, k)][:] (+ base[b][q][k][:]),
+ * pos [batch][n] (int32, any order and values; the difference is taken in 64
+ * bits), table [rows][h], out and base [batch][n][n][h] (dtype; base NULL =
+ * none, and out may be base itself).  rows = n_edges + 1; with chain
+ * [batch][n] (int32; NULL = one chain) tokens of different chains have the
+ * bucket n_edges + 1 instead, and rows = n_edges + 2.
+ *   edges: a HOST array of n_edges ascending int32 (TRIATTN_ERR_INVALID_ARG
+ *          if one is not above the one before it), read during the call;
+ *          1 <= n_edges <= 255 (TRIATTN_ERR_UNSUPPORTED above).
+ *   1 <= batch <= 2^20, 1 <= n <= 8192, 1 <= h <= 256 (TRIATTN_ERR_UNSUPPORTED
+ *   above).  The sum with base is rounded once.  base may hold -inf.  No
+ *   workspace.  pos and chain need 4-byte alignment, the other pointers 16.
+ *   Same stream and error rules as above. */
+int tri_rel_bias_fwd(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges,
+                     const int32_t* edges, const int32_t* pos, const int32_t* chain,
+                     const void* table, const void* base, void* out, void* stream);
+
+/* Bytes of device workspace tri_rel_bias_bwd needs for these sizes. */
+int tri_rel_bias_bwd_workspace_bytes(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges,
+                                     size_t* bytes);
+
+/* Gradient of the table for L = sum(dout * out):
+ *   dtable[r][:] = sum over b, q, k with bucket r of dout[b][q][k][:]
+ * [rows][h] (fp32, fixed order: bitwise reproducible; rows no pair falls into
+ * are 0).  dout [batch][n][n][h] (dtype; TRIATTN_F32 also takes the fp32
+ * dbias_partial of a row range).  base's gradient is dout.  Same rules as the
+ * forward. */
+int tri_rel_bias_bwd(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges,
+                     const int32_t* edges, const int32_t* pos, const int32_t* chain,
+                     const void* dout, float* dtable, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
 /* Static, human-readable name of a status code ("unknown status" otherwise). */
 const char* tri_attn_status_string(int status);
 

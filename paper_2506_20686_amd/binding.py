@@ -23,6 +23,7 @@ FWD_NOALLOC_SCRATCH_BYTES = 32 << 20  # TRIATTN_FWD_NOALLOC_SCRATCH_BYTES
 STARTING, ENDING = 0, 1
 F32, BF16 = 0, 1
 HEAD_DIM = 32
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 
 _LIB = None
 _vp, _i64, _f, _int, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_float, ctypes.c_int, ctypes.c_size_t
@@ -91,6 +92,24 @@ def lib():
             L.tri_transition_fwd_workspace_bytes.argtypes
         L.tri_transition_fwd.argtypes = [_int, _i64, _i64, _i64, _f] + [_vp] * 9 + [_sz, _vp]
         L.tri_transition_bwd.argtypes = [_int, _i64, _i64, _i64] + [_vp] * 14 + [_sz, _vp]
+        L.tri_layer_norm_fwd.argtypes = [_int, _i64, _i64, _f] + [_vp] * 7
+        L.tri_layer_norm_bwd_workspace_bytes.argtypes = [_int, _i64, _i64, ctypes.POINTER(_sz)]
+        L.tri_layer_norm_bwd.argtypes = [_int, _i64, _i64] + [_vp] * 9 + [_sz, _vp]
+        L.tri_linear_fwd.argtypes = [_int, _i64, _i64, _i64, _int] + [_vp] * 7
+        L.tri_linear_bwd_workspace_bytes.argtypes = [_int, _i64, _i64, _i64, _int,
+                                                     ctypes.POINTER(_sz)]
+        L.tri_linear_bwd.argtypes = [_int, _i64, _i64, _i64, _int] + [_vp] * 8 + [_sz, _vp]
+        _i32p = ctypes.POINTER(ctypes.c_int32)
+        L.tri_rel_bias_fwd.argtypes = [_int, _i64, _i64, _i64, _int, _i32p] + [_vp] * 6
+        L.tri_rel_bias_bwd_workspace_bytes.argtypes = [_int, _i64, _i64, _i64, _int,
+                                                       ctypes.POINTER(_sz)]
+        L.tri_rel_bias_bwd.argtypes = [_int, _i64, _i64, _i64, _int, _i32p] + [_vp] * 5 + \
+            [_sz, _vp]
+        for name in ("tri_layer_norm_fwd", "tri_layer_norm_bwd_workspace_bytes",
+                     "tri_layer_norm_bwd", "tri_linear_fwd", "tri_linear_bwd_workspace_bytes",
+                     "tri_linear_bwd", "tri_rel_bias_fwd", "tri_rel_bias_bwd_workspace_bytes",
+                     "tri_rel_bias_bwd"):
+            getattr(L, name).restype = _int
         for name in ("tri_transition_fwd_workspace_bytes", "tri_transition_bwd_workspace_bytes",
                      "tri_transition_fwd", "tri_transition_bwd"):
             getattr(L, name).restype = _int
@@ -281,6 +300,80 @@ def tri_transition_bwd(dtype, m, c, f, x, gamma, beta, w1, w2, mean, rstd, dout,
     return lib().tri_transition_bwd(dtype, m, c, f, x, gamma, beta, w1, w2, mean, rstd, dout,
                                     dx, dw1, dw2, dgamma, dbeta, workspace, workspace_bytes,
                                     stream)
+
+
+def tri_layer_norm_fwd(dtype, m, c, eps, x, gamma, beta, out, mean, rstd, stream) -> int:
+    """Raw call: every tensor argument is an integer device address (or None)."""
+    return lib().tri_layer_norm_fwd(dtype, m, c, eps, x, gamma, beta, out, mean, rstd, stream)
+
+
+def tri_layer_norm_bwd_workspace_bytes(dtype: int, m: int, c: int) -> int:
+    out = _sz(0)
+    st = lib().tri_layer_norm_bwd_workspace_bytes(dtype, m, c, ctypes.byref(out))
+    if st != OK:
+        raise TriAttnError(st, "tri_layer_norm_bwd_workspace_bytes")
+    return out.value
+
+
+def tri_layer_norm_bwd(dtype, m, c, x, gamma, mean, rstd, dout, dx, dgamma, dbeta, workspace,
+                       workspace_bytes, stream) -> int:
+    """Raw call: every tensor argument is an integer device address (or None)."""
+    return lib().tri_layer_norm_bwd(dtype, m, c, x, gamma, mean, rstd, dout, dx, dgamma, dbeta,
+                                    workspace, workspace_bytes, stream)
+
+
+def tri_linear_fwd(dtype, m, k, n, act, x, w, bias, residual, out, z, stream) -> int:
+    """Raw call: every tensor argument is an integer device address (or None)."""
+    return lib().tri_linear_fwd(dtype, m, k, n, act, x, w, bias, residual, out, z, stream)
+
+
+def tri_linear_bwd_workspace_bytes(dtype: int, m: int, k: int, n: int, act: int) -> int:
+    out = _sz(0)
+    st = lib().tri_linear_bwd_workspace_bytes(dtype, m, k, n, act, ctypes.byref(out))
+    if st != OK:
+        raise TriAttnError(st, "tri_linear_bwd_workspace_bytes")
+    return out.value
+
+
+def tri_linear_bwd(dtype, m, k, n, act, x, w, z, dout, dx, dw, dbias, workspace, workspace_bytes,
+                   stream) -> int:
+    """Raw call: every tensor argument is an integer device address (or None)."""
+    return lib().tri_linear_bwd(dtype, m, k, n, act, x, w, z, dout, dx, dw, dbias, workspace,
+                                workspace_bytes, stream)
+
+
+def _edges_arr(edges):
+    try:
+        values = [int(e) for e in edges]
+    except (TypeError, ValueError) as e:
+        raise TypeError("edges must be a sequence of integers") from e
+    if values and not (-(1 << 31) <= min(values) and max(values) < 1 << 31):
+        raise ValueError("edges must fit 32 bits")
+    return (ctypes.c_int32 * len(values))(*values)
+
+
+def tri_rel_bias_fwd(dtype, batch, n, h, edges, pos, chain, table, base, out, stream) -> int:
+    """Raw call: tensor arguments are integer device addresses (or None); edges
+    is a Python sequence (passed as a host array)."""
+    return lib().tri_rel_bias_fwd(dtype, batch, n, h, len(edges), _edges_arr(edges), pos, chain,
+                                  table, base, out, stream)
+
+
+def tri_rel_bias_bwd_workspace_bytes(dtype: int, batch: int, n: int, h: int,
+                                     n_edges: int) -> int:
+    out = _sz(0)
+    st = lib().tri_rel_bias_bwd_workspace_bytes(dtype, batch, n, h, n_edges, ctypes.byref(out))
+    if st != OK:
+        raise TriAttnError(st, "tri_rel_bias_bwd_workspace_bytes")
+    return out.value
+
+
+def tri_rel_bias_bwd(dtype, batch, n, h, edges, pos, chain, dout, dtable, workspace,
+                     workspace_bytes, stream) -> int:
+    """Raw call: tensor arguments are integer device addresses (or None); edges
+    is a Python sequence (passed as a host array)."""
+    return lib().tri_rel_bias_bwd(dtype, batch, n, h, len(edges), _edges_arr(edges), pos, chain,
+                                  dout, dtable, workspace, workspace_bytes, stream)
 
 
 def tri_attn_timing_enable(on: bool) -> None:
@@ -686,3 +779,204 @@ def transition_bwd(x, gamma, beta, w1, w2, mean, rstd, dout,
     if st != OK:
         raise TriAttnError(st, "tri_transition_bwd")
     return dx, dw1, dw2, dgamma, dbeta
+
+
+# ---- layer norm, linear projection with epilogue, relative position bias -------------------
+
+def _on(dev, fn, *args):
+    """fn(*args, stream) on torch's current stream of `dev`, with `dev` current."""
+    if dev.index is None or torch._C._cuda_getDevice() == dev.index:
+        return fn(*args, _stream(dev))
+    with torch.cuda.device(dev):
+        return fn(*args, _stream(dev))
+
+
+def _workspace(workspace, need, dev):
+    """The caller's workspace if it is large enough, else a new one."""
+    if workspace is not None:
+        if workspace.device != dev or workspace.dtype is not torch.uint8 or \
+                not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
+        if workspace.numel() >= need:
+            return workspace
+    return torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+
+
+def _check_2d(name, t):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two axes (got shape {tuple(t.shape)})")
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"unsupported dtype {t.dtype}")
+    _check(name, t, t.shape, t.dtype, t.device)
+    return _DTYPES[t.dtype]
+
+
+def layer_norm_fwd(x, gamma=None, beta=None, eps: float = 1e-5):
+    """out = (x - mean) * rstd * gamma + beta over the rows of x [m, c] (fp32 or
+    bf16; any c up to 8192); gamma and beta [c] may be None (ones, zeros).
+    Returns (out, mean, rstd), the statistics [m] in fp32."""
+    dt = _check_2d("x", x)
+    m, c = x.shape
+    dev = x.device
+    if gamma is not None:
+        _check("gamma", gamma, (c,), x.dtype, dev)
+    if beta is not None:
+        _check("beta", beta, (c,), x.dtype, dev)
+    out = torch.empty_like(x)
+    mean = torch.empty(m, dtype=torch.float32, device=dev)
+    rstd = torch.empty(m, dtype=torch.float32, device=dev)
+    st = _on(dev, tri_layer_norm_fwd, dt, m, c, float(eps), _ptr(x), _ptr(gamma), _ptr(beta),
+             _ptr(out), _ptr(mean), _ptr(rstd))
+    if st != OK:
+        raise TriAttnError(st, "tri_layer_norm_fwd")
+    return out, mean, rstd
+
+
+def layer_norm_bwd(x, gamma, mean, rstd, dout, workspace: Optional[torch.Tensor] = None):
+    """Gradients of sum(dout * out) for layer_norm_fwd.  Returns (dx [m, c],
+    dgamma [c] fp32, dbeta [c] fp32)."""
+    dt = _check_2d("x", x)
+    m, c = x.shape
+    dev = x.device
+    if gamma is not None:
+        _check("gamma", gamma, (c,), x.dtype, dev)
+    _check("mean", mean, (m,), torch.float32, dev)
+    _check("rstd", rstd, (m,), torch.float32, dev)
+    _check("dout", dout, (m, c), x.dtype, dev)
+    dx = torch.empty_like(x)
+    dgamma = torch.empty(c, dtype=torch.float32, device=dev)
+    dbeta = torch.empty(c, dtype=torch.float32, device=dev)
+    workspace = _workspace(workspace, tri_layer_norm_bwd_workspace_bytes(dt, m, c), dev)
+    st = _on(dev, tri_layer_norm_bwd, dt, m, c, _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd),
+             _ptr(dout), _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(workspace),
+             workspace.numel())
+    if st != OK:
+        raise TriAttnError(st, "tri_layer_norm_bwd")
+    return dx, dgamma, dbeta
+
+
+def linear_fwd(x, w, bias=None, residual=None, act: int = ACT_NONE, save_z: bool = False):
+    """out = act(x @ w + bias) + residual; x [m, k], w [k, n], bias [n] or None,
+    residual [m, n] or None, all fp32 or all bf16; act one of ACT_NONE,
+    ACT_RELU, ACT_GELU (error function), ACT_SILU.  Returns (out, z): z is the
+    value before the activation, in x's dtype, if save_z (linear_bwd takes it
+    when there is an activation), else None."""
+    dt = _check_2d("x", x)
+    m, k = x.shape
+    dev, dtype = x.device, x.dtype
+    _check_2d("w", w)
+    n = w.shape[1]
+    _check("w", w, (k, n), dtype, dev)
+    if bias is not None:
+        _check("bias", bias, (n,), dtype, dev)
+    if residual is not None:
+        _check("residual", residual, (m, n), dtype, dev)
+    out = torch.empty((m, n), dtype=dtype, device=dev)
+    z = torch.empty((m, n), dtype=dtype, device=dev) if save_z else None
+    st = _on(dev, tri_linear_fwd, dt, m, k, n, act, _ptr(x), _ptr(w), _ptr(bias),
+             _ptr(residual), _ptr(out), _ptr(z))
+    if st != OK:
+        raise TriAttnError(st, "tri_linear_fwd")
+    return out, z
+
+
+def linear_bwd(x, w, dout, z=None, act: int = ACT_NONE,
+               workspace: Optional[torch.Tensor] = None):
+    """Gradients of sum(dout * out) for linear_fwd: z as it returned it (None
+    without an activation).  Returns (dx [m, k] in x's dtype, dw [k, n] fp32,
+    dbias [n] fp32); the residual's gradient is dout."""
+    dt = _check_2d("x", x)
+    m, k = x.shape
+    dev, dtype = x.device, x.dtype
+    _check_2d("w", w)
+    n = w.shape[1]
+    _check("w", w, (k, n), dtype, dev)
+    _check("dout", dout, (m, n), dtype, dev)
+    if z is not None:
+        _check("z", z, (m, n), dtype, dev)
+    dx = torch.empty_like(x)
+    dw = torch.empty((k, n), dtype=torch.float32, device=dev)
+    dbias = torch.empty(n, dtype=torch.float32, device=dev)
+    workspace = _workspace(workspace, tri_linear_bwd_workspace_bytes(dt, m, k, n, act), dev)
+    st = _on(dev, tri_linear_bwd, dt, m, k, n, act, _ptr(x), _ptr(w), _ptr(z), _ptr(dout),
+             _ptr(dx), _ptr(dw), _ptr(dbias), _ptr(workspace), workspace.numel())
+    if st != OK:
+        raise TriAttnError(st, "tri_linear_bwd")
+    return dx, dw, dbias
+
+
+def rel_bias_edges(exact: int, far: int = 0, steps: int = 0):
+    """Ascending bucket borders for rel_bias_fwd, alike on both sides: the
+    differences -exact .. exact - 1 have buckets of their own, and beyond them
+    `steps` buckets a side grow geometrically up to `far` (fewer where two
+    borders would round to one); what is further shares the outermost bucket.
+    With steps = 0, bucket i is the difference clipped to [-exact, exact],
+    plus exact."""
+    exact, far, steps = int(exact), int(far), int(steps)
+    if exact < 1 or steps < 0 or (steps > 0 and far <= exact):
+        raise ValueError("exact >= 1, steps >= 0 and, with steps, far > exact are needed")
+    up = list(range(1, exact + 1))
+    up += sorted({math.ceil(exact * (far / exact) ** ((i + 1) / steps)) for i in range(steps)})
+    return [1 - e for e in reversed(up)] + up
+
+
+def _rel_common(pos, chain, t, name):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"unsupported dtype {t.dtype}")
+    if not isinstance(pos, torch.Tensor):
+        raise TypeError("pos must be a torch.Tensor")
+    if pos.dim() not in (1, 2):
+        raise ValueError("pos must be [n] or [b, n]")
+    dev = t.device
+    _check("pos", pos, pos.shape, torch.int32, dev)
+    if chain is not None:
+        _check("chain", chain, pos.shape, torch.int32, dev)
+    lead, n = tuple(pos.shape[:-1]), pos.shape[-1]
+    return _DTYPES[t.dtype], lead, lead[0] if lead else 1, n, dev
+
+
+def rel_bias_fwd(pos, edges, table, chain=None, base=None):
+    """Relative position bias: out[q, k, :] = table[bucket][:] (+ base[q, k, :])
+    with bucket the number of `edges` (ascending integers) at or below pos[q] -
+    pos[k], or the table's last row where chain[q] != chain[k].  pos and chain
+    [n] int32, table [len(edges) + 1 (+ 1 with chain), h] fp32 or bf16, base
+    [n, n, h] or None.  Returns out [n, n, h], the layout of the attention's
+    bias; with a leading batch axis on pos, chain and base, a batch."""
+    dt, lead, batch, n, dev = _rel_common(pos, chain, table, "table")
+    if table.dim() != 2:
+        raise ValueError("table must be [rows, h]")
+    h = table.shape[1]
+    _check("table", table, (len(edges) + 1 + (chain is not None), h), table.dtype, dev)
+    shape = lead + (n, n, h)
+    if base is not None:
+        _check("base", base, shape, table.dtype, dev)
+    out = torch.empty(shape, dtype=table.dtype, device=dev)
+    st = _on(dev, tri_rel_bias_fwd, dt, batch, n, h, edges, _ptr(pos), _ptr(chain), _ptr(table),
+             _ptr(base), _ptr(out))
+    if st != OK:
+        raise TriAttnError(st, "tri_rel_bias_fwd")
+    return out
+
+
+def rel_bias_bwd(pos, edges, dout, chain=None, workspace: Optional[torch.Tensor] = None):
+    """Gradient of sum(dout * out) for rel_bias_fwd: dout [n, n, h] (with a batch
+    axis if pos has one).  Returns dtable [rows, h] fp32; base's gradient is
+    dout."""
+    dt, lead, batch, n, dev = _rel_common(pos, chain, dout, "dout")
+    if dout.dim() != len(lead) + 3:
+        raise ValueError("dout must be [n, n, h] ([b, n, n, h] with pos [b, n])")
+    h = dout.shape[-1]
+    _check("dout", dout, lead + (n, n, h), dout.dtype, dev)
+    dtable = torch.empty((len(edges) + 1 + (chain is not None), h), dtype=torch.float32,
+                         device=dev)
+    need = tri_rel_bias_bwd_workspace_bytes(dt, batch, n, h, len(edges))
+    workspace = _workspace(workspace, need, dev)
+    st = _on(dev, tri_rel_bias_bwd, dt, batch, n, h, edges, _ptr(pos), _ptr(chain), _ptr(dout),
+             _ptr(dtable), _ptr(workspace), workspace.numel())
+    if st != OK:
+        raise TriAttnError(st, "tri_rel_bias_bwd")
+    return dtable

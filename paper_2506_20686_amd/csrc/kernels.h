@@ -187,4 +187,79 @@ int trn_bwd_parts(int64_t m, int f);
 hipError_t launch_trn_fwd(const TrnFwdArgs& a, hipStream_t s);
 hipError_t launch_trn_bwd(const TrnBwdArgs& a, hipStream_t s);
 
+// ---- layer norm (ln.hip) ----------------------------------------------------------------
+constexpr int LN_MAX_C = 8192;
+
+struct LnArgs {
+  int64_t m;
+  int c;
+  float eps;
+  const void *x, *gamma, *beta;  // x [m][c]; gamma and beta [c] or null
+  void* out;                     // [m][c]
+  float *mean, *rstd;            // [m]
+};
+
+struct LnBwdArgs {
+  int64_t m;
+  int c;
+  const void *x, *gamma, *dout;
+  const float *mean, *rstd;
+  void* dx;                // [m][c]
+  float *dgamma, *dbeta;   // [c] or null
+  float* part;             // workspace: [nwg][2][c] partial sums (dgamma's, dbeta's)
+  int nwg;
+};
+
+int ln_bwd_parts(int dtype, int64_t m, int c);  // nwg
+hipError_t launch_ln_fwd(int dtype, const LnArgs& a, hipStream_t s);
+hipError_t launch_ln_bwd(int dtype, const LnBwdArgs& a, hipStream_t s);
+
+// ---- linear projection with epilogue (lin.hip) --------------------------------------------
+constexpr int LIN_MAX_K = 8192;
+
+struct LinArgs {
+  int64_t m;
+  int k, n;
+  int act;                                // triattn_act
+  const void *x, *w, *bias, *residual;    // x [m][k], w [k][n]; bias, residual or null
+  void *out, *z;                          // [m][n]; z or null
+};
+
+struct LinBwdArgs {
+  int64_t m;
+  int k, n;
+  int act;
+  const void *x, *w, *z, *dout;
+  void* dx;                // [m][k] or null
+  float *dw, *dbias;       // [k][n], [n], or null
+  float* part;             // workspace: [splits] partial sums of k * n + n floats
+  int splits;
+};
+
+int lin_bwd_splits(int dtype, int64_t m, int k, int n);
+hipError_t launch_lin_fwd(int dtype, const LinArgs& a, hipStream_t s);
+hipError_t launch_lin_bwd(int dtype, const LinBwdArgs& a, hipStream_t s);
+
+// ---- relative position bias (rel.hip) -------------------------------------------------------
+constexpr int REL_MAX_EDGES = 255;
+constexpr int REL_MAX_H = 256;
+
+struct RelArgs {
+  int64_t batch;
+  int n, h;
+  int ne, rows;               // edges; table rows
+  const int32_t *pos, *chain; // [batch][n]; chain or null
+  const void *table, *base;   // [rows][h]; [batch][n][n][h] or null
+  void* out;                  // [batch][n][n][h]
+  const void* dout;           // backward
+  float* dtable;              // backward: [rows][h]
+  float* part;                // backward, workspace: [nwg][rows][h] partial sums
+  int nwg;
+  int32_t edges[REL_MAX_EDGES + 1];
+};
+
+int rel_bwd_parts(int dtype, int64_t batch, int64_t n, int h);
+hipError_t launch_rel_fwd(int dtype, const RelArgs& a, hipStream_t s);
+hipError_t launch_rel_bwd(int dtype, const RelArgs& a, hipStream_t s);
+
 }  // namespace triattn

@@ -32,6 +32,16 @@ enum KernelId {
   K_TRN_REDUCE,
   K_TRN_FINISH,
   K_PAD,
+  K_LN_FWD,
+  K_LN_BWD,
+  K_LN_REDUCE,
+  K_LIN_FWD,
+  K_LIN_BWD_DX,
+  K_LIN_BWD_W,
+  K_LIN_REDUCE,
+  K_REL_FWD,
+  K_REL_BWD,
+  K_REL_REDUCE,
   K_COUNT
 };
 

@@ -1,0 +1,153 @@
+"""The layer norm, the linear projection and the relative position bias as they
+are used around the attention: one block of a pair stack, forward and backward,
+against torch's 64-bit autograd; the same captured into a graph; two streams."""
+import math
+
+import pytest
+import torch
+
+import ops_ref as R
+from paper_2506_20686_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF = torch.bfloat16
+H, D, C = 4, 32, 128
+EDGES = B.rel_bias_edges(8)
+EPS = 1e-5
+
+
+def inputs(n, seed):
+    g = torch.Generator().manual_seed(seed)
+
+    def normal(*shape, std=1.0, mean=0.0):
+        return (torch.randn(*shape, generator=g) * std + mean).to(BF)
+
+    half = n // 2
+    return {"x": normal(n * n, C), "g1": normal(C, std=0.2, mean=1.0), "b1": normal(C, std=0.2),
+            "w": normal(C, 4 * C + H, std=C ** -0.5), "table": normal(len(EDGES) + 2, H),
+            "wo": normal(C, C, std=C ** -0.5), "bo": normal(C, std=0.2),
+            "g2": normal(C, std=0.2, mean=1.0), "b2": normal(C, std=0.2),
+            "wh": normal(C, 72, std=C ** -0.5), "bh": normal(72, std=0.2),
+            "dy": normal(n * n, 72),
+            "pos": torch.cat([torch.arange(half), torch.arange(n - half)]).to(torch.int32),
+            "chain": (torch.arange(n) >= half).to(torch.int32)}
+
+
+def block(t, n):
+    """Outputs and gradients of one block with the framework's calls: projection,
+    bias, attention, output projection with residual, layer norm, hidden layer."""
+    pair = (n, n, H, D)
+    (q, k, v, g, b), mean1, rstd1 = B.ln_linear_fwd(t["x"], t["g1"], t["b1"], t["w"],
+                                                    (C, C, C, C, H), EPS)
+    q, k, v, g = (a.view(pair) for a in (q, k, v, g))
+    bias = B.rel_bias_fwd(t["pos"], EDGES, t["table"], t["chain"], b.view(n, n, H))
+    o, lse = B.fwd(q, k, v, g, bias)
+    x2, _ = B.linear_fwd(o.view(n * n, C), t["wo"], t["bo"], t["x"])
+    y, mean2, rstd2 = B.layer_norm_fwd(x2, t["g2"], t["b2"], EPS)
+    out, z = B.linear_fwd(y, t["wh"], t["bh"], None, B.ACT_SILU, True)
+    # backward
+    dyn, dwh, dbh = B.linear_bwd(y, t["wh"], t["dy"], z, B.ACT_SILU)
+    dx2, dg2, db2 = B.layer_norm_bwd(x2, t["g2"], mean2, rstd2, dyn)
+    do, dwo, dbo = B.linear_bwd(o.view(n * n, C), t["wo"], dx2)
+    dq, dk, dv, dg, dbias = B.bwd(q, k, v, g, bias, o, lse, do.view(pair))
+    dtable = B.rel_bias_bwd(t["pos"], EDGES, dbias, t["chain"])
+    douts = [a.view(n * n, C) for a in (dq, dk, dv, dg)] + [dbias.view(n * n, H)]
+    dx, dw, dg1, db1 = B.ln_linear_bwd(t["x"], t["g1"], t["b1"], t["w"], mean1, rstd1, douts)
+    return {"out": out, "x2": x2, "dx": dx.float() + dx2.float(), "g1": dg1, "b1": db1, "w": dw,
+            "table": dtable, "wo": dwo, "bo": dbo, "g2": dg2, "b2": db2, "wh": dwh, "bh": dbh}
+
+
+def plain(t, n):
+    f8 = torch.float64
+    p = {k: v.to(f8).requires_grad_(True) for k, v in t.items() if v.dtype == BF and k != "dy"}
+
+    def norm(x, g, b):
+        d = x - x.mean(1, keepdim=True)
+        return d / torch.sqrt((d * d).mean(1, keepdim=True) + EPS) * g + b
+
+    q, k, v, g, b = torch.split(norm(p["x"], p["g1"], p["b1"]) @ p["w"], [C, C, C, C, H], dim=1)
+    q, k, v, g = (a.view(n, n, H, D) for a in (q, k, v, g))
+    bias = p["table"][R.buckets(t["pos"][None], EDGES, t["chain"][None])[0]] + b.view(n, n, H)
+    s = torch.einsum("rqhd,rkhd->rhqk", q, k) / math.sqrt(D) + bias.permute(2, 0, 1)[None]
+    o = torch.sigmoid(g) * torch.einsum("rhqk,rkhd->rqhd", torch.softmax(s, dim=3), v)
+    x2 = o.reshape(n * n, C) @ p["wo"] + p["bo"] + p["x"]
+    out = R.act(norm(x2, p["g2"], p["b2"]) @ p["wh"] + p["bh"], B.ACT_SILU)
+    (out * t["dy"].to(f8)).sum().backward()
+    got = {k: v.grad for k, v in p.items() if k != "x"}
+    return dict(got, out=out.detach(), x2=x2.detach(), dx=p["x"].grad)
+
+
+@pytest.mark.parametrize("n", [5, 24, 41])
+def test_block(n):
+    # some seven bf16 stages, each good to 2^-8 / sqrt(3) or, for the attention's
+    # gradients, 3.5e-3 of an output's norm; their errors add in squares to under 1e-2
+    t = inputs(n, n)
+    got = block({k: v.to(DEV) for k, v in t.items()}, n)
+    ref = plain(t, n)
+    for k in got:
+        R.fro(k, got[k], ref[k], 2e-2)
+
+
+def test_block_in_a_graph():
+    # captured once, replayed on other inputs with the program's own work between
+    n = 24
+    t = {k: v.to(DEV) for k, v in inputs(n, 1).items()}
+    other = {k: v.to(DEV) for k, v in inputs(n, 2).items()}
+    first = {k: v.clone() for k, v in t.items()}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        block(t, n)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = block(t, n)
+    for src in (other, first, other):
+        want = block(src, n)  # eager work between the replays
+        for k in t:
+            t[k].copy_(src[k])
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in out:
+            assert torch.equal(out[k], want[k]), k
+
+
+def test_two_graphs_with_one_workspace():
+    # calls that share a workspace follow each other on one stream
+    m, k, n = 700, 64, 96
+    g = torch.Generator(DEV).manual_seed(4)
+    x, dy = (torch.randn(m, c, generator=g, device=DEV).to(BF) for c in (k, n))
+    w = torch.randn(k, n, generator=g, device=DEV).to(BF)
+    mean, rstd = B.layer_norm_fwd(x)[1:]
+    need = max(B.tri_linear_bwd_workspace_bytes(B.BF16, m, k, n, 0),
+               B.tri_layer_norm_bwd_workspace_bytes(B.BF16, m, k))
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    lin, ln = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(lin):
+        a = B.linear_bwd(x, w, dy, workspace=ws)
+    with torch.cuda.graph(ln):
+        b = B.layer_norm_bwd(x, None, mean, rstd, x, workspace=ws)
+    want_a, want_b = B.linear_bwd(x, w, dy), B.layer_norm_bwd(x, None, mean, rstd, x)
+    for _ in range(3):
+        ws.fill_(255)
+        lin.replay()
+        ln.replay()
+        torch.cuda.synchronize()
+        for got, want in zip((*a, *b), (*want_a, *want_b)):
+            assert torch.equal(got, want)
+
+
+def test_two_streams_at_once():
+    n = 24
+    t = [{k: v.to(DEV) for k, v in inputs(n, s).items()} for s in (5, 6)]
+    want = [block(a, n) for a in t]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in t], []
+    for a, s in zip(t, streams):
+        with torch.cuda.stream(s):
+            got.append(block(a, n))
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        for k in w:
+            assert torch.equal(g[k], w[k]), k

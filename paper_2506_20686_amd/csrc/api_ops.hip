@@ -45,8 +45,7 @@ int lin_check(int dtype, int64_t m, int64_t k, int64_t n, int act) {
 }
 
 size_t lin_ws(int dtype, int64_t m, int64_t k, int64_t n) {
-  return round256((size_t)triattn::lin_bwd_splits(dtype, m, (int)k, (int)n) *
-                  (size_t)(k * n + n) * sizeof(float));
+  return round256(triattn::lin_bwd_ws(dtype, m, (int)k, (int)n));
 }
 
 int rel_check(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges) {

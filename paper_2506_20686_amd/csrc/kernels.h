@@ -232,11 +232,12 @@ struct LinBwdArgs {
   const void *x, *w, *z, *dout;
   void* dx;                // [m][k] or null
   float *dw, *dbias;       // [k][n], [n], or null
-  float* part;             // workspace: [splits] partial sums of k * n + n floats
+  float* part;             // workspace: [splits] partial sums (dw, dbias); none for 1 split
   int splits;
 };
 
 int lin_bwd_splits(int dtype, int64_t m, int k, int n);
+size_t lin_bwd_ws(int dtype, int64_t m, int k, int n);  // bytes of workspace
 hipError_t launch_lin_fwd(int dtype, const LinArgs& a, hipStream_t s);
 hipError_t launch_lin_bwd(int dtype, const LinBwdArgs& a, hipStream_t s);
 

@@ -1,5 +1,29 @@
-// Linear projection with bias, activation and residual, and its backward.
+// Linear projection with bias, activation and residual, and its backward:
+//   forward  z = x W + bias, out = act(z) + residual      contraction over k
+//   dx = dz W^T, dz = dout act'(z)                        contraction over n
+//   dW = x^T dz, dbias = column sums of dz                contraction over the m rows
+//
+// All three products run through one kernel body: a workgroup of 4 waves (2 x 2) makes an
+// R x R tile of the result, R = 128 or 64, staging tiles of both operands through
+// registers into two LDS buffers in turn, and multiplies them on the matrix cores (bf16
+// 32 x 32 x 16, fp32 sums).  Loads of the tile after next are in flight while one is
+// multiplied; one barrier a step.
+//
+// Operands: a tile is stored as it lies in memory, either [row][contraction] ("K major":
+// fragments are 16-byte reads) or [contraction][row] (fragments are the LDS's transposing
+// reads), so neither W, W^T nor x^T is ever copied.
+//
+// Precision: an fp32 value is the sum of three bf16 (8 bits each, rounded to nearest), so
+// fp32 operands are staged as three planes and a product is the six plane products above
+// 2^-24 of it; sums are fp32 throughout.  Six bf16 instructions for what would be 8 fp32
+// ones of four times the length each.  With bf16 tensors, dz of a smooth activation is
+// not a bf16 value: it enters dW (an fp32 result) as three planes and dx (a bf16 result)
+// as two, 16 bits, so that the result's own rounding is the only one that shows.
+//
+// Every sum over rows is split over workgroups; their partial sums, in the workspace, are
+// added in a fixed order.
 #include "kernels.h"
+#include "dma.h"
 #include "timing.h"
 #include "triattn.h"
 
@@ -25,132 +49,564 @@ __device__ inline float act_grad(float z, int act) {
   return 1.f;
 }
 
-// A 16 x 16 output tile per workgroup: C[i][j] = sum over t of A(i, t) B(t, j), the
-// operands staged through LDS in fp32.
-template <typename FA, typename FB>
-__device__ inline float tile_product(int64_t t0, int64_t t1, FA fa, FB fb) {
-  __shared__ float sa[16][17], sb[16][17];
-  const int ti = threadIdx.x >> 4, tj = threadIdx.x & 15;
-  float acc = 0.f;
-  for (int64_t t = t0; t < t1; t += 16) {
-    sa[ti][tj] = t + tj < t1 ? fa(ti, t + tj) : 0.f;
-    sb[ti][tj] = t + ti < t1 ? fb(t + ti, tj) : 0.f;
-    __syncthreads();
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// Eight consecutive elements as they lie in memory.
+template <typename T>
+struct Raw8 {
+  static constexpr int N = (int)sizeof(T) / 2;  // 16-byte words
+  u32x4 v[N];
+};
+template <typename T>
+__device__ inline void unpack(const Raw8<T>& r, float (&f)[8]) {
+  struct E {
+    T x[8];
+  };
+  const E e = __builtin_bit_cast(E, r);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) acc += sa[ti][e] * sb[e][tj];
-    __syncthreads();
-  }
-  return acc;
+  for (int i = 0; i < 8; ++i) f[i] = (float)e.x[i];
 }
 
+struct __attribute__((packed)) Any16 {
+  u32x4 v;
+};
+
+// A row-major matrix [rows][cols] seen from a tile's corner.
 template <typename T>
+struct Mat {
+  const T* p;
+  int64_t rows;
+  int cols;
+};
+
+// Chunk (r, c .. c + 7) of the window at (r0, c0) of a matrix, `lim` rows high: zeros
+// outside.  ALIGNED: the width is a multiple of 8 elements, so a chunk is all in or all
+// out and the buffer resource's range check gives the zeros.  Otherwise rows start at any
+// element (16-byte loads may), and a row's last chunk goes element by element.
+template <typename T, bool ALIGNED>
+__device__ inline Raw8<T> fetch(const Mat<T>& m, int64_t r0, int c0, int lim, int r, int c) {
+  Raw8<T> x{};
+  const int64_t left = m.rows - r0;
+  const int rows = left < lim ? (left < 0 ? 0 : (int)left) : lim;
+  const T* base = m.p + r0 * m.cols + c0;
+  if constexpr (ALIGNED) {
+    // the last row's end past the corner; a row is at most 32 KB, a window 4 MB
+    const rsrc_t rs = buf_rsrc_n(base, rows ? (uint32_t)(rows * m.cols - c0) * sizeof(T) : 0u);
+    const uint32_t off = c0 + c < m.cols ? (uint32_t)(r * m.cols + c) * sizeof(T) : 0x80000000u;
+#pragma unroll
+    for (int i = 0; i < Raw8<T>::N; ++i)
+      x.v[i] = __builtin_bit_cast(
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(off + 16 * i), 0, 0));
+  } else if (r < rows) {
+    const T* s = base + (int64_t)r * m.cols + c;
+    const int have = m.cols - (c0 + c);
+    if (have >= 8) {
+#pragma unroll
+      for (int i = 0; i < Raw8<T>::N; ++i) x.v[i] = ((const Any16*)s)[i].v;
+    } else if (have > 0) {
+      struct E {
+        T e[8];
+      } y{};
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < have) y.e[i] = s[i];
+      x = __builtin_bit_cast(Raw8<T>, y);
+    }
+  }
+  return x;
+}
+
+// One operand's tile of R rows x BK contraction indices in LDS, as P planes of bf16.
+// Reads of a fragment (32 rows x 16 indices: lane l holds row l % 32, indices
+// 8 (l / 32) .. + 7) and the stores of staged chunks are free of bank conflicts whether
+// the LDS serves 128 or 256 bytes a cycle: the 16-byte chunks of a K major row are
+// permuted by XOR with a value that differs between any 8 (and, with the row's parity or
+// row % 4, any 16) consecutive rows; the 64-byte pieces of a transposed tile's line by
+// one that differs between the four lines of a transposing read.
+template <int R, int BK, bool KM, int P>
+struct Tile {
+  static constexpr int PLANE = R * BK * 2;
+  static constexpr int BYTES = P * PLANE;
+  static constexpr int LINE = KM ? BK / 8 : R / 8;  // chunks of a line
+  __device__ static inline int chunk_at(int line, int c) {
+    if constexpr (KM) {
+      static_assert(BK == 64 || BK == 32, "chunks of a line");
+      const int s = BK == 64 ? (line & 7) ^ ((line >> 3) & 1) : swz(line);
+      return (line * LINE + (c ^ s)) * 16;
+    } else {
+      static_assert(R == 128 || R == 64, "chunks of a line");
+      const int s = R == 128 ? (line & 3) << 2 : ((line >> 1) & 1) << 2;
+      return (line * LINE + (c ^ s)) * 16;
+    }
+  }
+  // Fragment of rows r0 .. r0 + 31, indices k0 .. k0 + 15.
+  __device__ static inline bf16x8 frag(const char* plane, int r0, int k0, int lane) {
+    if constexpr (KM) {
+      return *(const bf16x8*)(plane + chunk_at(r0 + (lane & 31), (k0 >> 3) + (lane >> 5)));
+    } else {
+      // lane 4 e + j of a group of 16 gives 8 bytes (rows r0 + 16 G + 4 j .. + 3) of index
+      // k0 + 8 g + e (+ 4) and receives its own row's four indices
+      const int i = lane & 15, row = r0 + (lane & 16) + 4 * (i & 3);
+      const int k = k0 + 8 * (lane >> 5) + (i >> 2);
+      typedef TRIATTN_LDS s16x4* lds4;
+      const char* a = plane + chunk_at(k, row >> 3) + (row & 4) * 2;
+      const char* b = plane + chunk_at(k + 4, row >> 3) + (row & 4) * 2;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(uintptr_t)lds_addr(a));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(uintptr_t)lds_addr(b));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+};
+
+// What dz is made of.
+enum Dz { DZ_X, DZ_RELU, DZ_ACT };  // the tensor itself; dout where z > 0; dout act'(z)
+
+// Staging of one operand: this thread's chunks of a tile, from memory to LDS.
+template <typename T, int R, int BK, bool KM, int P, int DZ, bool ALIGNED>
+struct Stage {
+  using L = Tile<R, BK, KM, P>;
+  static constexpr int N = R * BK / 8 / 256;  // chunks a thread
+  Raw8<T> x[N], z[DZ == DZ_X ? 1 : N];
+
+  // Tile at rows i0, indices k0 (of k1): lines are rows (K major) or indices.
+  __device__ inline void load(const Mat<T>& m, const T* zp, int64_t i0, int64_t k0, int64_t k1) {
+    Mat<T> w = m;
+    if (!KM) w.rows = k1;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int id = (int)threadIdx.x + 256 * u, line = id / L::LINE, c = 8 * (id % L::LINE);
+      const int64_t r0 = KM ? i0 : k0;
+      const int c0 = (int)(KM ? k0 : i0), lim = KM ? R : BK;
+      x[u] = fetch<T, ALIGNED>(w, r0, c0, lim, line, c);
+      if constexpr (DZ != DZ_X)
+        z[u] = fetch<T, ALIGNED>(Mat<T>{zp, w.rows, w.cols}, r0, c0, lim, line, c);
+    }
+  }
+  // The values of chunk u.
+  __device__ inline void values(int u, int act, float (&f)[8]) const {
+    unpack(x[u], f);
+    if constexpr (DZ != DZ_X) {
+      float g[8];
+      unpack(z[u], g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        f[e] = DZ == DZ_RELU ? (g[e] > 0.f ? f[e] : 0.f) : f[e] * act_grad(g[e], act);
+    }
+  }
+  // Stores the planes; with SUM, adds the values to the thread's column sums (its chunks
+  // lie in the same columns of every line).
+  template <bool SUM>
+  __device__ inline void store(char* tile, int act, bool sum, float (&col)[8]) const {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int id = (int)threadIdx.x + 256 * u;
+      char* d = tile + L::chunk_at(id / L::LINE, id % L::LINE);
+      float f[8];
+      if (P > 1 || DZ != DZ_X || SUM) values(u, act, f);
+      if (SUM && sum) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) col[e] += f[e];
+      }
+      if constexpr (P == 1 && DZ == DZ_X) {
+        *(u32x4*)d = x[u].v[0];
+      } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          bf16x8 b;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            b[e] = (bf16)f[e];
+            if (p + 1 < P) f[e] -= (float)b[e];
+          }
+          *(bf16x8*)(d + p * L::PLANE) = b;
+        }
+      }
+    }
+  }
+};
+
+// C tile (rows i0 .. i0 + R - 1, columns j0 .. j0 + R - 1) = sum over indices [k0, k1) of
+// A(i, k) B(k, j), in registers: acc[u][v] of wave (wi, wj) holds rows wi R/2 + 32 u + l % 32
+// and columns wj R/2 + 32 v + accumulator rows (acc_row).
+template <typename T, int R, int BK, bool AKM, bool BKM, int PA, int PB, int DZA, int DZB,
+          bool ALIGNED, bool SUM>
+struct Product {
+  static constexpr int NT = R / 64;  // 32-wide tiles of a wave, each way
+  using SA = Stage<T, R, BK, AKM, PA, DZA, ALIGNED>;
+  using SB = Stage<T, R, BK, BKM, PB, DZB, ALIGNED>;
+  using LA = typename SA::L;
+  using LB = typename SB::L;
+  static constexpr int BUF = LA::BYTES + LB::BYTES;
+  static constexpr int EPI = 4 * 32 * (R / 2 + 4) * 4;  // the result's staging
+  static constexpr int LDS = 2 * BUF > EPI ? 2 * BUF : EPI;
+
+  __device__ static inline void run(char* lds, const Mat<T>& a, const T* az, const Mat<T>& b,
+                                    const T* bz, int act, int64_t i0, int j0, int64_t k0,
+                                    int64_t k1, bool sum, float (&col)[8],
+                                    f32x16 (&acc)[NT][NT]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int ri = (wave >> 1) * (R / 2), rj = (wave & 1) * (R / 2);
+#pragma unroll
+    for (int u = 0; u < NT; ++u)
+#pragma unroll
+      for (int v = 0; v < NT; ++v) acc[u][v] = f32x16{};
+    SA sa;
+    SB sb;
+    sa.load(a, az, i0, k0, k1);
+    sb.load(b, bz, j0, k0, k1);
+    const int steps = (int)((k1 - k0 + BK - 1) / BK);
+    for (int it = 0; it < steps; ++it) {
+      char* buf = lds + (it & 1) * BUF;
+      float none[8];
+      sa.template store<false>(buf, act, false, none);
+      sb.template store<SUM>(buf + LA::BYTES, act, sum, col);
+      if (it + 1 < steps) {
+        const int64_t k = k0 + (int64_t)(it + 1) * BK;
+        sa.load(a, az, i0, k, k1);
+        sb.load(b, bz, j0, k, k1);
+      }
+      // the buffer of step it was last read in step it - 2, before the barrier of it - 1
+      __syncthreads();
+#pragma unroll
+      for (int kk = 0; kk < BK; kk += 16) {
+        bf16x8 fa[PA][NT], fb[PB][NT];
+#pragma unroll
+        for (int p = 0; p < PA; ++p)
+#pragma unroll
+          for (int u = 0; u < NT; ++u)
+            fa[p][u] = LA::frag(buf + p * LA::PLANE, ri + 32 * u, kk, lane);
+#pragma unroll
+        for (int p = 0; p < PB; ++p)
+#pragma unroll
+          for (int v = 0; v < NT; ++v)
+            fb[p][v] = LB::frag(buf + LA::BYTES + p * LB::PLANE, rj + 32 * v, kk, lane);
+        // plane products down to 2^-24 of the whole, the smallest first
+        constexpr int MOST = (PA > PB ? PA : PB) - 1;
+#pragma unroll
+        for (int order = MOST; order >= 0; --order)
+#pragma unroll
+          for (int p = 0; p < PA; ++p) {
+            const int q = order - p;
+            if (q < 0 || q >= PB) continue;
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+#pragma unroll
+              for (int v = 0; v < NT; ++v)
+                acc[u][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[q][v], fa[p][u], acc[u][v],
+                                                                    0, 0, 0);
+          }
+      }
+    }
+  }
+
+  // Hands the result, 8 consecutive columns at a time, to f(i, j, values): through LDS, 32
+  // rows a wave at a time, so that the accesses f makes are whole rows' pieces.
+  template <typename F>
+  __device__ static inline void result(char* lds, const f32x16 (&acc)[NT][NT], F f) {
+    constexpr int W = R / 2, ROW = W + 4, PER = 64 / (W / 8);  // rows a pass
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float* mine = (float*)lds + wave * 32 * ROW;
+    const int j = 8 * (lane % (W / 8));
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      __syncthreads();
+#pragma unroll
+      for (int v = 0; v < NT; ++v)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x16& c = acc[u][v];
+          *(f32x4*)(mine + (lane & 31) * ROW + 32 * v + 8 * q + 4 * (lane >> 5)) =
+              f32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+        }
+      __syncthreads();
+#pragma unroll
+      for (int s = 0; s < 32; s += PER) {
+        const int i = s + lane / (W / 8);
+        float o[8];
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+          const f32x4 x = *(const f32x4*)(mine + i * ROW + j + e);
+          o[e] = x[0], o[e + 1] = x[1], o[e + 2] = x[2], o[e + 3] = x[3];
+        }
+        f((wave >> 1) * W + 32 * u + i, (wave & 1) * W + j, o);
+      }
+    }
+  }
+};
+
+// Writes the first `have` of 8 values to p; ALIGNED: all of them, at 16 bytes.
+template <typename T, bool ALIGNED>
+__device__ inline void put8(T* p, int have, const float (&f)[8]) {
+  struct E {
+    T e[8];
+  } y;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y.e[i] = (T)f[i];
+  const Raw8<T> r = __builtin_bit_cast(Raw8<T>, y);
+  if (ALIGNED) {
+#pragma unroll
+    for (int i = 0; i < Raw8<T>::N; ++i) ((u32x4*)p)[i] = r.v[i];
+  } else if (have >= 8) {
+#pragma unroll
+    for (int i = 0; i < Raw8<T>::N; ++i) ((Any16*)p)[i].v = r.v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < have) p[i] = y.e[i];
+  }
+}
+// Reads the first `have` of 8 values (zeros after them).
+template <typename T, bool ALIGNED>
+__device__ inline void get8(const T* p, int have, float (&f)[8]) {
+  Raw8<T> r{};
+  if (ALIGNED) {
+#pragma unroll
+    for (int i = 0; i < Raw8<T>::N; ++i) r.v[i] = ((const u32x4*)p)[i];
+  } else if (have >= 8) {
+#pragma unroll
+    for (int i = 0; i < Raw8<T>::N; ++i) r.v[i] = ((const Any16*)p)[i].v;
+  } else {
+    struct E {
+      T e[8];
+    } y{};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < have) y.e[i] = p[i];
+    r = __builtin_bit_cast(Raw8<T>, y);
+  }
+  unpack(r, f);
+}
+
+// Contraction indices a step: as many as two buffers of three planes leave room for.
+template <typename T>
+constexpr int step_k() {
+  return sizeof(T) == 2 ? 64 : 32;
+}
+template <typename T>
+constexpr int planes() {
+  return sizeof(T) == 2 ? 1 : 3;
+}
+
+template <typename T, int R, bool ALIGNED>
 __global__ __launch_bounds__(256) void lin_fwd_kernel(LinArgs a) {
-  const int64_t i0 = (int64_t)blockIdx.x * 16;
-  const int j0 = blockIdx.y * 16;
-  const T *x = (const T*)a.x, *w = (const T*)a.w;
-  float z = tile_product(
-      0, a.k, [&](int i, int64_t t) { return i0 + i < a.m ? (float)x[(i0 + i) * a.k + t] : 0.f; },
-      [&](int64_t t, int j) { return j0 + j < a.n ? (float)w[t * a.n + j0 + j] : 0.f; });
-  const int64_t i = i0 + (threadIdx.x >> 4);
-  const int j = j0 + (threadIdx.x & 15);
-  if (i >= a.m || j >= a.n) return;
-  if (a.bias) z += (float)((const T*)a.bias)[j];
-  float o = act_value(z, a.act);
-  if (a.residual) o += (float)((const T*)a.residual)[i * a.n + j];
-  ((T*)a.out)[i * a.n + j] = (T)o;
-  if (a.z) ((T*)a.z)[i * a.n + j] = (T)z;
+  using G = Product<T, R, step_k<T>(), true, false, planes<T>(), planes<T>(), DZ_X, DZ_X, ALIGNED,
+                    false>;
+  __shared__ __attribute__((aligned(16))) char lds[G::LDS];
+  const int nj = (a.n + R - 1) / R, wg = xcd_swizzle(blockIdx.x, gridDim.x);
+  const int64_t i0 = (int64_t)(wg / nj) * R;
+  const int j0 = (wg % nj) * R;
+  f32x16 acc[G::NT][G::NT];
+  float none[8];
+  G::run(lds, Mat<T>{(const T*)a.x, a.m, a.k}, nullptr, Mat<T>{(const T*)a.w, a.k, a.n}, nullptr,
+         0, i0, j0, 0, a.k, false, none, acc);
+  G::result(lds, acc, [&](int di, int dj, float (&o)[8]) {
+    const int64_t i = i0 + di;
+    const int j = j0 + dj, have = a.n - j;
+    if (i >= a.m || have <= 0) return;
+    const int64_t at = i * a.n + j;
+    float b[8];
+    if (a.bias) {
+      get8<T, ALIGNED>((const T*)a.bias + j, have, b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] += b[e];
+    }
+    if (a.z) put8<T, ALIGNED>((T*)a.z + at, have, o);
+    if (a.act != TRIATTN_ACT_NONE) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = act_value(o[e], a.act);
+    }
+    if (a.residual) {
+      get8<T, ALIGNED>((const T*)a.residual + at, have, b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] += b[e];
+    }
+    put8<T, ALIGNED>((T*)a.out + at, have, o);
+  });
 }
 
-template <typename T>
-__device__ inline float dz_at(const LinBwdArgs& a, int64_t i, int j) {
-  const float dy = (float)((const T*)a.dout)[i * a.n + j];
-  return a.act == TRIATTN_ACT_NONE ? dy
-                                   : dy * act_grad((float)((const T*)a.z)[i * a.n + j], a.act);
-}
-
-template <typename T>
+// dx = dz W^T: W's rows are the columns of dx, its columns the contraction.
+template <typename T, int R, int DZ, bool ALIGNED>
 __global__ __launch_bounds__(256) void lin_bwd_dx_kernel(LinBwdArgs a) {
-  const int64_t i0 = (int64_t)blockIdx.x * 16;
-  const int j0 = blockIdx.y * 16;
-  const T* w = (const T*)a.w;
-  const float d = tile_product(
-      0, a.n, [&](int i, int64_t t) { return i0 + i < a.m ? dz_at<T>(a, i0 + i, (int)t) : 0.f; },
-      [&](int64_t t, int j) { return j0 + j < a.k ? (float)w[(int64_t)(j0 + j) * a.n + t] : 0.f; });
-  const int64_t i = i0 + (threadIdx.x >> 4);
-  const int j = j0 + (threadIdx.x & 15);
-  if (i < a.m && j < a.k) ((T*)a.dx)[i * a.k + j] = (T)d;
+  constexpr int PA = sizeof(T) == 4 ? 3 : DZ == DZ_ACT ? 2 : 1;
+  using G = Product<T, R, (PA > 1 ? 32 : 64), true, true, PA, planes<T>(), DZ, DZ_X, ALIGNED, false>;
+  __shared__ __attribute__((aligned(16))) char lds[G::LDS];
+  const int nj = (a.k + R - 1) / R, wg = xcd_swizzle(blockIdx.x, gridDim.x);
+  const int64_t i0 = (int64_t)(wg / nj) * R;
+  const int j0 = (wg % nj) * R;
+  f32x16 acc[G::NT][G::NT];
+  float none[8];
+  G::run(lds, Mat<T>{(const T*)a.dout, a.m, a.n}, (const T*)a.z, Mat<T>{(const T*)a.w, a.k, a.n},
+         nullptr, a.act, i0, j0, 0, a.n, false, none, acc);
+  G::result(lds, acc, [&](int di, int dj, float (&o)[8]) {
+    const int64_t i = i0 + di;
+    const int j = j0 + dj, have = a.k - j;
+    if (i < a.m && have > 0) put8<T, ALIGNED>((T*)a.dx + i * a.k + j, have, o);
+  });
 }
 
-// Workgroup (i tile, j tile, split): one split's rows of dw and, in the i tile past the
-// last one, of dbias (x taken as ones).
-template <typename T>
+// Rows of a split, a multiple of the largest step.
+__host__ __device__ inline int64_t split_rows(int64_t m, int splits) {
+  const int64_t per = (m + splits - 1) / splits;
+  return (per + 63) / 64 * 64;
+}
+// Floats of one split's partial sums: dw, then dbias.
+__host__ __device__ inline int64_t slab_floats(int k, int n) {
+  return ((int64_t)k * n + n + 3) / 4 * 4;
+}
+
+// One split's dW tile and, in the first row of tiles, its dbias.  Without splits the
+// results themselves.
+template <typename T, int R, int DZ, bool ALIGNED>
 __global__ __launch_bounds__(256) void lin_bwd_w_kernel(LinBwdArgs a) {
-  const int64_t per = (a.m + a.splits - 1) / a.splits;
-  const int64_t r0 = blockIdx.z * per, r1 = min(a.m, r0 + per);
-  const int i0 = blockIdx.x * 16, j0 = blockIdx.y * 16;
-  const bool ones = i0 >= a.k;
-  const T* x = (const T*)a.x;
-  const float d = tile_product(
-      r0, r1,
-      [&](int i, int64_t t) {
-        return ones ? 1.f : (i0 + i < a.k ? (float)x[t * a.k + i0 + i] : 0.f);
-      },
-      [&](int64_t t, int j) { return j0 + j < a.n ? dz_at<T>(a, t, j0 + j) : 0.f; });
-  const int i = i0 + (threadIdx.x >> 4);
-  const int j = j0 + (threadIdx.x & 15);
-  float* part = a.part + (int64_t)blockIdx.z * ((int64_t)a.k * a.n + a.n);
-  if (j >= a.n) return;
-  if (ones) {
-    if ((threadIdx.x >> 4) == 0) part[(int64_t)a.k * a.n + j] = d;
-  } else if (i < a.k) {
-    part[(int64_t)i * a.n + j] = d;
+  constexpr int PB = sizeof(T) == 4 || DZ == DZ_ACT ? 3 : 1;
+  using G = Product<T, R, (PB > 1 ? 32 : 64), false, false, planes<T>(), PB, DZ_X, DZ, ALIGNED,
+                    true>;
+  __shared__ __attribute__((aligned(16))) char lds[G::LDS];
+  const int ni = (a.k + R - 1) / R, nj = (a.n + R - 1) / R;
+  const int wg = xcd_swizzle(blockIdx.x, gridDim.x), split = wg / (ni * nj);
+  const int i0 = wg % (ni * nj) / nj * R, j0 = wg % nj * R;
+  const int64_t per = split_rows(a.m, a.splits), k0 = split * per;
+  const int64_t k1 = k0 + per < a.m ? k0 + per : a.m;
+  const bool sum = i0 == 0 && a.dbias != nullptr;
+  float* dw = a.splits > 1 ? a.part + split * slab_floats(a.k, a.n) : a.dw;
+  float* db = a.splits > 1 ? dw + (int64_t)a.k * a.n : a.dbias;
+  f32x16 acc[G::NT][G::NT];
+  float col[8] = {};
+  G::run(lds, Mat<T>{(const T*)a.x, a.m, a.k}, nullptr, Mat<T>{(const T*)a.dout, a.m, a.n},
+         (const T*)a.z, a.act, i0, j0, k0, k1, sum, col, acc);
+  if (a.dw)
+    G::result(lds, acc, [&](int di, int dj, float (&o)[8]) {
+      const int i = i0 + di, j = j0 + dj, have = a.n - j;
+      if (i < a.k && have > 0) put8<float, ALIGNED>(dw + (int64_t)i * a.n + j, have, o);
+    });
+  if (sum) {  // the threads of a column chunk, in order
+    constexpr int C = R / 8;
+    __syncthreads();
+    float* part = (float*)lds;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[threadIdx.x / C * R + threadIdx.x % C * 8 + e] = col[e];
+    __syncthreads();
+    if ((int)threadIdx.x < R && j0 + (int)threadIdx.x < a.n) {
+      float s = 0.f;
+      for (int t = 0; t < 256 / C; ++t) s += part[t * R + threadIdx.x];
+      db[j0 + threadIdx.x] = s;
+    }
   }
 }
 
-__global__ __launch_bounds__(256) void lin_reduce_kernel(LinBwdArgs a) {
-  const int64_t kn = (int64_t)a.k * a.n, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= kn + a.n) return;
-  float s = 0.f;
-  for (int w = 0; w < a.splits; ++w) s += a.part[w * (kn + a.n) + i];
-  if (i < kn) {
-    if (a.dw) a.dw[i] = s;
-  } else if (a.dbias) {
-    a.dbias[i - kn] = s;
+// Sums of the splits' slabs: `slices` threads (a power of two) to 4 consecutive sums, each
+// every slices-th slab, then their sums through LDS, in a fixed order.
+__global__ __launch_bounds__(256) void lin_reduce_kernel(LinBwdArgs a, int slices) {
+  __shared__ f32x4 sum[256];
+  const int cols = 256 / slices, slice = threadIdx.x / cols;
+  const int64_t kn = (int64_t)a.k * a.n, all = kn + a.n, slab = slab_floats(a.k, a.n);
+  const int64_t i = ((int64_t)blockIdx.x * cols + threadIdx.x % cols) * 4;
+  f32x4 s{};
+  if (i < all) {
+#pragma unroll 4
+    for (int w = slice; w < a.splits; w += slices) s += *(const f32x4*)(a.part + w * slab + i);
+  }
+  sum[threadIdx.x] = s;
+  for (int half = slices / 2; half > 0; half >>= 1) {
+    __syncthreads();
+    if (slice < half) sum[threadIdx.x] += sum[threadIdx.x + half * cols];
+  }
+  if (slice > 0) return;
+  s = sum[threadIdx.x];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (i + e < kn) {
+      if (a.dw) a.dw[i + e] = s[e];
+    } else if (i + e < all && a.dbias) {
+      a.dbias[i + e - kn] = s[e];
+    }
   }
 }
+
+bool aligned8(int k, int n) { return k % 8 == 0 && n % 8 == 0; }
+int64_t tiles_of(int64_t m, int64_t n, int r) { return (m + r - 1) / r * ((n + r - 1) / r); }
+
+// 128-wide tiles where there are enough of them for the 256 CUs, else 64-wide ones (four
+// times as many, at half the reuse of an operand).
+bool wide(int64_t tiles128) { return tiles128 >= 256; }
 
 template <typename T>
 hipError_t fwd(const LinArgs& a, hipStream_t s) {
   KernelTimer t(K_LIN_FWD, s);
-  hipLaunchKernelGGL(lin_fwd_kernel<T>, dim3((unsigned)((a.m + 15) / 16), (a.n + 15) / 16),
-                     dim3(256), 0, s, a);
+  const bool big = wide(tiles_of(a.m, a.n, 128)), al = aligned8(a.k, a.n);
+  const dim3 grid((unsigned)tiles_of(a.m, a.n, big ? 128 : 64)), wg(256);
+  if (big && al) hipLaunchKernelGGL((lin_fwd_kernel<T, 128, true>), grid, wg, 0, s, a);
+  else if (big) hipLaunchKernelGGL((lin_fwd_kernel<T, 128, false>), grid, wg, 0, s, a);
+  else if (al) hipLaunchKernelGGL((lin_fwd_kernel<T, 64, true>), grid, wg, 0, s, a);
+  else hipLaunchKernelGGL((lin_fwd_kernel<T, 64, false>), grid, wg, 0, s, a);
   return hipGetLastError();
 }
 
+template <typename T, int R, int DZ, bool AL>
+void bwd_launch(const LinBwdArgs& a, hipStream_t s, bool weights) {
+  if (!weights) {
+    KernelTimer t(K_LIN_BWD_DX, s);
+    hipLaunchKernelGGL((lin_bwd_dx_kernel<T, R, DZ, AL>), dim3((unsigned)tiles_of(a.m, a.k, R)),
+                       dim3(256), 0, s, a);
+  } else {
+    KernelTimer t(K_LIN_BWD_W, s);
+    hipLaunchKernelGGL((lin_bwd_w_kernel<T, R, DZ, AL>),
+                       dim3((unsigned)(tiles_of(a.k, a.n, R) * a.splits)), dim3(256), 0, s, a);
+  }
+}
+template <typename T, int DZ>
+void bwd_tile(const LinBwdArgs& a, hipStream_t s, bool weights, bool big) {
+  const bool al = aligned8(a.k, a.n);
+  if (big && al) bwd_launch<T, 128, DZ, true>(a, s, weights);
+  else if (big) bwd_launch<T, 128, DZ, false>(a, s, weights);
+  else if (al) bwd_launch<T, 64, DZ, true>(a, s, weights);
+  else bwd_launch<T, 64, DZ, false>(a, s, weights);
+}
+template <typename T>
+void bwd_part(const LinBwdArgs& a, hipStream_t s, bool weights, bool big) {
+  if (a.act == TRIATTN_ACT_NONE) return bwd_tile<T, DZ_X>(a, s, weights, big);
+  if constexpr (sizeof(T) == 2) {  // dout where z > 0 is a bf16 value: one plane
+    if (a.act == TRIATTN_ACT_RELU) return bwd_tile<T, DZ_RELU>(a, s, weights, big);
+  }
+  bwd_tile<T, DZ_ACT>(a, s, weights, big);
+}
+
+// Tiles of dW are 128 wide unless k or n would fill no more than half of one.
+bool wide_w(int k, int n) { return k > 64 && n > 64; }
+
 template <typename T>
 hipError_t bwd(const LinBwdArgs& a, hipStream_t s) {
-  if (a.dx) {
-    KernelTimer t(K_LIN_BWD_DX, s);
-    hipLaunchKernelGGL(lin_bwd_dx_kernel<T>, dim3((unsigned)((a.m + 15) / 16), (a.k + 15) / 16),
-                       dim3(256), 0, s, a);
-  }
+  if (a.dx) bwd_part<T>(a, s, false, wide(tiles_of(a.m, a.k, 128)));
   if (a.dw || a.dbias) {
-    {
-      KernelTimer t(K_LIN_BWD_W, s);
-      hipLaunchKernelGGL(lin_bwd_w_kernel<T>,
-                         dim3((a.k + 15) / 16 + 1, (a.n + 15) / 16, a.splits), dim3(256), 0, s, a);
+    bwd_part<T>(a, s, true, wide_w(a.k, a.n));
+    if (a.splits > 1) {
+      KernelTimer t(K_LIN_REDUCE, s);
+      int slices = 1;
+      while (slices < 32 && slices * 4 < a.splits) slices *= 2;
+      const int64_t quads = ((int64_t)a.k * a.n + a.n + 3) / 4, cols = 256 / slices;
+      hipLaunchKernelGGL(lin_reduce_kernel, dim3((unsigned)((quads + cols - 1) / cols)), dim3(256),
+                         0, s, a, slices);
     }
-    KernelTimer t(K_LIN_REDUCE, s);
-    hipLaunchKernelGGL(lin_reduce_kernel,
-                       dim3((unsigned)(((int64_t)a.k * a.n + a.n + 255) / 256)), dim3(256), 0, s,
-                       a);
   }
   return hipGetLastError();
 }
 
 }  // namespace
 
-int lin_bwd_splits(int, int64_t m, int, int) { return (int)((m + 511) / 512 < 128 ? (m + 511) / 512 : 128); }
+// Splits of the rows for dW: enough workgroups for two rounds of the 256 CUs, each of at
+// least 128 rows.
+int lin_bwd_splits(int, int64_t m, int k, int n) {
+  const int64_t tiles = tiles_of(k, n, wide_w(k, n) ? 128 : 64);
+  int64_t s = 512 / tiles, most = (m + 127) / 128;
+  if (s > most) s = most;
+  if (s < 1) s = 1;
+  const int64_t per = split_rows(m, (int)s);
+  return (int)((m + per - 1) / per);  // no split without rows
+}
+size_t lin_bwd_ws(int dtype, int64_t m, int k, int n) {
+  const int s = lin_bwd_splits(dtype, m, k, n);
+  return s > 1 ? (size_t)s * (size_t)slab_floats(k, n) * sizeof(float) : 256;
+}
 
 hipError_t launch_lin_fwd(int dtype, const LinArgs& a, hipStream_t s) {
   return dtype == TRIATTN_BF16 ? fwd<bf16>(a, s) : fwd<float>(a, s);

@@ -56,10 +56,11 @@ int rel_check(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges) {
                                                                      : TRIATTN_OK;
 }
 
-// The workspace does not depend on whether there are chains: the larger table counts.
-size_t rel_ws(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges) {
-  return round256((size_t)triattn::rel_bwd_parts(dtype, batch, n, (int)h) * (size_t)(n_edges + 2) *
-                  (size_t)h * sizeof(float));
+// The workspace does not depend on whether there are chains: the larger need counts.
+size_t rel_ws(int64_t batch, int64_t n, int64_t h, int n_edges) {
+  const size_t one = triattn::rel_bwd_ws(batch, (int)n, (int)h, n_edges + 1);
+  const size_t two = triattn::rel_bwd_ws(batch, (int)n, (int)h, n_edges + 2);
+  return round256(one > two ? one : two);
 }
 
 int rel_args(int64_t batch, int64_t n, int64_t h, int n_edges, const int32_t* edges,
@@ -224,7 +225,7 @@ int tri_rel_bias_bwd_workspace_bytes(int dtype, int64_t batch, int64_t n, int64_
   const int st = rel_check(dtype, batch, n, h, n_edges);
   if (st != TRIATTN_OK) return st;
   if (bytes == nullptr) return TRIATTN_ERR_INVALID_ARG;
-  *bytes = rel_ws(dtype, batch, n, h, n_edges);
+  *bytes = rel_ws(batch, n, h, n_edges);
   return TRIATTN_OK;
 }
 
@@ -240,12 +241,11 @@ int tri_rel_bias_bwd(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges
   if (bad_pointers({(const void*)dout, (const void*)dtable}, {(const void*)nullptr}))
     return TRIATTN_ERR_INVALID_ARG;
   if (workspace == nullptr || !aligned16(workspace) ||
-      workspace_bytes < rel_ws(dtype, batch, n, h, n_edges))
+      workspace_bytes < rel_ws(batch, n, h, n_edges))
     return TRIATTN_ERR_WORKSPACE;
   a.dout = dout;
   a.dtable = dtable;
   a.part = (float*)workspace;
-  a.nwg = triattn::rel_bwd_parts(dtype, batch, n, (int)h);
   return launched(triattn::launch_rel_bwd(dtype, a, (hipStream_t)stream));
 }
 

@@ -245,6 +245,9 @@ hipError_t launch_lin_bwd(int dtype, const LinBwdArgs& a, hipStream_t s);
 constexpr int REL_MAX_EDGES = 255;
 constexpr int REL_MAX_H = 256;
 
+// Differences the edges may span to be looked up by difference, in bytes of the arguments.
+constexpr int REL_LUT = 2048;
+
 struct RelArgs {
   int64_t batch;
   int n, h;
@@ -254,12 +257,16 @@ struct RelArgs {
   void* out;                  // [batch][n][n][h]
   const void* dout;           // backward
   float* dtable;              // backward: [rows][h]
-  float* part;                // backward, workspace: [nwg][rows][h] partial sums
-  int nwg;
-  int32_t edges[REL_MAX_EDGES + 1];
+  float* part;                // backward, workspace: slabs of [rows][h] partial sums
+  uint32_t inv_h;             // 2^32 / h rounded up (0 for h = 1)
+  int32_t low, span;          // lut: differences low .. low + span
+  union {
+    int32_t edges[REL_MAX_EDGES + 1];
+    uint8_t lut[REL_LUT];     // bucket of difference low + i
+  };
 };
 
-int rel_bwd_parts(int dtype, int64_t batch, int64_t n, int h);
+size_t rel_bwd_ws(int64_t batch, int n, int h, int rows);  // bytes of workspace
 hipError_t launch_rel_fwd(int dtype, const RelArgs& a, hipStream_t s);
 hipError_t launch_rel_bwd(int dtype, const RelArgs& a, hipStream_t s);
 

@@ -14,6 +14,7 @@
 // The variance is the mean square of the deviations from the mean (the row is at hand),
 // not a difference of squares, which would lose what a row far from zero has of it.
 #include "kernels.h"
+#include "slabs.h"
 #include "timing.h"
 #include "triattn.h"
 
@@ -264,25 +265,13 @@ __global__ __launch_bounds__(LN_WG) void ln_bwd_kernel(LnBwdArgs a) {
     }
 }
 
-// Column sums of the slabs [nwg][2 c]: 16 columns per workgroup, 64 threads to a column,
-// each every 64th slab, then their sums in LDS (a fixed order).
-__global__ __launch_bounds__(1024) void ln_reduce_kernel(const float* part, int nwg, int c,
-                                                         float* dgamma, float* dbeta) {
-  __shared__ float sum[64][17];
-  const int col = threadIdx.x & 15, k = threadIdx.x >> 4, i = blockIdx.x * 16 + col;
-  float s = 0.f;
-  if (i < 2 * c) {
-#pragma unroll 8
-    for (int w = k; w < nwg; w += 64) s += part[(int64_t)w * 2 * c + i];
-  }
-  sum[k][col] = s;
-  for (int half = 32; half > 0; half >>= 1) {
-    __syncthreads();
-    if (k < half) sum[k][col] += sum[k + half][col];
-  }
-  if (k > 0 || i >= 2 * c) return;
+__global__ __launch_bounds__(SLAB_WG) void ln_reduce_kernel(const float* part, int nwg, int c,
+                                                            float* dgamma, float* dbeta) {
+  const float s = slab_column_sum(part, nwg, 2 * c, 2 * c);
+  const int i = blockIdx.x * SLAB_COLS + threadIdx.x;
+  if (threadIdx.x >= SLAB_COLS || i >= 2 * c) return;
   float* out = i < c ? dgamma : dbeta;
-  if (out) out[i < c ? i : i - c] = sum[0][col];
+  if (out) out[i < c ? i : i - c] = s;
 }
 
 // Lanes a row of `chunks` 16-byte chunks takes: the fewest chunks a lane with no more
@@ -358,7 +347,7 @@ hipError_t bwd(const LnBwdArgs& a, hipStream_t s) {
   }
   if (weights) {
     KernelTimer t(K_LN_REDUCE, s);
-    hipLaunchKernelGGL(ln_reduce_kernel, dim3((2 * a.c + 15) / 16), dim3(1024), 0, s, a.part,
+    hipLaunchKernelGGL(ln_reduce_kernel, dim3(slab_grid(2 * a.c)), dim3(SLAB_WG), 0, s, a.part,
                        a.nwg, a.c, a.dgamma, a.dbeta);
   }
   return hipGetLastError();

@@ -1,107 +1,334 @@
 // Learned relative position bias by buckets, and the gradient of its table.
+//
+// A pair's bucket is the number of edges at or below the difference of its positions.
+// Where the edges span fewer than REL_LUT differences (a clipped difference and buckets
+// that widen up to a thousand tokens do), the host turns them into a table of buckets by
+// difference, one LDS read a pair; edges further apart are searched, eight dependent LDS
+// reads a pair.  Both forms travel in the kernel's arguments.
+#include <limits.h>
+
 #include "kernels.h"
+#include "slabs.h"
 #include "timing.h"
 #include "triattn.h"
 
 namespace triattn {
 namespace {
 
-// Number of edges at or below d (edges ascending, in LDS).
-__device__ inline int bucket_of(const int32_t* edges, int ne, int64_t d) {
-  int lo = 0, hi = ne;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (edges[mid] <= d) lo = mid + 1;
-    else hi = mid;
+struct Buckets {
+  const uint8_t* lut;    // LDS: bucket of difference low + i
+  const int32_t* edges;  // LDS
+};
+
+// Copies the arguments' buckets to LDS (2 KB).
+template <bool LUT>
+__device__ inline Buckets load_buckets(const RelArgs& a, uint32_t* lds) {
+  const uint32_t* src = (const uint32_t*)(LUT ? (const void*)a.lut : (const void*)a.edges);
+  const int words = LUT ? a.span / 4 + 1 : a.ne;
+  for (int i = threadIdx.x; i < words; i += blockDim.x) lds[i] = src[i];
+  return Buckets{(const uint8_t*)lds, (const int32_t*)lds};
+}
+
+// Bucket of position pq less pk.  The difference may need 33 bits: LUT saturates it,
+// which keeps its order against any edge above -2^31 (the host sees to that); the search
+// takes it in 64.
+template <bool LUT>
+__device__ inline int bucket_of(const RelArgs& a, const Buckets& b, int32_t pq, int32_t pk) {
+  if constexpr (LUT) {
+    const int32_t d = __builtin_elementwise_sub_sat(
+        __builtin_elementwise_sub_sat(pq, pk), a.low);
+    return b.lut[min(max(d, 0), a.span)];
+  } else {
+    const int64_t d = (int64_t)pq - (int64_t)pk;
+    int lo = 0, hi = a.ne;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (b.edges[mid] <= d) lo = mid + 1;
+      else hi = mid;
+    }
+    return lo;
   }
-  return lo;
 }
 
-__device__ inline int pair_bucket(const RelArgs& a, const int32_t* edges, int64_t q, int64_t k) {
-  if (a.chain && a.chain[q] != a.chain[k]) return a.ne + 1;
-  return bucket_of(edges, a.ne, (int64_t)a.pos[q] - (int64_t)a.pos[k]);
+// Value of a row's uniform index, by a scalar load (the arrays are only read here).
+__device__ inline int32_t uniform(const int32_t* p, int64_t i) {
+  return *(const __attribute__((address_space(4))) int32_t*)(p + i);
 }
 
-template <typename T>
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+struct __attribute__((packed)) Any16 {
+  u32x4 v;
+};
+
+// Forward.  Bound by the write of the result (and the read of base).  A wave takes 64 U
+// consecutive 16-byte chunks of one query's row; P elements of a chunk (P divides the
+// chunk and h) belong to one pair and take one bucket and one read of the table, which
+// lies in LDS if it has room.  Rows need not start at 16 bytes; a row's last, partial
+// chunk goes element by element.
+constexpr int REL_U = 2;
+template <typename T, int P, bool LUT, bool LDS_TABLE>
 __global__ __launch_bounds__(256) void rel_fwd_kernel(RelArgs a) {
-  __shared__ int32_t edges[REL_MAX_EDGES + 1];
-  if ((int)threadIdx.x < a.ne) edges[threadIdx.x] = a.edges[threadIdx.x];
+  constexpr int N = 16 / (int)sizeof(T);
+  struct Piece {
+    T x[P];
+  };
+  struct Elems {
+    T x[N];
+  };
+  __shared__ uint32_t words[REL_LUT / 4];
+  extern __shared__ __attribute__((aligned(16))) char table_lds[];
+  const Buckets buckets = load_buckets<LUT>(a, words);
+  const T* table = (const T*)a.table;
+  if (LDS_TABLE) {
+    T* t = (T*)table_lds;
+    for (int i = threadIdx.x; i < a.rows * a.h; i += 256) t[i] = table[i];
+    table = t;
+  }
   __syncthreads();
-  const int64_t total = a.batch * a.n * a.n * a.h;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total;
-       i += (int64_t)gridDim.x * 256) {
-    const int64_t pair = i / a.h, row = pair / a.n, b = row / a.n;
-    const int c = (int)(i - pair * a.h);
-    const int r = pair_bucket(a, edges, row, b * a.n + (pair - row * a.n));
-    float o = (float)((const T*)a.table)[r * a.h + c];
-    if (a.base) o += (float)((const T*)a.base)[i];
-    ((T*)a.out)[i] = (T)o;
+  const int len = a.n * a.h, chunks = (len + N - 1) / N;
+  const int segs = (chunks + 64 * REL_U - 1) / (64 * REL_U), lane = threadIdx.x & 63;
+  const int64_t tasks = a.batch * a.n * segs;
+  for (int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); task < tasks;
+       task += (int64_t)gridDim.x * 4) {
+    const int64_t row = task / segs, b0 = row / a.n * a.n;  // row b n + q; its sample's first
+    const int seg = (int)(task - row * segs);
+    const int32_t pq = a.pos[row], cq = a.chain ? a.chain[row] : 0;
+    const T* base = a.base ? (const T*)a.base + row * len : nullptr;
+    T* out = (T*)a.out + row * len;
+#pragma unroll
+    for (int u = 0; u < REL_U; ++u) {
+      const int e0 = ((seg * REL_U + u) * 64 + lane) * N;
+      if (e0 >= len) continue;
+      const bool whole = e0 + N <= len;
+      Elems add{}, o;
+      if (base) {
+        if (whole) {
+          add = __builtin_bit_cast(Elems, *(const Any16*)(base + e0));
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (e0 + e < len) add.x[e] = base[e0 + e];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < N; e += P) {
+        const unsigned at = min(e0 + e, len - P);  // a piece past the row is not stored
+        const int k = a.inv_h ? (int)__umulhi(at, a.inv_h) : (int)at;
+        int r = bucket_of<LUT>(a, buckets, pq, a.pos[b0 + k]);
+        if (a.chain && a.chain[b0 + k] != cq) r = a.ne + 1;
+        const Piece t = *(const Piece*)(table + r * a.h + ((int)at - k * a.h));
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+          o.x[e + i] = base ? (T)((float)t.x[i] + (float)add.x[e + i]) : t.x[i];
+      }
+      if (whole) {
+        *(Any16*)(out + e0) = __builtin_bit_cast(Any16, o);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (e0 + e < len) out[e0 + e] = o.x[e];
+      }
+    }
   }
 }
 
-// Workgroup (stretch of query rows, 64 channels): one thread per channel adds its pairs
-// into its own column of the LDS sums.
+// Backward: sums over the pairs of a bucket, for any positions in any order.
+//
+// A lane belongs to one channel (lane = pair offset * h + channel for h <= 64; 64 channels
+// of one pair at a time above) and adds its values into its own column of the wave's LDS
+// sums [rows][64]: no two lanes share a sum, so nothing depends on the order lanes run in,
+// no atomics are needed, and a wave's lanes never meet in an LDS bank.  A read, an add and
+// a write take 14 cycles a wave and CU with the lookup before them (8 waves in turn); the
+// LDS's own fp32 add, although nothing waits for it, takes 200.  A wave keeps its keys
+// (positions in registers) and walks over query rows.  At the end the workgroup adds its lanes' and waves' columns in a fixed
+// order into its slab, and rel_reduce_kernel the slabs.
+constexpr int REL_K = 4;  // key groups of a wave
+constexpr int REL_Q = 4;  // query rows whose loads are in flight together
+
+// Geometry of the backward, from the sizes alone.
+struct RelPlan {
+  int hc;      // channels of a wave: min(h, 64)
+  int groups;  // channel groups of 64
+  int pl;      // pairs of a wave's load
+  int waves;   // waves of a workgroup: what leaves their sums 64 KB of LDS, or half of it
+  int kblocks; // workgroups along the keys
+  int units;   // row chunks of a sample
+  int qlen;    // rows of a chunk
+  int w;       // workgroups that share a key block's units
+  int slabs() const { return w * kblocks; }
+};
+
+__host__ __device__ inline RelPlan rel_plan(int64_t batch, int n, int h, int rows) {
+  RelPlan p;
+  p.hc = h < 64 ? h : 64;
+  p.groups = (h + 63) / 64;
+  p.pl = 64 / p.hc;
+  p.waves = rows <= 64 + 8 ? 4 : rows <= 128 + 8 ? 2 : 1;
+  const int keys = p.pl * REL_K * p.waves;
+  p.kblocks = (n + keys - 1) / keys;
+  // about two workgroups a CU, and at least 16 rows to each (its sums are cleared and
+  // added up once)
+  int64_t want = 512 / (p.groups * p.kblocks);
+  if (want < 1) want = 1;
+  int64_t per = (batch * n + want - 1) / want;
+  if (per < 16) per = 16;
+  p.qlen = (int)(per < n ? per : n);
+  p.units = (n + p.qlen - 1) / p.qlen;
+  const int64_t all = batch * p.units;
+  p.w = (int)(all < want ? all : want);
+  return p;
+}
+
+template <typename T, bool LUT>
+__global__ __launch_bounds__(256) void rel_bwd_kernel(RelArgs a, RelPlan p) {
+  __shared__ uint32_t words[REL_LUT / 4];
+  extern __shared__ __attribute__((aligned(16))) float sums[];  // [waves][rows][64]
+  const Buckets buckets = load_buckets<LUT>(a, words);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float* mine = sums + wave * a.rows * 64;
+  for (int i = 4 * lane; i < a.rows * 64; i += 256) *(f32x4*)(mine + i) = f32x4{};
+  __syncthreads();
+  const int kb = blockIdx.x % p.kblocks, w = blockIdx.x / p.kblocks, c0 = blockIdx.y * 64;
+  const int off = lane / p.hc, c = c0 + lane % p.hc;
+  const int k0 = (kb * p.waves + wave) * p.pl * REL_K + off;
+  const bool lane_in = off < p.pl && c < a.h;
+  float* column = mine + lane;
+  for (int64_t unit = w; unit < a.batch * p.units; unit += p.w) {
+    const int64_t b0 = unit / p.units * a.n;  // the sample's first row
+    const int q0 = (int)(unit % p.units) * p.qlen, q1 = min(q0 + p.qlen, a.n);
+    int32_t pk[REL_K], ck[REL_K];
+    bool in[REL_K];
+#pragma unroll
+    for (int u = 0; u < REL_K; ++u) {
+      const int k = k0 + u * p.pl;
+      in[u] = lane_in && k < a.n;
+      pk[u] = in[u] ? a.pos[b0 + k] : 0;
+      ck[u] = in[u] && a.chain ? a.chain[b0 + k] : 0;
+    }
+    for (int q = q0; q < q1; q += REL_Q) {
+      T x[REL_Q][REL_K];
+#pragma unroll
+      for (int v = 0; v < REL_Q; ++v) {
+        const int qq = min(q + v, q1 - 1);
+        const T* src = (const T*)a.dout + (b0 + qq) * a.n * a.h + (int64_t)k0 * a.h + c;
+#pragma unroll
+        for (int u = 0; u < REL_K; ++u)
+          if (in[u]) x[v][u] = src[u * p.pl * a.h];
+      }
+#pragma unroll
+      for (int v = 0; v < REL_Q; ++v) {
+        if (q + v >= q1) break;
+        const int32_t pq = uniform(a.pos, b0 + q + v);
+        const int32_t cq = a.chain ? uniform(a.chain, b0 + q + v) : 0;
+#pragma unroll
+        for (int u = 0; u < REL_K; ++u) {
+          int r = bucket_of<LUT>(a, buckets, pq, pk[u]);
+          if (a.chain && ck[u] != cq) r = a.ne + 1;
+          if (in[u]) column[r * 64] += (float)x[v][u];
+        }
+      }
+    }
+  }
+  __syncthreads();
+  // channel c of row r: the lanes off * hc + c of every wave, beginning at another one in
+  // every row so that the rows' reads fall into different banks
+  float* slab = a.part + (int64_t)blockIdx.x * a.rows * a.h;
+  for (int i = threadIdx.x; i < a.rows * p.hc; i += blockDim.x) {
+    const int r = i / p.hc, ch = i - r * p.hc;
+    if (c0 + ch >= a.h) continue;
+    float s = 0.f;
+    int at = r % p.pl;
+    for (int t = 0; t < p.pl; ++t) {
+      for (int v = 0; v < p.waves; ++v) s += sums[(v * a.rows + r) * 64 + at * p.hc + ch];
+      at = at + 1 == p.pl ? 0 : at + 1;
+    }
+    slab[r * a.h + c0 + ch] = s;
+  }
+}
+
+__global__ __launch_bounds__(SLAB_WG) void rel_reduce_kernel(const float* part, int count,
+                                                             int total, float* dtable) {
+  const float s = slab_column_sum(part, count, total, total);
+  const int i = blockIdx.x * SLAB_COLS + threadIdx.x;
+  if (threadIdx.x < SLAB_COLS && i < total) dtable[i] = s;
+}
+
+// Fills in how buckets are found.  False: by search.
+bool use_lut(RelArgs& a) {
+  int32_t edges[REL_MAX_EDGES];
+  const int64_t span = (int64_t)a.edges[a.ne - 1] - a.edges[0] + 1;
+  if (a.edges[0] == INT_MIN || span >= REL_LUT) return false;
+  for (int i = 0; i < a.ne; ++i) edges[i] = a.edges[i];
+  a.low = edges[0] - 1;
+  a.span = (int32_t)span;  // difference low + span is the last edge
+  a.lut[0] = 0;
+  for (int i = 0; i < a.ne; ++i) {
+    const int from = edges[i] - a.low, to = i + 1 < a.ne ? edges[i + 1] - a.low : a.span + 1;
+    for (int d = from; d < to; ++d) a.lut[d] = (uint8_t)(i + 1);
+  }
+  return true;
+}
+
+constexpr size_t REL_LDS_TABLE = 32 << 10;
+
+template <typename T, int P>
+void fwd_piece(const RelArgs& a, bool lut, unsigned grid, hipStream_t s) {
+  const size_t table = (size_t)a.rows * a.h * sizeof(T);
+  const dim3 g(grid), wg(256);
+  if (table <= REL_LDS_TABLE) {
+    if (lut) hipLaunchKernelGGL((rel_fwd_kernel<T, P, true, true>), g, wg, table, s, a);
+    else hipLaunchKernelGGL((rel_fwd_kernel<T, P, false, true>), g, wg, table, s, a);
+  } else {
+    if (lut) hipLaunchKernelGGL((rel_fwd_kernel<T, P, true, false>), g, wg, 0, s, a);
+    else hipLaunchKernelGGL((rel_fwd_kernel<T, P, false, false>), g, wg, 0, s, a);
+  }
+}
+
 template <typename T>
-__global__ __launch_bounds__(64) void rel_bwd_kernel(RelArgs a) {
-  __shared__ int32_t edges[REL_MAX_EDGES + 1];
-  __shared__ float sum[REL_MAX_EDGES + 2][64];
-  for (int i = threadIdx.x; i < a.ne; i += 64) edges[i] = a.edges[i];
-  for (int r = 0; r < a.rows; ++r) sum[r][threadIdx.x] = 0.f;
-  __syncthreads();
-  const int c = blockIdx.y * 64 + threadIdx.x;
-  if (c >= a.h) return;
-  const int64_t nrow = a.batch * a.n, per = (nrow + a.nwg - 1) / a.nwg;
-  const int64_t r0 = blockIdx.x * per, r1 = min(nrow, r0 + per);
-  for (int64_t row = r0; row < r1; ++row) {
-    const int64_t b = row / a.n;
-    for (int k = 0; k < a.n; ++k)
-      sum[pair_bucket(a, edges, row, b * a.n + k)][threadIdx.x] +=
-          (float)((const T*)a.dout)[(row * a.n + k) * a.h + c];
-  }
-  for (int r = 0; r < a.rows; ++r)
-    a.part[((int64_t)blockIdx.x * a.rows + r) * a.h + c] = sum[r][threadIdx.x];
+hipError_t fwd(RelArgs a, hipStream_t s) {
+  KernelTimer t(K_REL_FWD, s);
+  const bool lut = use_lut(a);
+  a.inv_h = a.h == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + a.h - 1) / a.h);
+  const int64_t chunks = ((int64_t)a.n * a.h * sizeof(T) + 15) / 16;
+  const int64_t wgs = (a.batch * a.n * ((chunks + 64 * REL_U - 1) / (64 * REL_U)) + 3) / 4;
+  const unsigned grid = (unsigned)(wgs < 256 * 8 ? wgs : 256 * 8);
+  constexpr int N = 16 / (int)sizeof(T);
+  if (a.h % N == 0) fwd_piece<T, N>(a, lut, grid, s);
+  else if (N > 4 && a.h % 4 == 0) fwd_piece<T, 4>(a, lut, grid, s);
+  else if (a.h % 2 == 0) fwd_piece<T, 2>(a, lut, grid, s);
+  else fwd_piece<T, 1>(a, lut, grid, s);
+  return hipGetLastError();
 }
 
-__global__ __launch_bounds__(256) void rel_reduce_kernel(const float* part, int nwg, int total,
-                                                         float* dtable) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= total) return;
-  float s = 0.f;
-  for (int w = 0; w < nwg; ++w) s += part[(int64_t)w * total + i];
-  dtable[i] = s;
+template <typename T>
+hipError_t bwd(RelArgs a, hipStream_t s) {
+  const RelPlan p = rel_plan(a.batch, a.n, a.h, a.rows);
+  const bool lut = use_lut(a);
+  {
+    KernelTimer t(K_REL_BWD, s);
+    const dim3 grid((unsigned)p.slabs(), (unsigned)p.groups), wg(64 * p.waves);
+    const size_t lds = (size_t)p.waves * a.rows * 64 * sizeof(float);
+    if (lut) hipLaunchKernelGGL((rel_bwd_kernel<T, true>), grid, wg, lds, s, a, p);
+    else hipLaunchKernelGGL((rel_bwd_kernel<T, false>), grid, wg, lds, s, a, p);
+  }
+  KernelTimer t(K_REL_REDUCE, s);
+  const int total = a.rows * a.h;
+  hipLaunchKernelGGL(rel_reduce_kernel, dim3(slab_grid(total)), dim3(SLAB_WG), 0, s, a.part,
+                     p.slabs(), total, a.dtable);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-int rel_bwd_parts(int, int64_t batch, int64_t n, int) {
-  return (int)(batch * n < 512 ? batch * n : 512);
+size_t rel_bwd_ws(int64_t batch, int n, int h, int rows) {
+  return (size_t)rel_plan(batch, n, h, rows).slabs() * (size_t)rows * h * sizeof(float);
 }
 
 hipError_t launch_rel_fwd(int dtype, const RelArgs& a, hipStream_t s) {
-  KernelTimer t(K_REL_FWD, s);
-  const int64_t wgs = (a.batch * a.n * a.n * a.h + 255) / 256;
-  const dim3 grid((unsigned)(wgs < 16384 ? wgs : 16384));
-  if (dtype == TRIATTN_BF16)
-    hipLaunchKernelGGL(rel_fwd_kernel<bf16>, grid, dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL(rel_fwd_kernel<float>, grid, dim3(256), 0, s, a);
-  return hipGetLastError();
+  return dtype == TRIATTN_BF16 ? fwd<bf16>(a, s) : fwd<float>(a, s);
 }
-
 hipError_t launch_rel_bwd(int dtype, const RelArgs& a, hipStream_t s) {
-  {
-    KernelTimer t(K_REL_BWD, s);
-    const dim3 grid(a.nwg, (a.h + 63) / 64);
-    if (dtype == TRIATTN_BF16)
-      hipLaunchKernelGGL(rel_bwd_kernel<bf16>, grid, dim3(64), 0, s, a);
-    else
-      hipLaunchKernelGGL(rel_bwd_kernel<float>, grid, dim3(64), 0, s, a);
-  }
-  KernelTimer t(K_REL_REDUCE, s);
-  const int total = a.rows * a.h;
-  hipLaunchKernelGGL(rel_reduce_kernel, dim3((total + 255) / 256), dim3(256), 0, s, a.part, a.nwg,
-                     total, a.dtable);
-  return hipGetLastError();
+  return dtype == TRIATTN_BF16 ? bwd<bf16>(a, s) : bwd<float>(a, s);
 }
 
 }  // namespace triattn

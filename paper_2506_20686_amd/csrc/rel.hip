@@ -7,6 +7,7 @@
 // reads a pair.  Both forms travel in the kernel's arguments.
 #include <limits.h>
 
+#include "dma.h"
 #include "kernels.h"
 #include "slabs.h"
 #include "timing.h"
@@ -166,12 +167,11 @@ __host__ __device__ inline RelPlan rel_plan(int64_t batch, int n, int h, int row
   p.waves = rows <= 64 + 8 ? 4 : rows <= 128 + 8 ? 2 : 1;
   const int keys = p.pl * REL_K * p.waves;
   p.kblocks = (n + keys - 1) / keys;
-  // about two workgroups a CU, and at least 16 rows to each (its sums are cleared and
-  // added up once)
+  // about two workgroups a CU, and at least 4 rows to each
   int64_t want = 512 / (p.groups * p.kblocks);
   if (want < 1) want = 1;
   int64_t per = (batch * n + want - 1) / want;
-  if (per < 16) per = 16;
+  if (per < REL_Q) per = REL_Q;
   p.qlen = (int)(per < n ? per : n);
   p.units = (n + p.qlen - 1) / p.qlen;
   const int64_t all = batch * p.units;
@@ -179,7 +179,15 @@ __host__ __device__ inline RelPlan rel_plan(int64_t batch, int n, int h, int row
   return p;
 }
 
-template <typename T, bool LUT>
+// One element by a buffer load (zero past the resource).
+__device__ inline float load_one(rsrc_t r, uint32_t off, bf16) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b16(r, (int)off, 0, 0) << 16);
+}
+__device__ inline float load_one(rsrc_t r, uint32_t off, float) {
+  return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (int)off, 0, 0));
+}
+
+template <typename T, bool LUT, bool CHAIN>
 __global__ __launch_bounds__(256) void rel_bwd_kernel(RelArgs a, RelPlan p) {
   __shared__ uint32_t words[REL_LUT / 4];
   extern __shared__ __attribute__((aligned(16))) float sums[];  // [waves][rows][64]
@@ -191,41 +199,73 @@ __global__ __launch_bounds__(256) void rel_bwd_kernel(RelArgs a, RelPlan p) {
   const int kb = blockIdx.x % p.kblocks, w = blockIdx.x / p.kblocks, c0 = blockIdx.y * 64;
   const int off = lane / p.hc, c = c0 + lane % p.hc;
   const int k0 = (kb * p.waves + wave) * p.pl * REL_K + off;
-  const bool lane_in = off < p.pl && c < a.h;
+  const uint32_t row_bytes = (uint32_t)(a.n * a.h) * sizeof(T);  // at most 8 MB
+  // lanes without a channel and keys past the last read zeros (and add them to a sum of
+  // their own column)
+  int key[REL_K];
+  uint32_t at[REL_K];
+#pragma unroll
+  for (int u = 0; u < REL_K; ++u) {
+    const int k = k0 + u * p.pl;
+    const bool in = off < p.pl && c < a.h && k < a.n;
+    key[u] = in ? k : 0;
+    at[u] = in ? (uint32_t)(k * a.h + c) * sizeof(T) : 0x80000000u;
+  }
   float* column = mine + lane;
   for (int64_t unit = w; unit < a.batch * p.units; unit += p.w) {
     const int64_t b0 = unit / p.units * a.n;  // the sample's first row
     const int q0 = (int)(unit % p.units) * p.qlen, q1 = min(q0 + p.qlen, a.n);
     int32_t pk[REL_K], ck[REL_K];
-    bool in[REL_K];
 #pragma unroll
     for (int u = 0; u < REL_K; ++u) {
-      const int k = k0 + u * p.pl;
-      in[u] = lane_in && k < a.n;
-      pk[u] = in[u] ? a.pos[b0 + k] : 0;
-      ck[u] = in[u] && a.chain ? a.chain[b0 + k] : 0;
+      pk[u] = a.pos[b0 + key[u]];
+      ck[u] = CHAIN ? a.chain[b0 + key[u]] : 0;
     }
-    for (int q = q0; q < q1; q += REL_Q) {
-      T x[REL_Q][REL_K];
+    float x[REL_Q][REL_K];
+    auto load = [&](int q) {  // rows past the chunk give zeros
 #pragma unroll
       for (int v = 0; v < REL_Q; ++v) {
-        const int qq = min(q + v, q1 - 1);
-        const T* src = (const T*)a.dout + (b0 + qq) * a.n * a.h + (int64_t)k0 * a.h + c;
+        const rsrc_t row = buf_rsrc_n((const char*)a.dout + (b0 + q + v) * row_bytes,
+                                      q + v < q1 ? row_bytes : 0u);
 #pragma unroll
-        for (int u = 0; u < REL_K; ++u)
-          if (in[u]) x[v][u] = src[u * p.pl * a.h];
+        for (int u = 0; u < REL_K; ++u) x[v][u] = load_one(row, at[u], T());
       }
+    };
+    load(q0);
+    for (int q = q0; q < q1; q += REL_Q) {
+      int r[REL_Q][REL_K];
 #pragma unroll
       for (int v = 0; v < REL_Q; ++v) {
-        if (q + v >= q1) break;
-        const int32_t pq = uniform(a.pos, b0 + q + v);
-        const int32_t cq = a.chain ? uniform(a.chain, b0 + q + v) : 0;
+        const int64_t row = b0 + min(q + v, q1 - 1);
+        const int32_t pq = uniform(a.pos, row), cq = CHAIN ? uniform(a.chain, row) : 0;
 #pragma unroll
         for (int u = 0; u < REL_K; ++u) {
-          int r = bucket_of<LUT>(a, buckets, pq, pk[u]);
-          if (a.chain && ck[u] != cq) r = a.ne + 1;
-          if (in[u]) column[r * 64] += (float)x[v][u];
+          r[v][u] = bucket_of<LUT>(a, buckets, pq, pk[u]);
+          if (CHAIN && ck[u] != cq) r[v][u] = a.ne + 1;
         }
+      }
+      float f[REL_Q][REL_K];
+#pragma unroll
+      for (int v = 0; v < REL_Q; ++v)
+#pragma unroll
+        for (int u = 0; u < REL_K; ++u) f[v][u] = x[v][u];
+      load(q + REL_Q);
+      // four elements of a row at a time: their sums are read together; one that falls
+      // into an earlier one's bucket goes on from that one's new value, and the last
+      // write of a bucket is the one that stays
+#pragma unroll
+      for (int v = 0; v < REL_Q; ++v) {
+        float s[REL_K];
+#pragma unroll
+        for (int u = 0; u < REL_K; ++u) s[u] = column[r[v][u] * 64];
+#pragma unroll
+        for (int u = 0; u < REL_K; ++u) {
+#pragma unroll
+          for (int e = 0; e < u; ++e) s[u] = r[v][e] == r[v][u] ? s[e] : s[u];
+          s[u] += f[v][u];
+        }
+#pragma unroll
+        for (int u = 0; u < REL_K; ++u) column[r[v][u] * 64] = s[u];
       }
     }
   }
@@ -237,10 +277,14 @@ __global__ __launch_bounds__(256) void rel_bwd_kernel(RelArgs a, RelPlan p) {
     const int r = i / p.hc, ch = i - r * p.hc;
     if (c0 + ch >= a.h) continue;
     float s = 0.f;
-    int at = r % p.pl;
-    for (int t = 0; t < p.pl; ++t) {
-      for (int v = 0; v < p.waves; ++v) s += sums[(v * a.rows + r) * 64 + at * p.hc + ch];
-      at = at + 1 == p.pl ? 0 : at + 1;
+    const int first = r % p.pl;
+    for (int v = 0; v < p.waves; ++v) {
+      const float* row = sums + (v * a.rows + r) * 64 + ch;
+#pragma unroll 8
+      for (int t = 0; t < p.pl; ++t) {
+        const int at = first + t;
+        s += row[(at < p.pl ? at : at - p.pl) * p.hc];
+      }
     }
     slab[r * a.h + c0 + ch] = s;
   }
@@ -308,8 +352,10 @@ hipError_t bwd(RelArgs a, hipStream_t s) {
     KernelTimer t(K_REL_BWD, s);
     const dim3 grid((unsigned)p.slabs(), (unsigned)p.groups), wg(64 * p.waves);
     const size_t lds = (size_t)p.waves * a.rows * 64 * sizeof(float);
-    if (lut) hipLaunchKernelGGL((rel_bwd_kernel<T, true>), grid, wg, lds, s, a, p);
-    else hipLaunchKernelGGL((rel_bwd_kernel<T, false>), grid, wg, lds, s, a, p);
+    if (lut && a.chain) hipLaunchKernelGGL((rel_bwd_kernel<T, true, true>), grid, wg, lds, s, a, p);
+    else if (lut) hipLaunchKernelGGL((rel_bwd_kernel<T, true, false>), grid, wg, lds, s, a, p);
+    else if (a.chain) hipLaunchKernelGGL((rel_bwd_kernel<T, false, true>), grid, wg, lds, s, a, p);
+    else hipLaunchKernelGGL((rel_bwd_kernel<T, false, false>), grid, wg, lds, s, a, p);
   }
   KernelTimer t(K_REL_REDUCE, s);
   const int total = a.rows * a.h;

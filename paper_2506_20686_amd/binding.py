@@ -8,6 +8,7 @@ kernels; there is no fallback path.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import math
 import os
@@ -344,12 +345,12 @@ def tri_linear_bwd(dtype, m, k, n, act, x, w, z, dout, dx, dw, dbias, workspace,
 
 def _edges_arr(edges):
     try:
-        values = [int(e) for e in edges]
-    except (TypeError, ValueError) as e:
+        values = array.array("i", edges)  # 32 bits; checks every value
+    except OverflowError as e:
+        raise ValueError("edges must fit 32 bits") from e
+    except TypeError as e:
         raise TypeError("edges must be a sequence of integers") from e
-    if values and not (-(1 << 31) <= min(values) and max(values) < 1 << 31):
-        raise ValueError("edges must fit 32 bits")
-    return (ctypes.c_int32 * len(values))(*values)
+    return (ctypes.c_int32 * len(values)).from_buffer(values)
 
 
 def tri_rel_bias_fwd(dtype, batch, n, h, edges, pos, chain, table, base, out, stream) -> int:

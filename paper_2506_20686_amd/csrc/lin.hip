@@ -299,11 +299,21 @@ struct Product {
     }
   }
 
-  // Hands the result, 8 consecutive columns at a time, to f(i, j, values): through LDS, 32
-  // rows a wave at a time, so that the accesses f makes are whole rows' pieces.
+  // The result is handed out 8 consecutive columns at a time: piece t of PIECES of this
+  // thread lies at row piece_row(t), column piece_col() of the tile.
+  static constexpr int W = R / 2, PER = 64 / (W / 8), PIECES = NT * 32 / PER;
+  __device__ static inline int piece_row(int t) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    return (wave >> 1) * W + PER * t + lane / (W / 8);
+  }
+  __device__ static inline int piece_col() {
+    return ((threadIdx.x >> 6) & 1) * W + 8 * ((threadIdx.x & 63) % (W / 8));
+  }
+  // f(t, values) for every piece: through LDS, 32 rows a wave at a time, so that the
+  // accesses f makes are whole rows' pieces.
   template <typename F>
   __device__ static inline void result(char* lds, const f32x16 (&acc)[NT][NT], F f) {
-    constexpr int W = R / 2, ROW = W + 4, PER = 64 / (W / 8);  // rows a pass
+    constexpr int ROW = W + 4;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float* mine = (float*)lds + wave * 32 * ROW;
     const int j = 8 * (lane % (W / 8));
@@ -328,7 +338,7 @@ struct Product {
           const f32x4 x = *(const f32x4*)(mine + i * ROW + j + e);
           o[e] = x[0], o[e + 1] = x[1], o[e + 2] = x[2], o[e + 3] = x[3];
         }
-        f((wave >> 1) * W + 32 * u + i, (wave & 1) * W + j, o);
+        f((32 * u + s) / PER, o);
       }
     }
   }
@@ -355,9 +365,9 @@ __device__ inline void put8(T* p, int have, const float (&f)[8]) {
       if (i < have) p[i] = y.e[i];
   }
 }
-// Reads the first `have` of 8 values (zeros after them).
+// The first `have` of 8 values (zeros after them); ALIGNED: all of them, at 16 bytes.
 template <typename T, bool ALIGNED>
-__device__ inline void get8(const T* p, int have, float (&f)[8]) {
+__device__ inline Raw8<T> get8(const T* p, int have) {
   Raw8<T> r{};
   if (ALIGNED) {
 #pragma unroll
@@ -374,7 +384,7 @@ __device__ inline void get8(const T* p, int have, float (&f)[8]) {
       if (i < have) y.e[i] = p[i];
     r = __builtin_bit_cast(Raw8<T>, y);
   }
-  unpack(r, f);
+  return r;
 }
 
 // Contraction indices a step: as many as two buffers of three planes leave room for.
@@ -395,30 +405,38 @@ __global__ __launch_bounds__(256) void lin_fwd_kernel(LinArgs a) {
   const int nj = (a.n + R - 1) / R, wg = xcd_swizzle(blockIdx.x, gridDim.x);
   const int64_t i0 = (int64_t)(wg / nj) * R;
   const int j0 = (wg % nj) * R;
+  // what the epilogue reads is on its way before the product: the product of a narrow
+  // projection is shorter than a memory access
+  const int j = j0 + G::piece_col(), have = a.n - j;
+  Raw8<T> res[G::PIECES];
+  float bias[8] = {};
+  if (a.residual) {
+#pragma unroll
+    for (int t = 0; t < G::PIECES; ++t) {
+      const int64_t i = i0 + G::piece_row(t);
+      if (i < a.m && have > 0) res[t] = get8<T, ALIGNED>((const T*)a.residual + i * a.n + j, have);
+    }
+  }
+  if (a.bias && have > 0) unpack(get8<T, ALIGNED>((const T*)a.bias + j, have), bias);
   f32x16 acc[G::NT][G::NT];
   float none[8];
   G::run(lds, Mat<T>{(const T*)a.x, a.m, a.k}, nullptr, Mat<T>{(const T*)a.w, a.k, a.n}, nullptr,
          0, i0, j0, 0, a.k, false, none, acc);
-  G::result(lds, acc, [&](int di, int dj, float (&o)[8]) {
-    const int64_t i = i0 + di;
-    const int j = j0 + dj, have = a.n - j;
+  G::result(lds, acc, [&](int t, float (&o)[8]) {
+    const int64_t i = i0 + G::piece_row(t), at = i * a.n + j;
     if (i >= a.m || have <= 0) return;
-    const int64_t at = i * a.n + j;
-    float b[8];
-    if (a.bias) {
-      get8<T, ALIGNED>((const T*)a.bias + j, have, b);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] += b[e];
-    }
+    for (int e = 0; e < 8; ++e) o[e] += bias[e];
     if (a.z) put8<T, ALIGNED>((T*)a.z + at, have, o);
     if (a.act != TRIATTN_ACT_NONE) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = act_value(o[e], a.act);
     }
     if (a.residual) {
-      get8<T, ALIGNED>((const T*)a.residual + at, have, b);
+      float r[8];
+      unpack(res[t], r);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] += b[e];
+      for (int e = 0; e < 8; ++e) o[e] += r[e];
     }
     put8<T, ALIGNED>((T*)a.out + at, have, o);
   });
@@ -437,9 +455,9 @@ __global__ __launch_bounds__(256) void lin_bwd_dx_kernel(LinBwdArgs a) {
   float none[8];
   G::run(lds, Mat<T>{(const T*)a.dout, a.m, a.n}, (const T*)a.z, Mat<T>{(const T*)a.w, a.k, a.n},
          nullptr, a.act, i0, j0, 0, a.n, false, none, acc);
-  G::result(lds, acc, [&](int di, int dj, float (&o)[8]) {
-    const int64_t i = i0 + di;
-    const int j = j0 + dj, have = a.k - j;
+  const int j = j0 + G::piece_col(), have = a.k - j;
+  G::result(lds, acc, [&](int t, float (&o)[8]) {
+    const int64_t i = i0 + G::piece_row(t);
     if (i < a.m && have > 0) put8<T, ALIGNED>((T*)a.dx + i * a.k + j, have, o);
   });
 }
@@ -474,9 +492,10 @@ __global__ __launch_bounds__(256) void lin_bwd_w_kernel(LinBwdArgs a) {
   float col[8] = {};
   G::run(lds, Mat<T>{(const T*)a.x, a.m, a.k}, nullptr, Mat<T>{(const T*)a.dout, a.m, a.n},
          (const T*)a.z, a.act, i0, j0, k0, k1, sum, col, acc);
+  const int j = j0 + G::piece_col(), have = a.n - j;
   if (a.dw)
-    G::result(lds, acc, [&](int di, int dj, float (&o)[8]) {
-      const int i = i0 + di, j = j0 + dj, have = a.n - j;
+    G::result(lds, acc, [&](int t, float (&o)[8]) {
+      const int i = i0 + G::piece_row(t);
       if (i < a.k && have > 0) put8<float, ALIGNED>(dw + (int64_t)i * a.n + j, have, o);
     });
   if (sum) {  // the threads of a column chunk, in order

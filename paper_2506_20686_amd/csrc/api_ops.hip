@@ -44,9 +44,8 @@ int lin_check(int dtype, int64_t m, int64_t k, int64_t n, int act) {
   return (m + 63) / 64 * wide >= (int64_t)1 << 24 ? TRIATTN_ERR_UNSUPPORTED : TRIATTN_OK;
 }
 
-size_t lin_ws(int dtype, int64_t m, int64_t k, int64_t n) {
-  return round256(triattn::lin_bwd_ws(dtype, m, (int)k, (int)n));
-}
+// Partial sums, then dz; never 0, so that a workspace is always one.
+size_t lin_ws(const triattn::LinBwdPlan& p) { return round256(p.part) + round256(p.dz) + 256; }
 
 int rel_check(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges) {
   if (bad_dtype(dtype) || batch < 1 || batch > ((int64_t)1 << 20) || n < 1 || n > 8192 || h < 1 ||
@@ -171,7 +170,7 @@ int tri_linear_bwd_workspace_bytes(int dtype, int64_t m, int64_t k, int64_t n, i
   const int st = lin_check(dtype, m, k, n, act);
   if (st != TRIATTN_OK) return st;
   if (bytes == nullptr) return TRIATTN_ERR_INVALID_ARG;
-  *bytes = lin_ws(dtype, m, k, n);
+  *bytes = lin_ws(triattn::lin_bwd_plan(dtype, m, (int)k, (int)n, act));
   return TRIATTN_OK;
 }
 
@@ -183,8 +182,8 @@ int tri_linear_bwd(int dtype, int64_t m, int64_t k, int64_t n, int act, const vo
   if (bad_pointers({x, w, dout}, {z, dx, dw, dbias})) return TRIATTN_ERR_INVALID_ARG;
   if (act != TRIATTN_ACT_NONE && z == nullptr) return TRIATTN_ERR_INVALID_ARG;
   if (dx == nullptr && dw == nullptr && dbias == nullptr) return TRIATTN_ERR_INVALID_ARG;
-  if ((dw != nullptr || dbias != nullptr) &&
-      (workspace == nullptr || !aligned16(workspace) || workspace_bytes < lin_ws(dtype, m, k, n)))
+  const triattn::LinBwdPlan plan = triattn::lin_bwd_plan(dtype, m, (int)k, (int)n, act);
+  if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < lin_ws(plan))
     return TRIATTN_ERR_WORKSPACE;
   triattn::LinBwdArgs a{};
   a.m = m;
@@ -199,7 +198,8 @@ int tri_linear_bwd(int dtype, int64_t m, int64_t k, int64_t n, int act, const vo
   a.dw = dw;
   a.dbias = dbias;
   a.part = (float*)workspace;
-  a.splits = triattn::lin_bwd_splits(dtype, m, (int)k, (int)n);
+  a.splits = plan.splits;
+  if (plan.dz > 0) a.dz = (float*)((char*)workspace + round256(plan.part));
   return launched(triattn::launch_lin_bwd(dtype, a, (hipStream_t)stream));
 }
 

@@ -234,10 +234,14 @@ struct LinBwdArgs {
   float *dw, *dbias;       // [k][n], [n], or null
   float* part;             // workspace: [splits] partial sums (dw, dbias); none for 1 split
   int splits;
+  float* dz;               // workspace: dz [m][n], or null
 };
 
-int lin_bwd_splits(int dtype, int64_t m, int k, int n);
-size_t lin_bwd_ws(int dtype, int64_t m, int k, int n);  // bytes of workspace
+struct LinBwdPlan {
+  int splits;
+  size_t part, dz;  // bytes of workspace, 0 for none
+};
+LinBwdPlan lin_bwd_plan(int dtype, int64_t m, int k, int n, int act);
 hipError_t launch_lin_fwd(int dtype, const LinArgs& a, hipStream_t s);
 hipError_t launch_lin_bwd(int dtype, const LinBwdArgs& a, hipStream_t s);
 

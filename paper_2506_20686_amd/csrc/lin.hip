@@ -30,20 +30,41 @@
 namespace triattn {
 namespace {
 
+// Phi(z) and exp(-z^2 / 2), by Abramowitz and Stegun 7.1.26 (erf of x >= 0 is 1 - t (a1 +
+// t (...)) exp(-x^2) with t = 1 / (1 + p x), good to 1.5e-7 absolutely): one exponential
+// serves Phi and the density, where the library's erff alone takes three times as long.
+__device__ inline void normal_cdf(float z, float& cdf, float& e) {
+  const float x = fabsf(z) * 0.70710678118654752f;
+  e = __expf(-x * x);
+  const float t = fast_rcp(1.f + 0.3275911f * x);
+  const float tail =
+      0.5f * e * t *
+      (0.254829592f +
+       t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+  cdf = z < 0.f ? tail : 1.f - tail;
+}
+__device__ inline float sigmoid(float z) { return fast_rcp(1.f + __expf(-z)); }
+
 __device__ inline float act_value(float z, int act) {
   if (act == TRIATTN_ACT_RELU) return z > 0.f ? z : 0.f;
-  if (act == TRIATTN_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-  if (act == TRIATTN_ACT_SILU) return z / (1.f + expf(-z));
+  if (act == TRIATTN_ACT_GELU) {
+    float cdf, e;
+    normal_cdf(z, cdf, e);
+    return z * cdf;
+  }
+  if (act == TRIATTN_ACT_SILU) return z * sigmoid(z);
   return z;
 }
 
 __device__ inline float act_grad(float z, int act) {
   if (act == TRIATTN_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-  if (act == TRIATTN_ACT_GELU)
-    return 0.5f * (1.f + erff(z * 0.70710678118654752f)) +
-           z * 0.39894228040143268f * expf(-0.5f * z * z);
+  if (act == TRIATTN_ACT_GELU) {
+    float cdf, e;
+    normal_cdf(z, cdf, e);
+    return cdf + z * 0.39894228040143268f * e;
+  }
   if (act == TRIATTN_ACT_SILU) {
-    const float s = 1.f / (1.f + expf(-z));
+    const float s = sigmoid(z);
     return s * (1.f + z * (1.f - s));
   }
   return 1.f;
@@ -158,8 +179,9 @@ struct Tile {
   }
 };
 
-// What dz is made of.
-enum Dz { DZ_X, DZ_RELU, DZ_ACT };  // the tensor itself; dout where z > 0; dout act'(z)
+// What dz is made of in the staging: the tensor itself; dout where z > 0; dout act'(z); and
+// (not in the staging) dz made beforehand.
+enum Dz { DZ_X, DZ_RELU, DZ_ACT, DZ_MADE };
 
 // Staging of one operand: this thread's chunks of a tile, from memory to LDS.
 template <typename T, int R, int BK, bool KM, int P, int DZ, bool ALIGNED>
@@ -228,20 +250,20 @@ struct Stage {
 // C tile (rows i0 .. i0 + R - 1, columns j0 .. j0 + R - 1) = sum over indices [k0, k1) of
 // A(i, k) B(k, j), in registers: acc[u][v] of wave (wi, wj) holds rows wi R/2 + 32 u + l % 32
 // and columns wj R/2 + 32 v + accumulator rows (acc_row).
-template <typename T, int R, int BK, bool AKM, bool BKM, int PA, int PB, int DZA, int DZB,
-          bool ALIGNED, bool SUM>
+template <typename TA, typename TB, int R, int BK, bool AKM, bool BKM, int PA, int PB, int DZA,
+          int DZB, bool ALIGNED, bool SUM>
 struct Product {
   static constexpr int NT = R / 64;  // 32-wide tiles of a wave, each way
-  using SA = Stage<T, R, BK, AKM, PA, DZA, ALIGNED>;
-  using SB = Stage<T, R, BK, BKM, PB, DZB, ALIGNED>;
+  using SA = Stage<TA, R, BK, AKM, PA, DZA, ALIGNED>;
+  using SB = Stage<TB, R, BK, BKM, PB, DZB, ALIGNED>;
   using LA = typename SA::L;
   using LB = typename SB::L;
   static constexpr int BUF = LA::BYTES + LB::BYTES;
   static constexpr int EPI = 4 * 32 * (R / 2 + 4) * 4;  // the result's staging
   static constexpr int LDS = 2 * BUF > EPI ? 2 * BUF : EPI;
 
-  __device__ static inline void run(char* lds, const Mat<T>& a, const T* az, const Mat<T>& b,
-                                    const T* bz, int act, int64_t i0, int j0, int64_t k0,
+  __device__ static inline void run(char* lds, const Mat<TA>& a, const TA* az, const Mat<TB>& b,
+                                    const TB* bz, int act, int64_t i0, int j0, int64_t k0,
                                     int64_t k1, bool sum, float (&col)[8],
                                     f32x16 (&acc)[NT][NT]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -399,8 +421,8 @@ constexpr int planes() {
 
 template <typename T, int R, bool ALIGNED>
 __global__ __launch_bounds__(256) void lin_fwd_kernel(LinArgs a) {
-  using G = Product<T, R, step_k<T>(), true, false, planes<T>(), planes<T>(), DZ_X, DZ_X, ALIGNED,
-                    false>;
+  using G = Product<T, T, R, step_k<T>(), true, false, planes<T>(), planes<T>(), DZ_X, DZ_X,
+                    ALIGNED, false>;
   __shared__ __attribute__((aligned(16))) char lds[G::LDS];
   const int nj = (a.n + R - 1) / R, wg = xcd_swizzle(blockIdx.x, gridDim.x);
   const int64_t i0 = (int64_t)(wg / nj) * R;
@@ -442,19 +464,53 @@ __global__ __launch_bounds__(256) void lin_fwd_kernel(LinArgs a) {
   });
 }
 
+// What dz is read from, and as what: the call's dout (and z) in its own type, or the fp32
+// dz that lin_dz_kernel made of them.  P: planes of dx's product, Q: of dW's.
+template <typename T, int DZ>
+struct DzSource {
+  using E = T;
+  static constexpr int STAGE = DZ, P = sizeof(T) == 4 ? 3 : DZ == DZ_ACT ? 2 : 1,
+                       Q = sizeof(T) == 4 || DZ == DZ_ACT ? 3 : 1;
+};
+template <typename T>
+struct DzSource<T, DZ_MADE> {
+  using E = float;
+  static constexpr int STAGE = DZ_X, P = sizeof(T) == 4 ? 3 : 2, Q = 3;
+};
+
+// dz = dout act'(z) in fp32, where several column tiles of dx and dW would each form it
+// again from the two tensors (an exponential an element).
+template <typename T>
+__global__ __launch_bounds__(256) void lin_dz_kernel(LinBwdArgs a) {
+  const int64_t all = a.m * a.n;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < all;
+       i += (int64_t)gridDim.x * 2048) {
+    const int have = all - i < 8 ? (int)(all - i) : 8;
+    float d[8], z[8];
+    unpack(get8<T, false>((const T*)a.dout + i, have), d);
+    unpack(get8<T, false>((const T*)a.z + i, have), z);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d[e] *= act_grad(z[e], a.act);
+    put8<float, false>(a.dz + i, have, d);
+  }
+}
+
 // dx = dz W^T: W's rows are the columns of dx, its columns the contraction.
 template <typename T, int R, int DZ, bool ALIGNED>
 __global__ __launch_bounds__(256) void lin_bwd_dx_kernel(LinBwdArgs a) {
-  constexpr int PA = sizeof(T) == 4 ? 3 : DZ == DZ_ACT ? 2 : 1;
-  using G = Product<T, R, (PA > 1 ? 32 : 64), true, true, PA, planes<T>(), DZ, DZ_X, ALIGNED, false>;
+  using S = DzSource<T, DZ>;
+  using E = typename S::E;
+  using G = Product<E, T, R, (S::P > 1 ? 32 : 64), true, true, S::P, planes<T>(), S::STAGE, DZ_X,
+                    ALIGNED, false>;
   __shared__ __attribute__((aligned(16))) char lds[G::LDS];
   const int nj = (a.k + R - 1) / R, wg = xcd_swizzle(blockIdx.x, gridDim.x);
   const int64_t i0 = (int64_t)(wg / nj) * R;
   const int j0 = (wg % nj) * R;
+  const E* src = DZ == DZ_MADE ? (const E*)a.dz : (const E*)a.dout;
   f32x16 acc[G::NT][G::NT];
   float none[8];
-  G::run(lds, Mat<T>{(const T*)a.dout, a.m, a.n}, (const T*)a.z, Mat<T>{(const T*)a.w, a.k, a.n},
-         nullptr, a.act, i0, j0, 0, a.n, false, none, acc);
+  G::run(lds, Mat<E>{src, a.m, a.n}, (const E*)a.z, Mat<T>{(const T*)a.w, a.k, a.n}, nullptr,
+         a.act, i0, j0, 0, a.n, false, none, acc);
   const int j = j0 + G::piece_col(), have = a.k - j;
   G::result(lds, acc, [&](int t, float (&o)[8]) {
     const int64_t i = i0 + G::piece_row(t);
@@ -476,9 +532,10 @@ __host__ __device__ inline int64_t slab_floats(int k, int n) {
 // results themselves.
 template <typename T, int R, int DZ, bool ALIGNED>
 __global__ __launch_bounds__(256) void lin_bwd_w_kernel(LinBwdArgs a) {
-  constexpr int PB = sizeof(T) == 4 || DZ == DZ_ACT ? 3 : 1;
-  using G = Product<T, R, (PB > 1 ? 32 : 64), false, false, planes<T>(), PB, DZ_X, DZ, ALIGNED,
-                    true>;
+  using S = DzSource<T, DZ>;
+  using E = typename S::E;
+  using G = Product<T, E, R, (S::Q > 1 ? 32 : 64), false, false, planes<T>(), S::Q, DZ_X, S::STAGE,
+                    ALIGNED, true>;
   __shared__ __attribute__((aligned(16))) char lds[G::LDS];
   const int ni = (a.k + R - 1) / R, nj = (a.n + R - 1) / R;
   const int wg = xcd_swizzle(blockIdx.x, gridDim.x), split = wg / (ni * nj);
@@ -490,8 +547,9 @@ __global__ __launch_bounds__(256) void lin_bwd_w_kernel(LinBwdArgs a) {
   float* db = a.splits > 1 ? dw + (int64_t)a.k * a.n : a.dbias;
   f32x16 acc[G::NT][G::NT];
   float col[8] = {};
-  G::run(lds, Mat<T>{(const T*)a.x, a.m, a.k}, nullptr, Mat<T>{(const T*)a.dout, a.m, a.n},
-         (const T*)a.z, a.act, i0, j0, k0, k1, sum, col, acc);
+  const E* src = DZ == DZ_MADE ? (const E*)a.dz : (const E*)a.dout;
+  G::run(lds, Mat<T>{(const T*)a.x, a.m, a.k}, nullptr, Mat<E>{src, a.m, a.n}, (const E*)a.z,
+         a.act, i0, j0, k0, k1, sum, col, acc);
   const int j = j0 + G::piece_col(), have = a.n - j;
   if (a.dw)
     G::result(lds, acc, [&](int t, float (&o)[8]) {
@@ -587,14 +645,27 @@ void bwd_part(const LinBwdArgs& a, hipStream_t s, bool weights, bool big) {
   if constexpr (sizeof(T) == 2) {  // dout where z > 0 is a bf16 value: one plane
     if (a.act == TRIATTN_ACT_RELU) return bwd_tile<T, DZ_RELU>(a, s, weights, big);
   }
+  if (a.dz) return bwd_tile<T, DZ_MADE>(a, s, weights, big);
   bwd_tile<T, DZ_ACT>(a, s, weights, big);
 }
 
 // Tiles of dW are 128 wide unless k or n would fill no more than half of one.
 bool wide_w(int k, int n) { return k > 64 && n > 64; }
 
+// dz is made beforehand (fp32, in the workspace) where dx has several column tiles, and dW
+// as many: for one, forming it twice moves half the bytes.
+bool make_dz(int dtype, int act, int k) {
+  return act > TRIATTN_ACT_RELU && k > 128 || act == TRIATTN_ACT_RELU && dtype == TRIATTN_F32 && k > 128;
+}
+
 template <typename T>
 hipError_t bwd(const LinBwdArgs& a, hipStream_t s) {
+  if (a.dz) {
+    KernelTimer t(K_LIN_DZ, s);
+    const int64_t wgs = (a.m * a.n + 2047) / 2048;
+    hipLaunchKernelGGL(lin_dz_kernel<T>, dim3((unsigned)(wgs < 4096 ? wgs : 4096)), dim3(256), 0, s,
+                       a);
+  }
   if (a.dx) bwd_part<T>(a, s, false, wide(tiles_of(a.m, a.k, 128)));
   if (a.dw || a.dbias) {
     bwd_part<T>(a, s, true, wide_w(a.k, a.n));
@@ -614,7 +685,7 @@ hipError_t bwd(const LinBwdArgs& a, hipStream_t s) {
 
 // Splits of the rows for dW: enough workgroups for two rounds of the 256 CUs, each of at
 // least 128 rows.
-int lin_bwd_splits(int, int64_t m, int k, int n) {
+static int lin_bwd_splits(int, int64_t m, int k, int n) {
   const int64_t tiles = tiles_of(k, n, wide_w(k, n) ? 128 : 64);
   int64_t s = 512 / tiles, most = (m + 127) / 128;
   if (s > most) s = most;
@@ -622,9 +693,12 @@ int lin_bwd_splits(int, int64_t m, int k, int n) {
   const int64_t per = split_rows(m, (int)s);
   return (int)((m + per - 1) / per);  // no split without rows
 }
-size_t lin_bwd_ws(int dtype, int64_t m, int k, int n) {
-  const int s = lin_bwd_splits(dtype, m, k, n);
-  return s > 1 ? (size_t)s * (size_t)slab_floats(k, n) * sizeof(float) : 256;
+LinBwdPlan lin_bwd_plan(int dtype, int64_t m, int k, int n, int act) {
+  LinBwdPlan p{};
+  p.splits = lin_bwd_splits(dtype, m, k, n);
+  if (p.splits > 1) p.part = (size_t)p.splits * (size_t)slab_floats(k, n) * sizeof(float);
+  if (make_dz(dtype, act, k)) p.dz = (size_t)m * n * sizeof(float);
+  return p;
 }
 
 hipError_t launch_lin_fwd(int dtype, const LinArgs& a, hipStream_t s) {

@@ -139,8 +139,7 @@ def test_nothing_outside_the_outputs_is_written(m, k, n, dtype):
             b.fill_(7.0)
         args = [at[2 + i] if i == keep else None for i in range(3)]
         assert B.tri_linear_bwd(code, m, k, n, B.ACT_GELU, p["x"], p["w"], p["z"], p["dout"],
-                                *args, ws.data_ptr() if keep else None, need if keep else 0,
-                                s) == B.OK
+                                *args, ws.data_ptr(), need, s) == B.OK
         for i, b in enumerate(big[2:]):
             want = ref[2 + i].reshape(-1) if i == keep else torch.full_like(b[pad:-pad], 7.0)
             assert torch.equal(b[pad:-pad], want), (keep, i)

@@ -6,8 +6,8 @@
 // All three products run through one kernel body: a workgroup of 4 waves (2 x 2) makes an
 // R x R tile of the result, R = 128 or 64, staging tiles of both operands through
 // registers into two LDS buffers in turn, and multiplies them on the matrix cores (bf16
-// 32 x 32 x 16, fp32 sums).  Loads of the tile after next are in flight while one is
-// multiplied; one barrier a step.
+// 32 x 32 x 16, fp32 sums).  The loads of the next tile, or two, are in flight while one
+// is multiplied; one barrier a step.
 //
 // Operands: a tile is stored as it lies in memory, either [row][contraction] ("K major":
 // fragments are 16-byte reads) or [contraction][row] (fragments are the LDS's transposing
@@ -107,7 +107,7 @@ struct Mat {
 template <typename T, bool ALIGNED>
 __device__ inline Raw8<T> fetch(const Mat<T>& m, int64_t r0, int c0, int lim, int r, int c) {
   Raw8<T> x{};
-  const int64_t left = m.rows - r0;
+  const int64_t left = c0 < m.cols ? m.rows - r0 : 0;
   const int rows = left < lim ? (left < 0 ? 0 : (int)left) : lim;
   const T* base = m.p + r0 * m.cols + c0;
   if constexpr (ALIGNED) {
@@ -259,6 +259,8 @@ struct Product {
   using LA = typename SA::L;
   using LB = typename SB::L;
   static constexpr int BUF = LA::BYTES + LB::BYTES;
+  // steps whose loads are in flight: two where the registers allow two workgroups on a CU
+  static constexpr int D = R == 64 ? 2 : 1;
   static constexpr int EPI = 4 * 32 * (R / 2 + 4) * 4;  // the result's staging
   static constexpr int LDS = 2 * BUF > EPI ? 2 * BUF : EPI;
 
@@ -272,52 +274,63 @@ struct Product {
     for (int u = 0; u < NT; ++u)
 #pragma unroll
       for (int v = 0; v < NT; ++v) acc[u][v] = f32x16{};
-    SA sa;
-    SB sb;
-    sa.load(a, az, i0, k0, k1);
-    sb.load(b, bz, j0, k0, k1);
+    // Loads run D steps ahead and without a condition (past the end they give zeros and
+    // touch no memory), so that a step waits for its own loads only.
     const int steps = (int)((k1 - k0 + BK - 1) / BK);
-    for (int it = 0; it < steps; ++it) {
-      char* buf = lds + (it & 1) * BUF;
+    SA sa[D];
+    SB sb[D];
+    auto load = [&](int d, int it) {
+      sa[d].load(a, az, i0, k0 + (int64_t)it * BK, k1);
+      sb[d].load(b, bz, j0, k0 + (int64_t)it * BK, k1);
+    };
+    auto step = [&](int d, char* buf, int next) {
       float none[8];
-      sa.template store<false>(buf, act, false, none);
-      sb.template store<SUM>(buf + LA::BYTES, act, sum, col);
-      if (it + 1 < steps) {
-        const int64_t k = k0 + (int64_t)(it + 1) * BK;
-        sa.load(a, az, i0, k, k1);
-        sb.load(b, bz, j0, k, k1);
-      }
-      // the buffer of step it was last read in step it - 2, before the barrier of it - 1
+      sa[d].template store<false>(buf, act, false, none);
+      sb[d].template store<SUM>(buf + LA::BYTES, act, sum, col);
+      load(d, next);
+      // this buffer was last read two steps ago, before the barrier of the last step
       __syncthreads();
+      multiply(buf, ri, rj, lane, acc);
+    };
 #pragma unroll
-      for (int kk = 0; kk < BK; kk += 16) {
-        bf16x8 fa[PA][NT], fb[PB][NT];
+    for (int d = 0; d < D; ++d) load(d, d);
+    int it = 0;
+    for (; it + 2 <= steps; it += 2) {
+      step(0, lds, it + D);
+      step(D - 1, lds + BUF, it + 1 + D);
+    }
+    if (it < steps) step(0, lds, it + D);
+  }
+
+  __device__ static inline void multiply(const char* buf, int ri, int rj, int lane,
+                                         f32x16 (&acc)[NT][NT]) {
 #pragma unroll
-        for (int p = 0; p < PA; ++p)
+    for (int kk = 0; kk < BK; kk += 16) {
+      bf16x8 fa[PA][NT], fb[PB][NT];
+#pragma unroll
+      for (int p = 0; p < PA; ++p)
+#pragma unroll
+        for (int u = 0; u < NT; ++u) fa[p][u] = LA::frag(buf + p * LA::PLANE, ri + 32 * u, kk, lane);
+#pragma unroll
+      for (int p = 0; p < PB; ++p)
+#pragma unroll
+        for (int v = 0; v < NT; ++v)
+          fb[p][v] = LB::frag(buf + LA::BYTES + p * LB::PLANE, rj + 32 * v, kk, lane);
+      // plane products down to 2^-24 of the whole, the smallest first
+      constexpr int MOST = (PA > PB ? PA : PB) - 1;
+#pragma unroll
+      for (int order = MOST; order >= 0; --order)
+#pragma unroll
+        for (int p = 0; p < PA; ++p) {
+          const int q = order - p;
+          if (q < 0 || q >= PB) continue;
 #pragma unroll
           for (int u = 0; u < NT; ++u)
-            fa[p][u] = LA::frag(buf + p * LA::PLANE, ri + 32 * u, kk, lane);
 #pragma unroll
-        for (int p = 0; p < PB; ++p)
-#pragma unroll
-          for (int v = 0; v < NT; ++v)
-            fb[p][v] = LB::frag(buf + LA::BYTES + p * LB::PLANE, rj + 32 * v, kk, lane);
-        // plane products down to 2^-24 of the whole, the smallest first
-        constexpr int MOST = (PA > PB ? PA : PB) - 1;
-#pragma unroll
-        for (int order = MOST; order >= 0; --order)
-#pragma unroll
-          for (int p = 0; p < PA; ++p) {
-            const int q = order - p;
-            if (q < 0 || q >= PB) continue;
-#pragma unroll
-            for (int u = 0; u < NT; ++u)
-#pragma unroll
-              for (int v = 0; v < NT; ++v)
-                acc[u][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[q][v], fa[p][u], acc[u][v],
-                                                                    0, 0, 0);
-          }
-      }
+            for (int v = 0; v < NT; ++v)
+              acc[u][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[q][v], fa[p][u], acc[u][v], 0,
+                                                                  0, 0);
+        }
     }
   }
 
@@ -409,11 +422,9 @@ __device__ inline Raw8<T> get8(const T* p, int have) {
   return r;
 }
 
-// Contraction indices a step: as many as two buffers of three planes leave room for.
-template <typename T>
-constexpr int step_k() {
-  return sizeof(T) == 2 ? 64 : 32;
-}
+// Contraction indices a step: 64 while the two buffers leave room for two workgroups on a
+// CU, else 32 (three planes of each operand, or of one and 128 rows).
+constexpr int step_k(int r, int planes) { return r * planes <= 256 ? 64 : 32; }
 template <typename T>
 constexpr int planes() {
   return sizeof(T) == 2 ? 1 : 3;
@@ -421,8 +432,8 @@ constexpr int planes() {
 
 template <typename T, int R, bool ALIGNED>
 __global__ __launch_bounds__(256) void lin_fwd_kernel(LinArgs a) {
-  using G = Product<T, T, R, step_k<T>(), true, false, planes<T>(), planes<T>(), DZ_X, DZ_X,
-                    ALIGNED, false>;
+  using G = Product<T, T, R, step_k(R, 2 * planes<T>()), true, false, planes<T>(), planes<T>(), DZ_X,
+                    DZ_X, ALIGNED, false>;
   __shared__ __attribute__((aligned(16))) char lds[G::LDS];
   const int nj = (a.n + R - 1) / R, wg = xcd_swizzle(blockIdx.x, gridDim.x);
   const int64_t i0 = (int64_t)(wg / nj) * R;
@@ -500,8 +511,8 @@ template <typename T, int R, int DZ, bool ALIGNED>
 __global__ __launch_bounds__(256) void lin_bwd_dx_kernel(LinBwdArgs a) {
   using S = DzSource<T, DZ>;
   using E = typename S::E;
-  using G = Product<E, T, R, (S::P > 1 ? 32 : 64), true, true, S::P, planes<T>(), S::STAGE, DZ_X,
-                    ALIGNED, false>;
+  using G = Product<E, T, R, step_k(R, S::P + planes<T>()), true, true, S::P, planes<T>(), S::STAGE,
+                    DZ_X, ALIGNED, false>;
   __shared__ __attribute__((aligned(16))) char lds[G::LDS];
   const int nj = (a.k + R - 1) / R, wg = xcd_swizzle(blockIdx.x, gridDim.x);
   const int64_t i0 = (int64_t)(wg / nj) * R;
@@ -534,8 +545,8 @@ template <typename T, int R, int DZ, bool ALIGNED>
 __global__ __launch_bounds__(256) void lin_bwd_w_kernel(LinBwdArgs a) {
   using S = DzSource<T, DZ>;
   using E = typename S::E;
-  using G = Product<T, E, R, (S::Q > 1 ? 32 : 64), false, false, planes<T>(), S::Q, DZ_X, S::STAGE,
-                    ALIGNED, true>;
+  using G = Product<T, E, R, step_k(R, planes<T>() + S::Q), false, false, planes<T>(), S::Q, DZ_X,
+                    S::STAGE, ALIGNED, true>;
   __shared__ __attribute__((aligned(16))) char lds[G::LDS];
   const int ni = (a.k + R - 1) / R, nj = (a.n + R - 1) / R;
   const int wg = xcd_swizzle(blockIdx.x, gridDim.x), split = wg / (ni * nj);

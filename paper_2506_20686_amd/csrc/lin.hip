@@ -582,6 +582,194 @@ __global__ __launch_bounds__(256) void lin_bwd_w_kernel(LinBwdArgs a) {
   }
 }
 
+// ---- the whole backward of a narrow bf16 projection (k, n <= 128) -------------------------
+//
+// Bound by memory: for rows of 128 + 128 channels it multiplies 128 times per value moved,
+// a tenth of what the matrix cores do meanwhile.  So dx, dW and dbias come from one copy
+// of x and dout (the two kernels above read dout twice): a workgroup of 8 waves walks over
+// blocks of M rows, stages x and dz in LDS, and uses the dz tile both ways, its rows for
+// dx = dz W^T (W stays in LDS) and its columns for dW += x^T dz (in registers until the
+// end).  The next block's loads are in flight meanwhile.  dx goes through x's place in LDS,
+// each wave's part by itself, to be stored in whole rows' pieces.
+//
+// M = 128, or 64 where dz takes three planes (96 KB of LDS either way).
+// 589,824 x 128 x 128: 143 us by the two kernels and their sums, see lin_narrow below.
+struct Square {  // lines of 128 bf16, read along and across
+  // Both reads are free of bank conflicts: s differs between any 16 consecutive lines
+  // (its low three bits between 8) for 16-byte reads down the lines, and its bits 3, 2 as
+  // well as its bits 2, 1 between the four lines of a transposing read.
+  __device__ static inline int chunk_at(int line, int c) {
+    const int e = line & 3, s = ((e ^ (e << 1)) << 1) ^ ((line >> 2) & 3);
+    return (line * 16 + (c ^ s)) * 16;
+  }
+  // lines r0 .. + 31 as rows, columns k0 .. + 15 as indices
+  __device__ static inline bf16x8 along(const char* t, int r0, int k0, int lane) {
+    return *(const bf16x8*)(t + chunk_at(r0 + (lane & 31), (k0 >> 3) + (lane >> 5)));
+  }
+  // columns r0 .. + 31 as rows, lines k0 .. + 15 as indices
+  __device__ static inline bf16x8 across(const char* t, int r0, int k0, int lane) {
+    const int i = lane & 15, col = r0 + (lane & 16) + 4 * (i & 3);
+    const int line = k0 + 8 * (lane >> 5) + (i >> 2);
+    typedef TRIATTN_LDS s16x4* lds4;
+    const char* a = t + chunk_at(line, col >> 3) + (col & 4) * 2;
+    const char* b = t + chunk_at(line + 4, col >> 3) + (col & 4) * 2;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(uintptr_t)lds_addr(a));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(uintptr_t)lds_addr(b));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+constexpr int NARROW_WG = 512;
+constexpr int narrow_rows(int dz) { return dz == DZ_ACT ? 64 : 128; }
+
+template <int DZ>
+__global__ __launch_bounds__(NARROW_WG) void lin_narrow_kernel(LinBwdArgs a) {
+  using S = DzSource<bf16, DZ>;
+  constexpr int M = narrow_rows(DZ), N = M / 32;       // chunks a thread stages of a tile
+  constexpr int JT = M / 64, JW = 32 * JT;             // dx tiles, columns of a wave
+  constexpr int TILE_BYTES = M * 256, W_BYTES = 128 * 256;
+  __shared__ __attribute__((aligned(16))) char lds[W_BYTES + (1 + S::Q) * TILE_BYTES];
+  char *tw = lds, *tx = lds + W_BYTES, *tz = tx + TILE_BYTES;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const bool weights = a.dw || a.dbias;
+  const Mat<bf16> mx{(const bf16*)a.x, a.m, a.k}, md{(const bf16*)a.dout, a.m, a.n},
+      mz{(const bf16*)a.z, a.m, a.n}, mw{(const bf16*)a.w, a.k, a.n};
+  const int line0 = threadIdx.x / 16, chunk = threadIdx.x % 16;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int line = line0 + 32 * u;
+    *(u32x4*)(tw + Square::chunk_at(line, chunk)) =
+        fetch<bf16, true>(mw, 0, 0, 128, line, 8 * chunk).v[0];
+  }
+  Raw8<bf16> x[N], d[N], z[DZ == DZ_X ? 1 : N];
+  auto load = [&](int64_t r0) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int line = line0 + 32 * u;
+      x[u] = fetch<bf16, true>(mx, r0, 0, M, line, 8 * chunk);
+      d[u] = fetch<bf16, true>(md, r0, 0, M, line, 8 * chunk);
+      if constexpr (DZ != DZ_X) z[u] = fetch<bf16, true>(mz, r0, 0, M, line, 8 * chunk);
+    }
+  };
+  // this wave's tiles: dx rows di .. + 31, columns dj .. + JW - 1; dW rows (of k) wi .. + 31,
+  // columns wj .. + 63
+  const int di = M == 128 ? wave / 2 * 32 : wave / 4 * 32, dj = M == 128 ? wave % 2 * 64 : wave % 4 * 32;
+  const int wi = wave / 2 * 32, wj = wave % 2 * 64;
+  f32x16 gw[2] = {};
+  float col[8] = {};
+  load((int64_t)blockIdx.x * M);
+  for (int64_t r0 = (int64_t)blockIdx.x * M; r0 < a.m; r0 += (int64_t)gridDim.x * M) {
+    __syncthreads();  // dx of the last block has left x's place
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int at = Square::chunk_at(line0 + 32 * u, chunk);
+      *(u32x4*)(tx + at) = x[u].v[0];
+      float f[8];
+      unpack(d[u], f);
+      if constexpr (DZ != DZ_X) {
+        float g[8];
+        unpack(z[u], g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          f[e] = DZ == DZ_RELU ? (g[e] > 0.f ? f[e] : 0.f) : f[e] * act_grad(g[e], a.act);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) col[e] += f[e];
+#pragma unroll
+      for (int p = 0; p < S::Q; ++p) {
+        bf16x8 b;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          b[e] = (bf16)f[e];
+          if (p + 1 < S::Q) f[e] -= (float)b[e];
+        }
+        *(bf16x8*)(tz + p * TILE_BYTES + at) = b;
+      }
+    }
+    __syncthreads();
+    load(r0 + (int64_t)gridDim.x * M);
+    if (a.dw && wi < a.k && wj < a.n) {
+#pragma unroll
+      for (int kk = 0; kk < M; kk += 16) {
+        const bf16x8 fx = Square::across(tx, wi, kk, lane);
+#pragma unroll
+        for (int p = S::Q - 1; p >= 0; --p)
+#pragma unroll
+          for (int v = 0; v < 2; ++v)
+            gw[v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                Square::across(tz + p * TILE_BYTES, wj + 32 * v, kk, lane), fx, gw[v], 0, 0, 0);
+      }
+    }
+    f32x16 gx[JT] = {};
+    if (a.dx && dj < a.k) {
+#pragma unroll
+      for (int kk = 0; kk < 128; kk += 16) {
+        if (kk >= a.n) break;
+#pragma unroll
+        for (int p = S::P - 1; p >= 0; --p) {
+          const bf16x8 fz = Square::along(tz + p * TILE_BYTES, di, kk, lane);
+#pragma unroll
+          for (int v = 0; v < JT; ++v)
+            gx[v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                Square::along(tw, dj + 32 * v, kk, lane), fz, gx[v], 0, 0, 0);
+        }
+      }
+    }
+    __syncthreads();
+    if (a.dx && dj < a.k) {
+      // the wave's 32 rows x JW columns in its own part of x's place, 16-byte chunks
+      // permuted by the row
+      constexpr int CH = JW / 8;
+      char* mine = tx + wave * 32 * JW * 2;
+      auto at = [&](int i, int c) {
+        return mine + (i * CH + (c ^ (CH == 8 ? i & 7 : (i >> 1) & 3))) * 16;
+      };
+#pragma unroll
+      for (int v = 0; v < JT; ++v)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *(bf16x4*)(at(lane & 31, 4 * v + q) + 8 * (lane >> 5)) =
+              bf16x4{(bf16)gx[v][4 * q], (bf16)gx[v][4 * q + 1], (bf16)gx[v][4 * q + 2],
+                     (bf16)gx[v][4 * q + 3]};
+      // only this wave's lanes read it back, after their writes (LDS serves a wave in order)
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      const int j = dj + 8 * (lane % CH);
+#pragma unroll
+      for (int s = 0; s < 32; s += 64 / CH) {
+        const int i = s + lane / CH;
+        const u32x4 o = *(const u32x4*)at(i, lane % CH);
+        if (r0 + di + i < a.m && j < a.k) *(u32x4*)((bf16*)a.dx + (r0 + di + i) * a.k + j) = o;
+      }
+    }
+  }
+  if (!weights) return;
+  float* dw = a.splits > 1 ? a.part + blockIdx.x * slab_floats(a.k, a.n) : a.dw;
+  float* db = a.splits > 1 ? dw + (int64_t)a.k * a.n : a.dbias;
+  const int i = wi + (lane & 31);
+  if (a.dw && i < a.k)
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int j = wj + 32 * v + 8 * q + 4 * (lane >> 5);
+        if (j < a.n)
+          *(f32x4*)(dw + i * a.n + j) =
+              f32x4{gw[v][4 * q], gw[v][4 * q + 1], gw[v][4 * q + 2], gw[v][4 * q + 3]};
+      }
+  if (a.dbias) {  // the threads of a column, in order
+    __syncthreads();
+    float* part = (float*)lds;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[line0 * 128 + 8 * chunk + e] = col[e];
+    __syncthreads();
+    if ((int)threadIdx.x < a.n) {
+      float s = 0.f;
+      for (int t = 0; t < 32; ++t) s += part[t * 128 + threadIdx.x];
+      db[threadIdx.x] = s;
+    }
+  }
+}
+
 // Sums of the splits' slabs: `slices` threads (a power of two) to 4 consecutive sums, each
 // every slices-th slab, then their sums through LDS, in a fixed order.
 __global__ __launch_bounds__(256) void lin_reduce_kernel(LinBwdArgs a, int slices) {
@@ -669,8 +857,38 @@ bool make_dz(int dtype, int act, int k) {
   return act > TRIATTN_ACT_RELU && k > 128 || act == TRIATTN_ACT_RELU && dtype == TRIATTN_F32 && k > 128;
 }
 
+hipError_t reduce(const LinBwdArgs& a, hipStream_t s) {
+  KernelTimer t(K_LIN_REDUCE, s);
+  int slices = 1;
+  while (slices < 32 && slices * 4 < a.splits) slices *= 2;
+  const int64_t quads = ((int64_t)a.k * a.n + a.n + 3) / 4, cols = 256 / slices;
+  hipLaunchKernelGGL(lin_reduce_kernel, dim3((unsigned)((quads + cols - 1) / cols)), dim3(256), 0, s,
+                     a, slices);
+  return hipGetLastError();
+}
+
+bool narrow(int dtype, int k, int n) {
+  return dtype == TRIATTN_BF16 && aligned8(k, n) && k <= 128 && n <= 128;
+}
+int narrow_parts(int64_t m, int act) {
+  const int rows = narrow_rows(act > TRIATTN_ACT_RELU ? DZ_ACT : DZ_X);
+  const int64_t blocks = (m + rows - 1) / rows;
+  return (int)(blocks < 256 ? blocks : 256);  // one workgroup a CU
+}
+hipError_t bwd_narrow(const LinBwdArgs& a, hipStream_t s) {
+  {
+    KernelTimer t(K_LIN_NARROW, s);
+    const dim3 grid(narrow_parts(a.m, a.act)), wg(NARROW_WG);
+    if (a.act == TRIATTN_ACT_NONE) hipLaunchKernelGGL(lin_narrow_kernel<DZ_X>, grid, wg, 0, s, a);
+    else if (a.act == TRIATTN_ACT_RELU) hipLaunchKernelGGL(lin_narrow_kernel<DZ_RELU>, grid, wg, 0, s, a);
+    else hipLaunchKernelGGL(lin_narrow_kernel<DZ_ACT>, grid, wg, 0, s, a);
+  }
+  return (a.dw || a.dbias) && a.splits > 1 ? reduce(a, s) : hipGetLastError();
+}
+
 template <typename T>
 hipError_t bwd(const LinBwdArgs& a, hipStream_t s) {
+  if (sizeof(T) == 2 && narrow(TRIATTN_BF16, a.k, a.n)) return bwd_narrow(a, s);
   if (a.dz) {
     KernelTimer t(K_LIN_DZ, s);
     const int64_t wgs = (a.m * a.n + 2047) / 2048;
@@ -680,14 +898,7 @@ hipError_t bwd(const LinBwdArgs& a, hipStream_t s) {
   if (a.dx) bwd_part<T>(a, s, false, wide(tiles_of(a.m, a.k, 128)));
   if (a.dw || a.dbias) {
     bwd_part<T>(a, s, true, wide_w(a.k, a.n));
-    if (a.splits > 1) {
-      KernelTimer t(K_LIN_REDUCE, s);
-      int slices = 1;
-      while (slices < 32 && slices * 4 < a.splits) slices *= 2;
-      const int64_t quads = ((int64_t)a.k * a.n + a.n + 3) / 4, cols = 256 / slices;
-      hipLaunchKernelGGL(lin_reduce_kernel, dim3((unsigned)((quads + cols - 1) / cols)), dim3(256),
-                         0, s, a, slices);
-    }
+    if (a.splits > 1) return reduce(a, s);
   }
   return hipGetLastError();
 }
@@ -706,7 +917,7 @@ static int lin_bwd_splits(int, int64_t m, int k, int n) {
 }
 LinBwdPlan lin_bwd_plan(int dtype, int64_t m, int k, int n, int act) {
   LinBwdPlan p{};
-  p.splits = lin_bwd_splits(dtype, m, k, n);
+  p.splits = narrow(dtype, k, n) ? narrow_parts(m, act) : lin_bwd_splits(dtype, m, k, n);
   if (p.splits > 1) p.part = (size_t)p.splits * (size_t)slab_floats(k, n) * sizeof(float);
   if (make_dz(dtype, act, k)) p.dz = (size_t)m * n * sizeof(float);
   return p;

@@ -40,6 +40,7 @@ enum KernelId {
   K_LIN_BWD_W,
   K_LIN_REDUCE,
   K_LIN_DZ,
+  K_LIN_NARROW,
   K_REL_FWD,
   K_REL_BWD,
   K_REL_REDUCE,

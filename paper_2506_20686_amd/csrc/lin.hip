@@ -508,13 +508,15 @@ __global__ __launch_bounds__(256) void lin_dz_kernel(LinBwdArgs a) {
 
 // dx = dz W^T: W's rows are the columns of dx, its columns the contraction.
 template <typename T, int R, int DZ, bool ALIGNED>
-__global__ __launch_bounds__(256) void lin_bwd_dx_kernel(LinBwdArgs a) {
-  using S = DzSource<T, DZ>;
-  using E = typename S::E;
-  using G = Product<E, T, R, step_k(R, S::P + planes<T>()), true, true, S::P, planes<T>(), S::STAGE,
-                    DZ_X, ALIGNED, false>;
-  __shared__ __attribute__((aligned(16))) char lds[G::LDS];
-  const int nj = (a.k + R - 1) / R, wg = xcd_swizzle(blockIdx.x, gridDim.x);
+using DxProduct = Product<typename DzSource<T, DZ>::E, T, R,
+                          step_k(R, DzSource<T, DZ>::P + planes<T>()), true, true,
+                          DzSource<T, DZ>::P, planes<T>(), DzSource<T, DZ>::STAGE, DZ_X, ALIGNED,
+                          false>;
+template <typename T, int R, int DZ, bool ALIGNED>
+__device__ inline void dx_tile(const LinBwdArgs& a, char* lds, int wg) {
+  using E = typename DzSource<T, DZ>::E;
+  using G = DxProduct<T, R, DZ, ALIGNED>;
+  const int nj = (a.k + R - 1) / R;
   const int64_t i0 = (int64_t)(wg / nj) * R;
   const int j0 = (wg % nj) * R;
   const E* src = DZ == DZ_MADE ? (const E*)a.dz : (const E*)a.dout;
@@ -542,14 +544,15 @@ __host__ __device__ inline int64_t slab_floats(int k, int n) {
 // One split's dW tile and, in the first row of tiles, its dbias.  Without splits the
 // results themselves.
 template <typename T, int R, int DZ, bool ALIGNED>
-__global__ __launch_bounds__(256) void lin_bwd_w_kernel(LinBwdArgs a) {
-  using S = DzSource<T, DZ>;
-  using E = typename S::E;
-  using G = Product<T, E, R, step_k(R, planes<T>() + S::Q), false, false, planes<T>(), S::Q, DZ_X,
-                    S::STAGE, ALIGNED, true>;
-  __shared__ __attribute__((aligned(16))) char lds[G::LDS];
+using DwProduct = Product<T, typename DzSource<T, DZ>::E, R,
+                          step_k(R, planes<T>() + DzSource<T, DZ>::Q), false, false, planes<T>(),
+                          DzSource<T, DZ>::Q, DZ_X, DzSource<T, DZ>::STAGE, ALIGNED, true>;
+template <typename T, int R, int DZ, bool ALIGNED>
+__device__ inline void dw_tile(const LinBwdArgs& a, char* lds, int wg) {
+  using E = typename DzSource<T, DZ>::E;
+  using G = DwProduct<T, R, DZ, ALIGNED>;
   const int ni = (a.k + R - 1) / R, nj = (a.n + R - 1) / R;
-  const int wg = xcd_swizzle(blockIdx.x, gridDim.x), split = wg / (ni * nj);
+  const int split = wg / (ni * nj);
   const int i0 = wg % (ni * nj) / nj * R, j0 = wg % nj * R;
   const int64_t per = split_rows(a.m, a.splits), k0 = split * per;
   const int64_t k1 = k0 + per < a.m ? k0 + per : a.m;
@@ -580,6 +583,29 @@ __global__ __launch_bounds__(256) void lin_bwd_w_kernel(LinBwdArgs a) {
       db[j0 + threadIdx.x] = s;
     }
   }
+}
+
+template <typename T, int R, int DZ, bool ALIGNED>
+__global__ __launch_bounds__(256) void lin_bwd_dx_kernel(LinBwdArgs a) {
+  __shared__ __attribute__((aligned(16))) char lds[DxProduct<T, R, DZ, ALIGNED>::LDS];
+  dx_tile<T, R, DZ, ALIGNED>(a, lds, xcd_swizzle(blockIdx.x, gridDim.x));
+}
+template <typename T, int R, int DZ, bool ALIGNED>
+__global__ __launch_bounds__(256) void lin_bwd_w_kernel(LinBwdArgs a) {
+  __shared__ __attribute__((aligned(16))) char lds[DwProduct<T, R, DZ, ALIGNED>::LDS];
+  dw_tile<T, R, DZ, ALIGNED>(a, lds, xcd_swizzle(blockIdx.x, gridDim.x));
+}
+// Both in one launch, where dx does not fill the GPU: the first ndx workgroups make dx, the
+// others dW (in tiles of RW).
+template <typename T, int RW, int DZ, bool ALIGNED>
+__global__ __launch_bounds__(256) void lin_bwd_both_kernel(LinBwdArgs a, int ndx) {
+  constexpr int LX = DxProduct<T, 64, DZ, ALIGNED>::LDS, LW = DwProduct<T, RW, DZ, ALIGNED>::LDS;
+  __shared__ __attribute__((aligned(16))) char lds[LX > LW ? LX : LW];
+  const int wg = blockIdx.x, ndw = (int)gridDim.x - ndx;
+  if (wg < ndx)
+    dx_tile<T, 64, DZ, ALIGNED>(a, lds, xcd_swizzle(wg, ndx));
+  else
+    dw_tile<T, RW, DZ, ALIGNED>(a, lds, xcd_swizzle(wg - ndx, ndw));
 }
 
 // ---- the whole backward of a narrow bf16 projection (k, n <= 128) -------------------------
@@ -818,44 +844,51 @@ hipError_t fwd(const LinArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, int R, int DZ, bool AL>
-void bwd_launch(const LinBwdArgs& a, hipStream_t s, bool weights) {
-  if (!weights) {
-    KernelTimer t(K_LIN_BWD_DX, s);
-    hipLaunchKernelGGL((lin_bwd_dx_kernel<T, R, DZ, AL>), dim3((unsigned)tiles_of(a.m, a.k, R)),
-                       dim3(256), 0, s, a);
-  } else {
+// Tiles of dW: 128 wide if that leaves 256 workgroups of at least 512 rows, else 64 wide
+// (fewer splits for as many workgroups, and so fewer partial sums).
+bool wide_w(int64_t m, int k, int n) { return tiles_of(k, n, 128) * ((m + 511) / 512) >= 256; }
+
+template <typename T, int DZ, bool AL>
+void bwd_launch(const LinBwdArgs& a, hipStream_t s) {
+  const bool weights = a.dw || a.dbias, ww = wide_w(a.m, a.k, a.n);
+  const bool wx = wide(tiles_of(a.m, a.k, 128));
+  const unsigned ndx = (unsigned)tiles_of(a.m, a.k, wx ? 128 : 64);
+  const unsigned ndw = (unsigned)(tiles_of(a.k, a.n, ww ? 128 : 64) * a.splits);
+  const dim3 wg(256), both(ndx + ndw);
+  if (a.dx && weights && !wx) {
     KernelTimer t(K_LIN_BWD_W, s);
-    hipLaunchKernelGGL((lin_bwd_w_kernel<T, R, DZ, AL>),
-                       dim3((unsigned)(tiles_of(a.k, a.n, R) * a.splits)), dim3(256), 0, s, a);
+    if (ww) hipLaunchKernelGGL((lin_bwd_both_kernel<T, 128, DZ, AL>), both, wg, 0, s, a, (int)ndx);
+    else hipLaunchKernelGGL((lin_bwd_both_kernel<T, 64, DZ, AL>), both, wg, 0, s, a, (int)ndx);
+    return;
+  }
+  if (a.dx) {
+    KernelTimer t(K_LIN_BWD_DX, s);
+    if (wx) hipLaunchKernelGGL((lin_bwd_dx_kernel<T, 128, DZ, AL>), dim3(ndx), wg, 0, s, a);
+    else hipLaunchKernelGGL((lin_bwd_dx_kernel<T, 64, DZ, AL>), dim3(ndx), wg, 0, s, a);
+  }
+  if (weights) {
+    KernelTimer t(K_LIN_BWD_W, s);
+    if (ww) hipLaunchKernelGGL((lin_bwd_w_kernel<T, 128, DZ, AL>), dim3(ndw), wg, 0, s, a);
+    else hipLaunchKernelGGL((lin_bwd_w_kernel<T, 64, DZ, AL>), dim3(ndw), wg, 0, s, a);
   }
 }
 template <typename T, int DZ>
-void bwd_tile(const LinBwdArgs& a, hipStream_t s, bool weights, bool big) {
-  const bool al = aligned8(a.k, a.n);
-  if (big && al) bwd_launch<T, 128, DZ, true>(a, s, weights);
-  else if (big) bwd_launch<T, 128, DZ, false>(a, s, weights);
-  else if (al) bwd_launch<T, 64, DZ, true>(a, s, weights);
-  else bwd_launch<T, 64, DZ, false>(a, s, weights);
+void bwd_align(const LinBwdArgs& a, hipStream_t s) {
+  if (aligned8(a.k, a.n)) bwd_launch<T, DZ, true>(a, s);
+  else bwd_launch<T, DZ, false>(a, s);
 }
 template <typename T>
-void bwd_part(const LinBwdArgs& a, hipStream_t s, bool weights, bool big) {
-  if (a.act == TRIATTN_ACT_NONE) return bwd_tile<T, DZ_X>(a, s, weights, big);
-  if constexpr (sizeof(T) == 2) {  // dout where z > 0 is a bf16 value: one plane
-    if (a.act == TRIATTN_ACT_RELU) return bwd_tile<T, DZ_RELU>(a, s, weights, big);
-  }
-  if (a.dz) return bwd_tile<T, DZ_MADE>(a, s, weights, big);
-  bwd_tile<T, DZ_ACT>(a, s, weights, big);
+void bwd_products(const LinBwdArgs& a, hipStream_t s) {
+  if (a.act == TRIATTN_ACT_NONE) bwd_align<T, DZ_X>(a, s);
+  else if (a.act == TRIATTN_ACT_RELU) bwd_align<T, DZ_RELU>(a, s);
+  else if (a.dz) bwd_align<T, DZ_MADE>(a, s);
+  else bwd_align<T, DZ_ACT>(a, s);
 }
 
-// Tiles of dW are 128 wide unless k or n would fill no more than half of one.
-bool wide_w(int k, int n) { return k > 64 && n > 64; }
-
-// dz is made beforehand (fp32, in the workspace) where dx has several column tiles, and dW
-// as many: for one, forming it twice moves half the bytes.
-bool make_dz(int dtype, int act, int k) {
-  return act > TRIATTN_ACT_RELU && k > 128 || act == TRIATTN_ACT_RELU && dtype == TRIATTN_F32 && k > 128;
-}
+// A smooth activation's dz is made beforehand (fp32, in the workspace) where dx has several
+// column tiles, and dW as many: for one, forming it twice moves half the bytes.  (relu's
+// costs one comparison wherever it is formed.)
+bool make_dz(int act, int k) { return act > TRIATTN_ACT_RELU && k > 128; }
 
 hipError_t reduce(const LinBwdArgs& a, hipStream_t s) {
   KernelTimer t(K_LIN_REDUCE, s);
@@ -895,31 +928,28 @@ hipError_t bwd(const LinBwdArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(lin_dz_kernel<T>, dim3((unsigned)(wgs < 4096 ? wgs : 4096)), dim3(256), 0, s,
                        a);
   }
-  if (a.dx) bwd_part<T>(a, s, false, wide(tiles_of(a.m, a.k, 128)));
-  if (a.dw || a.dbias) {
-    bwd_part<T>(a, s, true, wide_w(a.k, a.n));
-    if (a.splits > 1) return reduce(a, s);
-  }
-  return hipGetLastError();
+  bwd_products<T>(a, s);
+  return (a.dw || a.dbias) && a.splits > 1 ? reduce(a, s) : hipGetLastError();
 }
-
-}  // namespace
 
 // Splits of the rows for dW: enough workgroups for two rounds of the 256 CUs, each of at
 // least 128 rows.
-static int lin_bwd_splits(int, int64_t m, int k, int n) {
-  const int64_t tiles = tiles_of(k, n, wide_w(k, n) ? 128 : 64);
+int dw_splits(int64_t m, int k, int n) {
+  const int64_t tiles = tiles_of(k, n, wide_w(m, k, n) ? 128 : 64);
   int64_t s = 512 / tiles, most = (m + 127) / 128;
   if (s > most) s = most;
   if (s < 1) s = 1;
   const int64_t per = split_rows(m, (int)s);
   return (int)((m + per - 1) / per);  // no split without rows
 }
+
+}  // namespace
+
 LinBwdPlan lin_bwd_plan(int dtype, int64_t m, int k, int n, int act) {
   LinBwdPlan p{};
-  p.splits = narrow(dtype, k, n) ? narrow_parts(m, act) : lin_bwd_splits(dtype, m, k, n);
+  p.splits = narrow(dtype, k, n) ? narrow_parts(m, act) : dw_splits(m, k, n);
   if (p.splits > 1) p.part = (size_t)p.splits * (size_t)slab_floats(k, n) * sizeof(float);
-  if (make_dz(dtype, act, k)) p.dz = (size_t)m * n * sizeof(float);
+  if (make_dz(act, k) && !narrow(dtype, k, n)) p.dz = (size_t)m * n * sizeof(float);
   return p;
 }
 

@@ -933,12 +933,12 @@ hipError_t bwd(const LinBwdArgs& a, hipStream_t s) {
 }
 
 // Splits of the rows for dW: enough workgroups for two rounds of the 256 CUs, each of at
-// least 128 rows.
+// least 128 rows; none, which needs no further sum, for up to 256 rows.
 int dw_splits(int64_t m, int k, int n) {
   const int64_t tiles = tiles_of(k, n, wide_w(m, k, n) ? 128 : 64);
   int64_t s = 512 / tiles, most = (m + 127) / 128;
   if (s > most) s = most;
-  if (s < 1) s = 1;
+  if (s < 1 || m <= 256) s = 1;
   const int64_t per = split_rows(m, (int)s);
   return (int)((m + per - 1) / per);  // no split without rows
 }

@@ -216,7 +216,9 @@ __global__ __launch_bounds__(LN_WG) void ln_bwd_kernel(LnBwdArgs a) {
     }
   }
   if (!WG) return;
-  float* part = a.part + (int64_t)blockIdx.x * 2 * a.c;
+  // the totals themselves where there is one workgroup
+  float* part_g = gridDim.x > 1 ? a.part + (int64_t)blockIdx.x * 2 * a.c : a.dgamma;
+  float* part_b = gridDim.x > 1 ? part_g + a.c : a.dbeta;
   if (L < 64) {  // the wave's groups
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -259,8 +261,8 @@ __global__ __launch_bounds__(LN_WG) void ln_bwd_kernel(LnBwdArgs a) {
     for (int e = 0; e < N; ++e) {
       const int i = (v * L + lane) * N + e;
       if (i < a.c) {
-        part[i] = dg[v][e];
-        part[a.c + i] = db[v][e];
+        if (part_g) part_g[i] = dg[v][e];
+        if (part_b) part_b[i] = db[v][e];
       }
     }
 }
@@ -345,7 +347,7 @@ hipError_t bwd(const LnBwdArgs& a, hipStream_t s) {
         hipLaunchKernelGGL((ln_bwd_kernel<T, L, V, false>), dim3(a.nwg), dim3(LN_WG), 0, s, a);
     });
   }
-  if (weights) {
+  if (weights && a.nwg > 1) {
     KernelTimer t(K_LN_REDUCE, s);
     hipLaunchKernelGGL(ln_reduce_kernel, dim3(slab_grid(2 * a.c)), dim3(SLAB_WG), 0, s, a.part,
                        a.nwg, a.c, a.dgamma, a.dbeta);
@@ -355,14 +357,14 @@ hipError_t bwd(const LnBwdArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Workgroups (and slabs) of the backward: up to four a CU, but no more than keep the
-// slabs, written and read once, at a tenth of the rows' traffic (3 values an element) --
-// unless there are so few rows that filling the CUs counts for more.
+// Workgroups (and slabs) of the backward: up to four a CU, fewer where their slabs,
+// written and read once, would pass a third of the rows' traffic (3 values an element),
+// and one alone, which needs no further sum, for up to 4 rounds.
 int ln_bwd_parts(int dtype, int64_t m, int c) {
   const int e = dtype == TRIATTN_BF16 ? 2 : 4;
   const int64_t groups = row_groups((c * e + 15) / 16, m);
-  int64_t most = m * e * 3 / 160;
-  most = most < 256 ? 256 : most > 1024 ? 1024 : most;
+  int64_t most = m * e / 16;
+  most = groups <= 4 ? 1 : most < 256 ? 256 : most > 1024 ? 1024 : most;
   return (int)(groups < most ? groups : most);
 }
 

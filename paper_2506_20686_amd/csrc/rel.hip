@@ -38,7 +38,9 @@ __device__ inline int bucket_of(const RelArgs& a, const Buckets& b, int32_t pq, 
   if constexpr (LUT) {
     const int32_t d = __builtin_elementwise_sub_sat(
         __builtin_elementwise_sub_sat(pq, pk), a.low);
-    return b.lut[min(max(d, 0), a.span)];
+    int32_t i;  // d clipped to [0, span]
+    asm("v_med3_i32 %0, %1, 0, %2" : "=v"(i) : "v"(d), "s"(a.span));
+    return b.lut[i];
   } else {
     const int64_t d = (int64_t)pq - (int64_t)pk;
     int lo = 0, hi = a.ne;
@@ -49,11 +51,6 @@ __device__ inline int bucket_of(const RelArgs& a, const Buckets& b, int32_t pq, 
     }
     return lo;
   }
-}
-
-// Value of a row's uniform index, by a scalar load (the arrays are only read here).
-__device__ inline int32_t uniform(const int32_t* p, int64_t i) {
-  return *(const __attribute__((address_space(4))) int32_t*)(p + i);
 }
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
@@ -156,7 +153,7 @@ struct RelPlan {
   int units;   // row chunks of a sample
   int qlen;    // rows of a chunk
   int w;       // workgroups that share a key block's units
-  int slabs() const { return w * kblocks; }
+  __host__ __device__ int slabs() const { return w * kblocks; }
 };
 
 __host__ __device__ inline RelPlan rel_plan(int64_t batch, int n, int h, int rows) {
@@ -167,9 +164,10 @@ __host__ __device__ inline RelPlan rel_plan(int64_t batch, int n, int h, int row
   p.waves = rows <= 64 + 8 ? 4 : rows <= 128 + 8 ? 2 : 1;
   const int keys = p.pl * REL_K * p.waves;
   p.kblocks = (n + keys - 1) / keys;
-  // about two workgroups a CU, and at least 4 rows to each
+  // about two workgroups a CU, and at least 4 rows to each; one alone, which needs no
+  // further sum, for up to 32 rows
   int64_t want = 512 / (p.groups * p.kblocks);
-  if (want < 1) want = 1;
+  if (want < 1 || (p.groups * p.kblocks == 1 && batch * n <= 32)) want = 1;
   int64_t per = (batch * n + want - 1) / want;
   if (per < REL_Q) per = REL_Q;
   p.qlen = (int)(per < n ? per : n);
@@ -232,59 +230,67 @@ __global__ __launch_bounds__(256) void rel_bwd_kernel(RelArgs a, RelPlan p) {
       }
     };
     load(q0);
+    int32_t prow = 0, crow = 0;  // lane i: position and chain of row i of the current 64
     for (int q = q0; q < q1; q += REL_Q) {
-      int r[REL_Q][REL_K];
-#pragma unroll
-      for (int v = 0; v < REL_Q; ++v) {
-        const int64_t row = b0 + min(q + v, q1 - 1);
-        const int32_t pq = uniform(a.pos, row), cq = CHAIN ? uniform(a.chain, row) : 0;
-#pragma unroll
-        for (int u = 0; u < REL_K; ++u) {
-          r[v][u] = bucket_of<LUT>(a, buckets, pq, pk[u]);
-          if (CHAIN && ck[u] != cq) r[v][u] = a.ne + 1;
-        }
+      if ((q - q0) % 64 == 0) {
+        const int64_t row = b0 + min(q + lane, q1 - 1);
+        prow = a.pos[row];
+        crow = CHAIN ? a.chain[row] : 0;
       }
       float f[REL_Q][REL_K];
 #pragma unroll
       for (int v = 0; v < REL_Q; ++v)
 #pragma unroll
         for (int u = 0; u < REL_K; ++u) f[v][u] = x[v][u];
+      // the next rows' loads leave now, not where the scheduler finds registers for them
+      __builtin_amdgcn_sched_barrier(0);
       load(q + REL_Q);
-      // four elements of a row at a time: their sums are read together; one that falls
-      // into an earlier one's bucket goes on from that one's new value, and the last
-      // write of a bucket is the one that stays
+      __builtin_amdgcn_sched_barrier(0);
+      int r[REL_Q][REL_K];
 #pragma unroll
       for (int v = 0; v < REL_Q; ++v) {
-        float s[REL_K];
-#pragma unroll
-        for (int u = 0; u < REL_K; ++u) s[u] = column[r[v][u] * 64];
+        const int32_t pq = __builtin_amdgcn_readlane(prow, (q - q0) % 64 + v);
+        const int32_t cq = CHAIN ? __builtin_amdgcn_readlane(crow, (q - q0) % 64 + v) : 0;
 #pragma unroll
         for (int u = 0; u < REL_K; ++u) {
-#pragma unroll
-          for (int e = 0; e < u; ++e) s[u] = r[v][e] == r[v][u] ? s[e] : s[u];
-          s[u] += f[v][u];
+          r[v][u] = bucket_of<LUT>(a, buckets, pq, pk[u]);
+          if (CHAIN && ck[u] != cq) r[v][u] = a.ne + 1;
         }
-#pragma unroll
-        for (int u = 0; u < REL_K; ++u) column[r[v][u] * 64] = s[u];
       }
+      // two at a time, which halves the chain of dependent LDS accesses: if both fall into
+      // one bucket, the second goes on from the first one's new value and its write stays
+#pragma unroll
+      for (int v = 0; v < REL_Q; ++v)
+#pragma unroll
+        for (int u = 0; u < REL_K; u += 2) {
+          float *s0 = column + r[v][u] * 64, *s1 = column + r[v][u + 1] * 64;
+          const float x0 = *s0, x1 = *s1, y0 = x0 + f[v][u];
+          *s0 = y0;
+          *s1 = (s1 == s0 ? y0 : x1) + f[v][u + 1];
+        }
     }
   }
   __syncthreads();
-  // channel c of row r: the lanes off * hc + c of every wave, beginning at another one in
-  // every row so that the rows' reads fall into different banks
-  float* slab = a.part + (int64_t)blockIdx.x * a.rows * a.h;
+  // the waves' sums onto the first wave's, row by row
+  for (int i = threadIdx.x; i < a.rows * 64; i += blockDim.x) {
+    float s = sums[i];
+    for (int v = 1; v < p.waves; ++v) s += sums[v * a.rows * 64 + i];
+    sums[i] = s;
+  }
+  __syncthreads();
+  // channel c of row r: the lanes off * hc + c, beginning at another one in every row so that
+  // the rows' reads fall into different banks
+  float* slab = p.slabs() > 1 ? a.part + (int64_t)blockIdx.x * a.rows * a.h : a.dtable;
   for (int i = threadIdx.x; i < a.rows * p.hc; i += blockDim.x) {
     const int r = i / p.hc, ch = i - r * p.hc;
     if (c0 + ch >= a.h) continue;
+    const float* row = sums + r * 64 + ch;
     float s = 0.f;
-    const int first = r % p.pl;
-    for (int v = 0; v < p.waves; ++v) {
-      const float* row = sums + (v * a.rows + r) * 64 + ch;
-#pragma unroll 8
-      for (int t = 0; t < p.pl; ++t) {
-        const int at = first + t;
-        s += row[(at < p.pl ? at : at - p.pl) * p.hc];
-      }
+    int at = r % p.pl;
+#pragma unroll 4
+    for (int t = 0; t < p.pl; ++t) {
+      s += row[at * p.hc];
+      at = at + 1 == p.pl ? 0 : at + 1;
     }
     slab[r * a.h + c0 + ch] = s;
   }
@@ -357,6 +363,7 @@ hipError_t bwd(RelArgs a, hipStream_t s) {
     else if (a.chain) hipLaunchKernelGGL((rel_bwd_kernel<T, false, true>), grid, wg, lds, s, a, p);
     else hipLaunchKernelGGL((rel_bwd_kernel<T, false, false>), grid, wg, lds, s, a, p);
   }
+  if (p.slabs() == 1) return hipGetLastError();
   KernelTimer t(K_REL_REDUCE, s);
   const int total = a.rows * a.h;
   hipLaunchKernelGGL(rel_reduce_kernel, dim3(slab_grid(total)), dim3(SLAB_WG), 0, s, a.part,

@@ -92,6 +92,31 @@ struct __attribute__((packed)) Any16 {
   u32x4 v;
 };
 
+// The first `have` of 8 values (zeros after them); ALIGNED: all of them, at 16 bytes.  A
+// partial chunk is 8 loads at once, those past its end of its last element.
+template <typename T, bool ALIGNED>
+__device__ inline Raw8<T> get8(const T* p, int have) {
+  Raw8<T> r{};
+  if (ALIGNED) {
+#pragma unroll
+    for (int i = 0; i < Raw8<T>::N; ++i) r.v[i] = ((const u32x4*)p)[i];
+  } else if (have >= 8) {
+#pragma unroll
+    for (int i = 0; i < Raw8<T>::N; ++i) r.v[i] = ((const Any16*)p)[i].v;
+  } else {
+    struct E {
+      T e[8];
+    } y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y.e[i] = p[min(i, have - 1)];
+#pragma unroll
+    for (int i = 1; i < 8; ++i)
+      if (i >= have) y.e[i] = (T)0.f;
+    r = __builtin_bit_cast(Raw8<T>, y);
+  }
+  return r;
+}
+
 // A row-major matrix [rows][cols] seen from a tile's corner.
 template <typename T>
 struct Mat {
@@ -100,41 +125,62 @@ struct Mat {
   int cols;
 };
 
-// Chunk (r, c .. c + 7) of the window at (r0, c0) of a matrix, `lim` rows high: zeros
-// outside.  ALIGNED: the width is a multiple of 8 elements, so a chunk is all in or all
-// out and the buffer resource's range check gives the zeros.  Otherwise rows start at any
-// element (16-byte loads may), and a row's last chunk goes element by element.
-template <typename T, bool ALIGNED>
+// Chunk (r, c .. c + 7) of the window at (r0, c0) of a matrix whose width is a multiple of
+// 8 elements, `lim` rows high: zeros outside.  A chunk is all in or all out, and the
+// buffer resource's range check gives the zeros.
+template <typename T>
 __device__ inline Raw8<T> fetch(const Mat<T>& m, int64_t r0, int c0, int lim, int r, int c) {
-  Raw8<T> x{};
+  Raw8<T> x;
   const int64_t left = c0 < m.cols ? m.rows - r0 : 0;
   const int rows = left < lim ? (left < 0 ? 0 : (int)left) : lim;
   const T* base = m.p + r0 * m.cols + c0;
-  if constexpr (ALIGNED) {
-    // the last row's end past the corner; a row is at most 32 KB, a window 4 MB
-    const rsrc_t rs = buf_rsrc_n(base, rows ? (uint32_t)(rows * m.cols - c0) * sizeof(T) : 0u);
-    const uint32_t off = c0 + c < m.cols ? (uint32_t)(r * m.cols + c) * sizeof(T) : 0x80000000u;
+  // the last row's end past the corner; a row is at most 32 KB, a window 4 MB
+  const rsrc_t rs = buf_rsrc_n(base, rows ? (uint32_t)(rows * m.cols - c0) * sizeof(T) : 0u);
+  const uint32_t off = c0 + c < m.cols ? (uint32_t)(r * m.cols + c) * sizeof(T) : 0x80000000u;
 #pragma unroll
-    for (int i = 0; i < Raw8<T>::N; ++i)
-      x.v[i] = __builtin_bit_cast(
-          u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(off + 16 * i), 0, 0));
-  } else if (r < rows) {
-    const T* s = base + (int64_t)r * m.cols + c;
-    const int have = m.cols - (c0 + c);
-    if (have >= 8) {
-#pragma unroll
-      for (int i = 0; i < Raw8<T>::N; ++i) x.v[i] = ((const Any16*)s)[i].v;
-    } else if (have > 0) {
-      struct E {
-        T e[8];
-      } y{};
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < have) y.e[i] = s[i];
-      x = __builtin_bit_cast(Raw8<T>, y);
-    }
-  }
+  for (int i = 0; i < Raw8<T>::N; ++i)
+    x.v[i] = __builtin_bit_cast(
+        u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(off + 16 * i), 0, 0));
   return x;
+}
+
+// The same of any width: rows start at any element (16-byte loads may), a row's last chunk
+// runs on into the next row, and what would pass the matrix's end is read from its last 8
+// elements.  `info` says what to make of it once it is needed (in repair): the valid
+// elements in bits 0..3, how far they lie behind in bits 4..6.  So the load itself has no
+// condition and nothing waits for it.  Matrices of fewer than 8 elements go element by
+// element.
+template <typename T>
+__device__ inline Raw8<T> fetch_any(const Mat<T>& m, int64_t r0, int c0, int lim, int r, int c,
+                                    int& info) {
+  const int64_t total = m.rows * m.cols, at = (r0 + r) * m.cols + c0 + c;
+  const int have = r < lim && r0 + r < m.rows ? min(max(m.cols - (c0 + c), 0), 8) : 0;
+  if (total < 8) {
+    info = 8;
+    return have > 0 ? get8<T, false>(m.p + at, have) : Raw8<T>{};
+  }
+  const int64_t last = total - 8, from = at < last ? at : last;
+  info = have | (have > 0 ? (int)(at - from) << 4 : 0);
+  Raw8<T> x;
+#pragma unroll
+  for (int i = 0; i < Raw8<T>::N; ++i) x.v[i] = ((const Any16*)(m.p + from))[i].v;
+  return x;
+}
+template <typename T>
+__device__ inline Raw8<T> repair(const Raw8<T>& x, int info) {
+  if (info == 8) return x;
+  struct E {
+    T e[8];
+  } y = __builtin_bit_cast(E, x);
+#pragma unroll
+  for (int bit = 1; bit < 8; bit *= 2)
+    if (info & (bit << 4))
+#pragma unroll
+      for (int i = 0; i + bit < 8; ++i) y.e[i] = y.e[i + bit];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i >= (info & 15)) y.e[i] = (T)0.f;
+  return __builtin_bit_cast(Raw8<T>, y);
 }
 
 // One operand's tile of R rows x BK contraction indices in LDS, as P planes of bf16.
@@ -189,27 +235,40 @@ struct Stage {
   using L = Tile<R, BK, KM, P>;
   static constexpr int N = R * BK / 8 / 256;  // chunks a thread
   Raw8<T> x[N], z[DZ == DZ_X ? 1 : N];
+  int info[ALIGNED ? 1 : N];
 
   // Tile at rows i0, indices k0 (of k1): lines are rows (K major) or indices.
   __device__ inline void load(const Mat<T>& m, const T* zp, int64_t i0, int64_t k0, int64_t k1) {
     Mat<T> w = m;
-    if (!KM) w.rows = k1;
+    if (!KM && ALIGNED) w.rows = k1;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int id = (int)threadIdx.x + 256 * u, line = id / L::LINE, c = 8 * (id % L::LINE);
       const int64_t r0 = KM ? i0 : k0;
-      const int c0 = (int)(KM ? k0 : i0), lim = KM ? R : BK;
-      x[u] = fetch<T, ALIGNED>(w, r0, c0, lim, line, c);
-      if constexpr (DZ != DZ_X)
-        z[u] = fetch<T, ALIGNED>(Mat<T>{zp, w.rows, w.cols}, r0, c0, lim, line, c);
+      const int c0 = (int)(KM ? k0 : i0);
+      if constexpr (ALIGNED) {
+        x[u] = fetch<T>(w, r0, c0, KM ? R : BK, line, c);
+        if constexpr (DZ != DZ_X) z[u] = fetch<T>(Mat<T>{zp, w.rows, w.cols}, r0, c0, KM ? R : BK, line, c);
+      } else {
+        const int lim = KM ? R : (int)(k1 - k0 < BK ? k1 - k0 : BK);
+        x[u] = fetch_any<T>(w, r0, c0, lim, line, c, info[u]);
+        if constexpr (DZ != DZ_X) {
+          int same;
+          z[u] = fetch_any<T>(Mat<T>{zp, w.rows, w.cols}, r0, c0, lim, line, c, same);
+        }
+      }
     }
+  }
+  __device__ inline Raw8<T> raw(const Raw8<T>& r, int u) const {
+    if constexpr (ALIGNED) return r;
+    else return repair(r, info[u]);
   }
   // The values of chunk u.
   __device__ inline void values(int u, int act, float (&f)[8]) const {
-    unpack(x[u], f);
+    unpack(raw(x[u], u), f);
     if constexpr (DZ != DZ_X) {
       float g[8];
-      unpack(z[u], g);
+      unpack(raw(z[u], u), g);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         f[e] = DZ == DZ_RELU ? (g[e] > 0.f ? f[e] : 0.f) : f[e] * act_grad(g[e], act);
@@ -230,7 +289,7 @@ struct Stage {
         for (int e = 0; e < 8; ++e) col[e] += f[e];
       }
       if constexpr (P == 1 && DZ == DZ_X) {
-        *(u32x4*)d = x[u].v[0];
+        *(u32x4*)d = raw(x[u], u).v[0];
       } else {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -283,29 +342,32 @@ struct Product {
       sa[d].load(a, az, i0, k0 + (int64_t)it * BK, k1);
       sb[d].load(b, bz, j0, k0 + (int64_t)it * BK, k1);
     };
-    auto step = [&](int d, char* buf, int next) {
+    auto step = [&](int d, char* buf, int it) {
+      const int next = it + D;
+      const int64_t left = k1 - k0 - (int64_t)it * BK;  // indices of this step and on
       float none[8];
       sa[d].template store<false>(buf, act, false, none);
       sb[d].template store<SUM>(buf + LA::BYTES, act, sum, col);
       load(d, next);
       // this buffer was last read two steps ago, before the barrier of the last step
       __syncthreads();
-      multiply(buf, ri, rj, lane, acc);
+      multiply(buf, ri, rj, lane, left, acc);
     };
 #pragma unroll
     for (int d = 0; d < D; ++d) load(d, d);
     int it = 0;
     for (; it + 2 <= steps; it += 2) {
-      step(0, lds, it + D);
-      step(D - 1, lds + BUF, it + 1 + D);
+      step(0, lds, it);
+      step(D - 1, lds + BUF, it + 1);
     }
-    if (it < steps) step(0, lds, it + D);
+    if (it < steps) step(0, lds, it);
   }
 
-  __device__ static inline void multiply(const char* buf, int ri, int rj, int lane,
+  __device__ static inline void multiply(const char* buf, int ri, int rj, int lane, int64_t left,
                                          f32x16 (&acc)[NT][NT]) {
 #pragma unroll
     for (int kk = 0; kk < BK; kk += 16) {
+      if (kk > 0 && kk >= left) break;
       bf16x8 fa[PA][NT], fb[PB][NT];
 #pragma unroll
       for (int p = 0; p < PA; ++p)
@@ -400,28 +462,6 @@ __device__ inline void put8(T* p, int have, const float (&f)[8]) {
       if (i < have) p[i] = y.e[i];
   }
 }
-// The first `have` of 8 values (zeros after them); ALIGNED: all of them, at 16 bytes.
-template <typename T, bool ALIGNED>
-__device__ inline Raw8<T> get8(const T* p, int have) {
-  Raw8<T> r{};
-  if (ALIGNED) {
-#pragma unroll
-    for (int i = 0; i < Raw8<T>::N; ++i) r.v[i] = ((const u32x4*)p)[i];
-  } else if (have >= 8) {
-#pragma unroll
-    for (int i = 0; i < Raw8<T>::N; ++i) r.v[i] = ((const Any16*)p)[i].v;
-  } else {
-    struct E {
-      T e[8];
-    } y{};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < have) y.e[i] = p[i];
-    r = __builtin_bit_cast(Raw8<T>, y);
-  }
-  return r;
-}
-
 // Contraction indices a step: 64 while the two buffers leave room for two workgroups on a
 // CU, else 32 (three planes of each operand, or of one and 128 rows).
 constexpr int step_k(int r, int planes) { return r * planes <= 256 ? 64 : 32; }
@@ -665,16 +705,16 @@ __global__ __launch_bounds__(NARROW_WG) void lin_narrow_kernel(LinBwdArgs a) {
   for (int u = 0; u < 4; ++u) {
     const int line = line0 + 32 * u;
     *(u32x4*)(tw + Square::chunk_at(line, chunk)) =
-        fetch<bf16, true>(mw, 0, 0, 128, line, 8 * chunk).v[0];
+        fetch<bf16>(mw, 0, 0, 128, line, 8 * chunk).v[0];
   }
   Raw8<bf16> x[N], d[N], z[DZ == DZ_X ? 1 : N];
   auto load = [&](int64_t r0) {
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int line = line0 + 32 * u;
-      x[u] = fetch<bf16, true>(mx, r0, 0, M, line, 8 * chunk);
-      d[u] = fetch<bf16, true>(md, r0, 0, M, line, 8 * chunk);
-      if constexpr (DZ != DZ_X) z[u] = fetch<bf16, true>(mz, r0, 0, M, line, 8 * chunk);
+      x[u] = fetch<bf16>(mx, r0, 0, M, line, 8 * chunk);
+      d[u] = fetch<bf16>(md, r0, 0, M, line, 8 * chunk);
+      if constexpr (DZ != DZ_X) z[u] = fetch<bf16>(mz, r0, 0, M, line, 8 * chunk);
     }
   };
   // this wave's tiles: dx rows di .. + 31, columns dj .. + JW - 1; dW rows (of k) wi .. + 31,
@@ -828,14 +868,20 @@ __global__ __launch_bounds__(256) void lin_reduce_kernel(LinBwdArgs a, int slice
 bool aligned8(int k, int n) { return k % 8 == 0 && n % 8 == 0; }
 int64_t tiles_of(int64_t m, int64_t n, int r) { return (m + r - 1) / r * ((n + r - 1) / r); }
 
-// 128-wide tiles where there are enough of them for the 256 CUs, else 64-wide ones (four
-// times as many, at half the reuse of an operand).
-bool wide(int64_t tiles128) { return tiles128 >= 256; }
+// 128-wide tiles of an [m][width] result where there are enough of them for the 256 CUs and
+// a second half of a tile to fill, else 64-wide ones (four times as many, at half the reuse
+// of an operand).  fp32 tiles of 128 leave one workgroup on a CU (96 KB of planes), which
+// pays where the products and not the memory take the time: from 256 terms a sum on
+// (measured, 300,000 x 32 x 72 fp32: 73 us in tiles of 128, see the table of cases).
+template <typename T>
+bool wide(int64_t m, int width, int terms) {
+  return width > 64 && tiles_of(m, width, 128) >= 256 && (sizeof(T) == 2 || terms >= 256);
+}
 
 template <typename T>
 hipError_t fwd(const LinArgs& a, hipStream_t s) {
   KernelTimer t(K_LIN_FWD, s);
-  const bool big = wide(tiles_of(a.m, a.n, 128)), al = aligned8(a.k, a.n);
+  const bool big = wide<T>(a.m, a.n, a.k), al = aligned8(a.k, a.n);
   const dim3 grid((unsigned)tiles_of(a.m, a.n, big ? 128 : 64)), wg(256);
   if (big && al) hipLaunchKernelGGL((lin_fwd_kernel<T, 128, true>), grid, wg, 0, s, a);
   else if (big) hipLaunchKernelGGL((lin_fwd_kernel<T, 128, false>), grid, wg, 0, s, a);
@@ -845,13 +891,16 @@ hipError_t fwd(const LinArgs& a, hipStream_t s) {
 }
 
 // Tiles of dW: 128 wide if that leaves 256 workgroups of at least 512 rows, else 64 wide
-// (fewer splits for as many workgroups, and so fewer partial sums).
-bool wide_w(int64_t m, int k, int n) { return tiles_of(k, n, 128) * ((m + 511) / 512) >= 256; }
+// (fewer splits for as many workgroups, and so fewer partial sums) or if k or n fills no
+// more than half of one.
+bool wide_w(int64_t m, int k, int n) {
+  return k > 64 && n > 64 && tiles_of(k, n, 128) * ((m + 511) / 512) >= 256;
+}
 
 template <typename T, int DZ, bool AL>
 void bwd_launch(const LinBwdArgs& a, hipStream_t s) {
   const bool weights = a.dw || a.dbias, ww = wide_w(a.m, a.k, a.n);
-  const bool wx = wide(tiles_of(a.m, a.k, 128));
+  const bool wx = wide<T>(a.m, a.k, a.n);
   const unsigned ndx = (unsigned)tiles_of(a.m, a.k, wx ? 128 : 64);
   const unsigned ndw = (unsigned)(tiles_of(a.k, a.n, ww ? 128 : 64) * a.splits);
   const dim3 wg(256), both(ndx + ndw);

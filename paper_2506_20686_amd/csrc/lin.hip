@@ -131,8 +131,10 @@ struct Mat {
 template <typename T>
 __device__ inline Raw8<T> fetch(const Mat<T>& m, int64_t r0, int c0, int lim, int r, int c) {
   Raw8<T> x;
-  const int64_t left = c0 < m.cols ? m.rows - r0 : 0;
-  const int rows = left < lim ? (left < 0 ? 0 : (int)left) : lim;
+  // rows of the window inside the matrix; the step after the last one may lie past the end,
+  // and `lim` be negative there
+  const int64_t left = c0 < m.cols ? m.rows - r0 : 0, high = left < lim ? left : lim;
+  const int rows = high > 0 ? (int)high : 0;
   const T* base = m.p + r0 * m.cols + c0;
   // the last row's end past the corner; a row is at most 32 KB, a window 4 MB
   const rsrc_t rs = buf_rsrc_n(base, rows ? (uint32_t)(rows * m.cols - c0) * sizeof(T) : 0u);
@@ -147,23 +149,32 @@ __device__ inline Raw8<T> fetch(const Mat<T>& m, int64_t r0, int c0, int lim, in
 // The same of any width: rows start at any element (16-byte loads may), a row's last chunk
 // runs on into the next row, and what would pass the matrix's end is read from its last 8
 // elements.  `info` says what to make of it once it is needed (in repair): the valid
-// elements in bits 0..3, how far they lie behind in bits 4..6.  So the load itself has no
-// condition and nothing waits for it.  Matrices of fewer than 8 elements go element by
+// elements in bits 0..3, how far they lie behind in bits 4..6.  So nothing waits for a load
+// before its values are stored.  Matrices of fewer than 8 elements go element by
 // element.
 template <typename T>
 __device__ inline Raw8<T> fetch_any(const Mat<T>& m, int64_t r0, int c0, int lim, int r, int c,
                                     int& info) {
-  const int64_t total = m.rows * m.cols, at = (r0 + r) * m.cols + c0 + c;
+  if (m.cols % 8 == 0) {  // this matrix's rows are whole chunks after all
+    info = 8;
+    return fetch<T>(m, r0, c0, lim, r, c);
+  }
+  const int64_t total = m.rows * m.cols, corner = r0 * m.cols + c0;
   const int have = r < lim && r0 + r < m.rows ? min(max(m.cols - (c0 + c), 0), 8) : 0;
   if (total < 8) {
     info = 8;
-    return have > 0 ? get8<T, false>(m.p + at, have) : Raw8<T>{};
+    return have > 0 ? get8<T, false>(m.p + corner + (int64_t)r * m.cols + c, have) : Raw8<T>{};
   }
-  const int64_t last = total - 8, from = at < last ? at : last;
-  info = have | (have > 0 ? (int)(at - from) << 4 : 0);
+  // 32-bit offsets from the corner, or from the last 8 elements if it lies past those
+  const int64_t last = total - 8, from = corner < last ? corner : last;
+  const int room = last - from < 0x7fffffff ? (int)(last - from) : 0x7fffffff;
+  const int at = r * m.cols + c + (int)(corner - from), in = min(at, room);
+  info = have | (have > 0 ? (at - in) << 4 : 0);
   Raw8<T> x;
+  if (have > 0) {
 #pragma unroll
-  for (int i = 0; i < Raw8<T>::N; ++i) x.v[i] = ((const Any16*)(m.p + from))[i].v;
+    for (int i = 0; i < Raw8<T>::N; ++i) x.v[i] = ((const Any16*)(m.p + from + in))[i].v;
+  }
   return x;
 }
 template <typename T>
@@ -318,8 +329,8 @@ struct Product {
   using LA = typename SA::L;
   using LB = typename SB::L;
   static constexpr int BUF = LA::BYTES + LB::BYTES;
-  // steps whose loads are in flight: two where the registers allow two workgroups on a CU
-  static constexpr int D = R == 64 ? 2 : 1;
+  // steps whose loads are in flight: two where the registers allow three workgroups on a CU
+  static constexpr int D = R == 64 && ALIGNED ? 2 : 1;
   static constexpr int EPI = 4 * 32 * (R / 2 + 4) * 4;  // the result's staging
   static constexpr int LDS = 2 * BUF > EPI ? 2 * BUF : EPI;
 
@@ -443,13 +454,7 @@ struct Product {
 
 // Writes the first `have` of 8 values to p; ALIGNED: all of them, at 16 bytes.
 template <typename T, bool ALIGNED>
-__device__ inline void put8(T* p, int have, const float (&f)[8]) {
-  struct E {
-    T e[8];
-  } y;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) y.e[i] = (T)f[i];
-  const Raw8<T> r = __builtin_bit_cast(Raw8<T>, y);
+__device__ inline void put_raw(T* p, int have, const Raw8<T>& r) {
   if (ALIGNED) {
 #pragma unroll
     for (int i = 0; i < Raw8<T>::N; ++i) ((u32x4*)p)[i] = r.v[i];
@@ -457,11 +462,24 @@ __device__ inline void put8(T* p, int have, const float (&f)[8]) {
 #pragma unroll
     for (int i = 0; i < Raw8<T>::N; ++i) ((Any16*)p)[i].v = r.v[i];
   } else {
+    struct E {
+      T e[8];
+    } y = __builtin_bit_cast(E, r);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i < have) p[i] = y.e[i];
   }
 }
+template <typename T, bool ALIGNED>
+__device__ inline void put8(T* p, int have, const float (&f)[8]) {
+  struct E {
+    T e[8];
+  } y;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y.e[i] = (T)f[i];
+  put_raw<T, ALIGNED>(p, have, __builtin_bit_cast(Raw8<T>, y));
+}
+
 // Contraction indices a step: 64 while the two buffers leave room for two workgroups on a
 // CU, else 32 (three planes of each operand, or of one and 128 rows).
 constexpr int step_k(int r, int planes) { return r * planes <= 256 ? 64 : 32; }
@@ -658,7 +676,8 @@ __global__ __launch_bounds__(256) void lin_bwd_both_kernel(LinBwdArgs a, int ndx
 // end).  The next block's loads are in flight meanwhile.  dx goes through x's place in LDS,
 // each wave's part by itself, to be stored in whole rows' pieces.
 //
-// M = 128, or 64 where dz takes three planes (96 KB of LDS either way).
+// M = 128, or 64 where dz takes three planes (96 KB of LDS either way) or where the repair
+// of ragged rows would not fit the registers beside two times 128 rows.
 // 589,824 x 128 x 128: 143 us by the two kernels and their sums, see lin_narrow below.
 struct Square {  // lines of 128 bf16, read along and across
   // Both reads are free of bank conflicts: s differs between any 16 consecutive lines
@@ -686,12 +705,14 @@ struct Square {  // lines of 128 bf16, read along and across
 };
 
 constexpr int NARROW_WG = 512;
-constexpr int narrow_rows(int dz) { return dz == DZ_ACT ? 64 : 128; }
+constexpr int narrow_rows(int dz, bool aligned) {
+  return dz == DZ_ACT || !aligned ? 64 : 128;
+}
 
-template <int DZ>
+template <int DZ, bool ALIGNED>
 __global__ __launch_bounds__(NARROW_WG) void lin_narrow_kernel(LinBwdArgs a) {
   using S = DzSource<bf16, DZ>;
-  constexpr int M = narrow_rows(DZ), N = M / 32;       // chunks a thread stages of a tile
+  constexpr int M = narrow_rows(DZ, ALIGNED), N = M / 32;       // chunks a thread stages of a tile
   constexpr int JT = M / 64, JW = 32 * JT;             // dx tiles, columns of a wave
   constexpr int TILE_BYTES = M * 256, W_BYTES = 128 * 256;
   __shared__ __attribute__((aligned(16))) char lds[W_BYTES + (1 + S::Q) * TILE_BYTES];
@@ -704,17 +725,28 @@ __global__ __launch_bounds__(NARROW_WG) void lin_narrow_kernel(LinBwdArgs a) {
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int line = line0 + 32 * u;
-    *(u32x4*)(tw + Square::chunk_at(line, chunk)) =
-        fetch<bf16>(mw, 0, 0, 128, line, 8 * chunk).v[0];
+    int info = 8;
+    Raw8<bf16> w;
+    if constexpr (ALIGNED) w = fetch<bf16>(mw, 0, 0, 128, line, 8 * chunk);
+    else w = fetch_any<bf16>(mw, 0, 0, 128, line, 8 * chunk, info);
+    *(u32x4*)(tw + Square::chunk_at(line, chunk)) = repair(w, info).v[0];
   }
   Raw8<bf16> x[N], d[N], z[DZ == DZ_X ? 1 : N];
+  int xi[N], ni[N];
   auto load = [&](int64_t r0) {
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int line = line0 + 32 * u;
-      x[u] = fetch<bf16>(mx, r0, 0, M, line, 8 * chunk);
-      d[u] = fetch<bf16>(md, r0, 0, M, line, 8 * chunk);
-      if constexpr (DZ != DZ_X) z[u] = fetch<bf16>(mz, r0, 0, M, line, 8 * chunk);
+      xi[u] = ni[u] = 8;
+      if constexpr (ALIGNED) {
+        x[u] = fetch<bf16>(mx, r0, 0, M, line, 8 * chunk);
+        d[u] = fetch<bf16>(md, r0, 0, M, line, 8 * chunk);
+        if constexpr (DZ != DZ_X) z[u] = fetch<bf16>(mz, r0, 0, M, line, 8 * chunk);
+      } else {
+        x[u] = fetch_any<bf16>(mx, r0, 0, M, line, 8 * chunk, xi[u]);
+        d[u] = fetch_any<bf16>(md, r0, 0, M, line, 8 * chunk, ni[u]);
+        if constexpr (DZ != DZ_X) z[u] = fetch_any<bf16>(mz, r0, 0, M, line, 8 * chunk, ni[u]);
+      }
     }
   };
   // this wave's tiles: dx rows di .. + 31, columns dj .. + JW - 1; dW rows (of k) wi .. + 31,
@@ -729,12 +761,12 @@ __global__ __launch_bounds__(NARROW_WG) void lin_narrow_kernel(LinBwdArgs a) {
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int at = Square::chunk_at(line0 + 32 * u, chunk);
-      *(u32x4*)(tx + at) = x[u].v[0];
+      *(u32x4*)(tx + at) = repair(x[u], xi[u]).v[0];
       float f[8];
-      unpack(d[u], f);
+      unpack(repair(d[u], ni[u]), f);
       if constexpr (DZ != DZ_X) {
         float g[8];
-        unpack(z[u], g);
+        unpack(repair(z[u], ni[u]), g);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           f[e] = DZ == DZ_RELU ? (g[e] > 0.f ? f[e] : 0.f) : f[e] * act_grad(g[e], a.act);
@@ -803,8 +835,9 @@ __global__ __launch_bounds__(NARROW_WG) void lin_narrow_kernel(LinBwdArgs a) {
 #pragma unroll
       for (int s = 0; s < 32; s += 64 / CH) {
         const int i = s + lane / CH;
-        const u32x4 o = *(const u32x4*)at(i, lane % CH);
-        if (r0 + di + i < a.m && j < a.k) *(u32x4*)((bf16*)a.dx + (r0 + di + i) * a.k + j) = o;
+        const Raw8<bf16> o = *(const Raw8<bf16>*)at(i, lane % CH);
+        if (r0 + di + i < a.m && j < a.k)
+          put_raw<bf16, ALIGNED>((bf16*)a.dx + (r0 + di + i) * a.k + j, a.k - j, o);
       }
     }
   }
@@ -818,9 +851,15 @@ __global__ __launch_bounds__(NARROW_WG) void lin_narrow_kernel(LinBwdArgs a) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int j = wj + 32 * v + 8 * q + 4 * (lane >> 5);
-        if (j < a.n)
-          *(f32x4*)(dw + i * a.n + j) =
-              f32x4{gw[v][4 * q], gw[v][4 * q + 1], gw[v][4 * q + 2], gw[v][4 * q + 3]};
+        if (ALIGNED) {
+          if (j < a.n)
+            *(f32x4*)(dw + i * a.n + j) =
+                f32x4{gw[v][4 * q], gw[v][4 * q + 1], gw[v][4 * q + 2], gw[v][4 * q + 3]};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (j + e < a.n) dw[i * a.n + j + e] = gw[v][4 * q + e];
+        }
       }
   if (a.dbias) {  // the threads of a column, in order
     __syncthreads();
@@ -881,10 +920,11 @@ bool wide(int64_t m, int width, int terms) {
 template <typename T>
 hipError_t fwd(const LinArgs& a, hipStream_t s) {
   KernelTimer t(K_LIN_FWD, s);
-  const bool big = wide<T>(a.m, a.n, a.k), al = aligned8(a.k, a.n);
+  // ragged rows take 64-wide tiles throughout: in 128-wide ones the repair and what the
+  // epilogue holds leave one workgroup on a CU (368,629 x 66 x 328: 286 against 220 us)
+  const bool al = aligned8(a.k, a.n), big = al && wide<T>(a.m, a.n, a.k);
   const dim3 grid((unsigned)tiles_of(a.m, a.n, big ? 128 : 64)), wg(256);
-  if (big && al) hipLaunchKernelGGL((lin_fwd_kernel<T, 128, true>), grid, wg, 0, s, a);
-  else if (big) hipLaunchKernelGGL((lin_fwd_kernel<T, 128, false>), grid, wg, 0, s, a);
+  if (big) hipLaunchKernelGGL((lin_fwd_kernel<T, 128, true>), grid, wg, 0, s, a);
   else if (al) hipLaunchKernelGGL((lin_fwd_kernel<T, 64, true>), grid, wg, 0, s, a);
   else hipLaunchKernelGGL((lin_fwd_kernel<T, 64, false>), grid, wg, 0, s, a);
   return hipGetLastError();
@@ -950,20 +990,23 @@ hipError_t reduce(const LinBwdArgs& a, hipStream_t s) {
 }
 
 bool narrow(int dtype, int k, int n) {
-  return dtype == TRIATTN_BF16 && aligned8(k, n) && k <= 128 && n <= 128;
+  return dtype == TRIATTN_BF16 && k <= 128 && n <= 128;
 }
-int narrow_parts(int64_t m, int act) {
-  const int rows = narrow_rows(act > TRIATTN_ACT_RELU ? DZ_ACT : DZ_X);
+int narrow_parts(int64_t m, int k, int n, int act) {
+  const int dz = act == TRIATTN_ACT_NONE ? DZ_X : act == TRIATTN_ACT_RELU ? DZ_RELU : DZ_ACT;
+  const int rows = narrow_rows(dz, aligned8(k, n));
   const int64_t blocks = (m + rows - 1) / rows;
   return (int)(blocks < 256 ? blocks : 256);  // one workgroup a CU
 }
 hipError_t bwd_narrow(const LinBwdArgs& a, hipStream_t s) {
   {
     KernelTimer t(K_LIN_NARROW, s);
-    const dim3 grid(narrow_parts(a.m, a.act)), wg(NARROW_WG);
-    if (a.act == TRIATTN_ACT_NONE) hipLaunchKernelGGL(lin_narrow_kernel<DZ_X>, grid, wg, 0, s, a);
-    else if (a.act == TRIATTN_ACT_RELU) hipLaunchKernelGGL(lin_narrow_kernel<DZ_RELU>, grid, wg, 0, s, a);
-    else hipLaunchKernelGGL(lin_narrow_kernel<DZ_ACT>, grid, wg, 0, s, a);
+    const dim3 grid(narrow_parts(a.m, a.k, a.n, a.act)), wg(NARROW_WG);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, wg, 0, s, a); };
+    const bool al = aligned8(a.k, a.n);
+    if (a.act == TRIATTN_ACT_NONE) go(al ? lin_narrow_kernel<DZ_X, true> : lin_narrow_kernel<DZ_X, false>);
+    else if (a.act == TRIATTN_ACT_RELU) go(al ? lin_narrow_kernel<DZ_RELU, true> : lin_narrow_kernel<DZ_RELU, false>);
+    else go(al ? lin_narrow_kernel<DZ_ACT, true> : lin_narrow_kernel<DZ_ACT, false>);
   }
   return (a.dw || a.dbias) && a.splits > 1 ? reduce(a, s) : hipGetLastError();
 }
@@ -996,7 +1039,7 @@ int dw_splits(int64_t m, int k, int n) {
 
 LinBwdPlan lin_bwd_plan(int dtype, int64_t m, int k, int n, int act) {
   LinBwdPlan p{};
-  p.splits = narrow(dtype, k, n) ? narrow_parts(m, act) : dw_splits(m, k, n);
+  p.splits = narrow(dtype, k, n) ? narrow_parts(m, k, n, act) : dw_splits(m, k, n);
   if (p.splits > 1) p.part = (size_t)p.splits * (size_t)slab_floats(k, n) * sizeof(float);
   if (make_dz(act, k) && !narrow(dtype, k, n)) p.dz = (size_t)m * n * sizeof(float);
   return p;

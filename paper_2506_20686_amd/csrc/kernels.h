@@ -249,8 +249,9 @@ hipError_t launch_lin_bwd(int dtype, const LinBwdArgs& a, hipStream_t s);
 constexpr int REL_MAX_EDGES = 255;
 constexpr int REL_MAX_H = 256;
 
-// Differences the edges may span to be looked up by difference, in bytes of the arguments.
-constexpr int REL_LUT = 2048;
+// Differences the edges may span to be looked up by difference (a byte of LDS each).
+constexpr int REL_SPAN = 8192;
+constexpr int REL_LUT = 2048;  // those whose table the arguments hold
 
 struct RelArgs {
   int64_t batch;
@@ -263,7 +264,7 @@ struct RelArgs {
   float* dtable;              // backward: [rows][h]
   float* part;                // backward, workspace: slabs of [rows][h] partial sums
   uint32_t inv_h;             // 2^32 / h rounded up (0 for h = 1)
-  int32_t low, span;          // lut: differences low .. low + span
+  int32_t low, span;          // looked up: differences low .. low + span
   union {
     int32_t edges[REL_MAX_EDGES + 1];
     uint8_t lut[REL_LUT];     // bucket of difference low + i

@@ -1,10 +1,12 @@
 // Learned relative position bias by buckets, and the gradient of its table.
 //
 // A pair's bucket is the number of edges at or below the difference of its positions.
-// Where the edges span fewer than REL_LUT differences (a clipped difference and buckets
-// that widen up to a thousand tokens do), the host turns them into a table of buckets by
-// difference, one LDS read a pair; edges further apart are searched, eight dependent LDS
-// reads a pair.  Both forms travel in the kernel's arguments.
+// Where the edges span fewer than REL_SPAN differences (a clipped difference and buckets
+// that widen up to four thousand tokens do), the bucket is one read of a table by difference
+// in LDS; edges further apart are searched, eight dependent LDS reads a pair (940 tokens x 16
+// heads with 209 edges, forward and backward: 328 us by search, 87 by table).  The host makes
+// tables of up to REL_LUT bytes, which travel in the kernel's arguments in the place of the
+// edges; longer ones every workgroup makes of the edges.
 #include <limits.h>
 
 #include "dma.h"
@@ -16,18 +18,48 @@
 namespace triattn {
 namespace {
 
+constexpr int REL_LDS_BUCKETS = REL_SPAN + REL_MAX_EDGES * 4 + 4;
+
 struct Buckets {
   const uint8_t* lut;    // LDS: bucket of difference low + i
   const int32_t* edges;  // LDS
 };
 
-// Copies the arguments' buckets to LDS (2 KB).
+__device__ inline int search(const int32_t* edges, int ne, int64_t d) {
+  int lo = 0, hi = ne;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (edges[mid] <= d) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Brings the table or the edges from the arguments to LDS (REL_LDS_BUCKETS bytes).  A table
+// too long for the arguments is made here: a thread searches its first difference and walks
+// on from there.  The caller's barrier follows.
 template <bool LUT>
-__device__ inline Buckets load_buckets(const RelArgs& a, uint32_t* lds) {
-  const uint32_t* src = (const uint32_t*)(LUT ? (const void*)a.lut : (const void*)a.edges);
-  const int words = LUT ? a.span / 4 + 1 : a.ne;
-  for (int i = threadIdx.x; i < words; i += blockDim.x) lds[i] = src[i];
-  return Buckets{(const uint8_t*)lds, (const int32_t*)lds};
+__device__ inline Buckets load_buckets(const RelArgs& a, char* lds) {
+  int32_t* edges = (int32_t*)(lds + REL_SPAN);
+  uint8_t* lut = (uint8_t*)lds;
+  if (LUT && a.span < REL_LUT) {
+    for (int i = threadIdx.x; i <= a.span / 4; i += blockDim.x)
+      ((uint32_t*)lds)[i] = ((const uint32_t*)a.lut)[i];
+    return Buckets{lut, edges};
+  }
+  for (int i = threadIdx.x; i < a.ne; i += blockDim.x) edges[i] = a.edges[i];
+  if constexpr (LUT) {
+    __syncthreads();
+    const int per = (a.span / (int)blockDim.x + 4) / 4 * 4, i0 = threadIdx.x * per;
+    if (i0 <= a.span) {
+      int r = search(edges, a.ne, (int64_t)a.low + i0);
+      for (int i = i0; i < i0 + per && i <= a.span; ++i) {
+        while (r < a.ne && edges[r] <= a.low + i) ++r;
+        lut[i] = (uint8_t)r;
+      }
+    }
+  }
+  return Buckets{lut, edges};
 }
 
 // Bucket of position pq less pk.  The difference may need 33 bits: LUT saturates it,
@@ -42,14 +74,7 @@ __device__ inline int bucket_of(const RelArgs& a, const Buckets& b, int32_t pq, 
     asm("v_med3_i32 %0, %1, 0, %2" : "=v"(i) : "v"(d), "s"(a.span));
     return b.lut[i];
   } else {
-    const int64_t d = (int64_t)pq - (int64_t)pk;
-    int lo = 0, hi = a.ne;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (b.edges[mid] <= d) lo = mid + 1;
-      else hi = mid;
-    }
-    return lo;
+    return search(b.edges, a.ne, (int64_t)pq - (int64_t)pk);
   }
 }
 
@@ -73,9 +98,9 @@ __global__ __launch_bounds__(256) void rel_fwd_kernel(RelArgs a) {
   struct Elems {
     T x[N];
   };
-  __shared__ uint32_t words[REL_LUT / 4];
+  __shared__ __attribute__((aligned(16))) char bucket_lds[REL_LDS_BUCKETS];
   extern __shared__ __attribute__((aligned(16))) char table_lds[];
-  const Buckets buckets = load_buckets<LUT>(a, words);
+  const Buckets buckets = load_buckets<LUT>(a, bucket_lds);
   const T* table = (const T*)a.table;
   if (LDS_TABLE) {
     T* t = (T*)table_lds;
@@ -164,16 +189,19 @@ __host__ __device__ inline RelPlan rel_plan(int64_t batch, int n, int h, int row
   p.waves = rows <= 64 + 8 ? 4 : rows <= 128 + 8 ? 2 : 1;
   const int keys = p.pl * REL_K * p.waves;
   p.kblocks = (n + keys - 1) / keys;
-  // about two workgroups a CU, and at least 4 rows to each; one alone, which needs no
-  // further sum, for up to 32 rows
-  int64_t want = 512 / (p.groups * p.kblocks);
+  // about as many workgroups as the CUs' LDS holds at once, each of at least 4 rows; one
+  // alone, which needs no further sum, for up to 32 rows
+  const int lds = p.waves * rows * 256 + REL_LDS_BUCKETS, fit = 160 * 1024 / lds;
+  int64_t want = 256 * fit / (p.groups * p.kblocks);
   if (want < 1 || (p.groups * p.kblocks == 1 && batch * n <= 32)) want = 1;
-  int64_t per = (batch * n + want - 1) / want;
-  if (per < REL_Q) per = REL_Q;
-  p.qlen = (int)(per < n ? per : n);
+  // a workgroup has one chunk of a sample's rows, or, where there are more samples than
+  // that, whole samples in turn
+  int64_t units = want / batch, most = (n + REL_Q - 1) / REL_Q;
+  if (units > most) units = most;
+  if (units < 1) units = 1;
+  p.qlen = (int)((n + units - 1) / units);
   p.units = (n + p.qlen - 1) / p.qlen;
-  const int64_t all = batch * p.units;
-  p.w = (int)(all < want ? all : want);
+  p.w = (int)(batch * p.units < want ? batch * p.units : want);
   return p;
 }
 
@@ -185,11 +213,25 @@ __device__ inline float load_one(rsrc_t r, uint32_t off, float) {
   return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (int)off, 0, 0));
 }
 
-template <typename T, bool LUT, bool CHAIN>
+// Value V of a group of SPREAD lanes, in all of them.
+template <int SPREAD, int V>
+__device__ inline int spread(int x) {
+  if constexpr (SPREAD == 4)
+    return __builtin_amdgcn_update_dpp(0, x, 0x55 * V, 0xf, 0xf, true);  // quad_perm V V V V
+  else
+    return __builtin_amdgcn_update_dpp(0, x, 0x150 + V, 0xf, 0xf, true);  // row_newbcast V
+}
+
+// SPREAD: the lanes of a pair (h = 4, 16, or 64 and up) look up one row of their key each,
+// SPREAD rows at a time, and hand the buckets round; 0: every lane looks up every row of
+// its key itself.
+template <typename T, bool LUT, int SPREAD>
 __global__ __launch_bounds__(256) void rel_bwd_kernel(RelArgs a, RelPlan p) {
-  __shared__ uint32_t words[REL_LUT / 4];
+  constexpr int BLOCK = SPREAD ? SPREAD : 64;  // rows whose positions (or buckets) lanes hold
+  const bool chains = a.chain != nullptr;
+  __shared__ __attribute__((aligned(16))) char bucket_lds[REL_LDS_BUCKETS];
   extern __shared__ __attribute__((aligned(16))) float sums[];  // [waves][rows][64]
-  const Buckets buckets = load_buckets<LUT>(a, words);
+  const Buckets buckets = load_buckets<LUT>(a, bucket_lds);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float* mine = sums + wave * a.rows * 64;
   for (int i = 4 * lane; i < a.rows * 64; i += 256) *(f32x4*)(mine + i) = f32x4{};
@@ -206,7 +248,7 @@ __global__ __launch_bounds__(256) void rel_bwd_kernel(RelArgs a, RelPlan p) {
   for (int u = 0; u < REL_K; ++u) {
     const int k = k0 + u * p.pl;
     const bool in = off < p.pl && c < a.h && k < a.n;
-    key[u] = in ? k : 0;
+    key[u] = k < a.n ? k : 0;  // the same for all lanes of a pair, with or without a channel
     at[u] = in ? (uint32_t)(k * a.h + c) * sizeof(T) : 0x80000000u;
   }
   float* column = mine + lane;
@@ -217,7 +259,7 @@ __global__ __launch_bounds__(256) void rel_bwd_kernel(RelArgs a, RelPlan p) {
 #pragma unroll
     for (int u = 0; u < REL_K; ++u) {
       pk[u] = a.pos[b0 + key[u]];
-      ck[u] = CHAIN ? a.chain[b0 + key[u]] : 0;
+      ck[u] = chains ? a.chain[b0 + key[u]] : 0;
     }
     float x[REL_Q][REL_K];
     auto load = [&](int q) {  // rows past the chunk give zeros
@@ -230,31 +272,63 @@ __global__ __launch_bounds__(256) void rel_bwd_kernel(RelArgs a, RelPlan p) {
       }
     };
     load(q0);
-    int32_t prow = 0, crow = 0;  // lane i: position and chain of row i of the current 64
+    // position and chain of one row of the current block and of the next one
+    const int mine_of = lane % BLOCK;
+    auto row_of = [&](int q) { return b0 + min(q + mine_of, q1 - 1); };
+    int32_t next_pos = a.pos[row_of(q0)], next_chain = chains ? a.chain[row_of(q0)] : 0;
+    int32_t prow = 0, crow = 0;
+    int bucket[REL_K];  // SPREAD: of this lane's row and key u
     for (int q = q0; q < q1; q += REL_Q) {
-      if ((q - q0) % 64 == 0) {
-        const int64_t row = b0 + min(q + lane, q1 - 1);
-        prow = a.pos[row];
-        crow = CHAIN ? a.chain[row] : 0;
-      }
+      const int at_row = (q - q0) % BLOCK;
       float f[REL_Q][REL_K];
 #pragma unroll
       for (int v = 0; v < REL_Q; ++v)
 #pragma unroll
         for (int u = 0; u < REL_K; ++u) f[v][u] = x[v][u];
+      if (at_row == 0) {
+        prow = next_pos;
+        crow = next_chain;
+        next_pos = a.pos[row_of(q + BLOCK)];
+        if (chains) next_chain = a.chain[row_of(q + BLOCK)];
+        if constexpr (SPREAD != 0) {
+#pragma unroll
+          for (int u = 0; u < REL_K; ++u) {
+            bucket[u] = bucket_of<LUT>(a, buckets, prow, pk[u]);
+            if (chains && ck[u] != crow) bucket[u] = a.ne + 1;
+          }
+        }
+      }
       // the next rows' loads leave now, not where the scheduler finds registers for them
       __builtin_amdgcn_sched_barrier(0);
       load(q + REL_Q);
       __builtin_amdgcn_sched_barrier(0);
       int r[REL_Q][REL_K];
+      if constexpr (SPREAD == 0) {
 #pragma unroll
-      for (int v = 0; v < REL_Q; ++v) {
-        const int32_t pq = __builtin_amdgcn_readlane(prow, (q - q0) % 64 + v);
-        const int32_t cq = CHAIN ? __builtin_amdgcn_readlane(crow, (q - q0) % 64 + v) : 0;
+        for (int v = 0; v < REL_Q; ++v) {
+          const int32_t pq = __builtin_amdgcn_readlane(prow, at_row + v);
+          const int32_t cq = __builtin_amdgcn_readlane(crow, at_row + v);
+#pragma unroll
+          for (int u = 0; u < REL_K; ++u) {
+            r[v][u] = bucket_of<LUT>(a, buckets, pq, pk[u]);
+            if (chains && ck[u] != cq) r[v][u] = a.ne + 1;
+          }
+        }
+      } else if constexpr (SPREAD == 64) {
+#pragma unroll
+        for (int v = 0; v < REL_Q; ++v)
+#pragma unroll
+          for (int u = 0; u < REL_K; ++u) r[v][u] = __builtin_amdgcn_readlane(bucket[u], at_row + v);
+      } else {
+        static_assert(REL_Q == 4, "spread's constants");
 #pragma unroll
         for (int u = 0; u < REL_K; ++u) {
-          r[v][u] = bucket_of<LUT>(a, buckets, pq, pk[u]);
-          if (CHAIN && ck[u] != cq) r[v][u] = a.ne + 1;
+          r[0][u] = spread<SPREAD, 0>(bucket[u]);
+          r[1][u] = spread<SPREAD, 1>(bucket[u]);
+          r[2][u] = spread<SPREAD, 2>(bucket[u]);
+          r[3][u] = spread<SPREAD, 3>(bucket[u]);
+          // the next four rows' buckets to the front (row_ror 12)
+          if (SPREAD == 16) bucket[u] = __builtin_amdgcn_update_dpp(0, bucket[u], 0x12c, 0xf, 0xf, true);
         }
       }
       // two at a time, which halves the chain of dependent LDS accesses: if both fall into
@@ -263,10 +337,10 @@ __global__ __launch_bounds__(256) void rel_bwd_kernel(RelArgs a, RelPlan p) {
       for (int v = 0; v < REL_Q; ++v)
 #pragma unroll
         for (int u = 0; u < REL_K; u += 2) {
-          float *s0 = column + r[v][u] * 64, *s1 = column + r[v][u + 1] * 64;
-          const float x0 = *s0, x1 = *s1, y0 = x0 + f[v][u];
-          *s0 = y0;
-          *s1 = (s1 == s0 ? y0 : x1) + f[v][u + 1];
+          const int r0 = r[v][u], r1 = r[v][u + 1];
+          const float x0 = column[r0 * 64], x1 = column[r1 * 64], y0 = x0 + f[v][u];
+          column[r0 * 64] = y0;
+          column[r1 * 64] = (r1 == r0 ? y0 : x1) + f[v][u + 1];
         }
     }
   }
@@ -303,18 +377,20 @@ __global__ __launch_bounds__(SLAB_WG) void rel_reduce_kernel(const float* part, 
   if (threadIdx.x < SLAB_COLS && i < total) dtable[i] = s;
 }
 
-// Fills in how buckets are found.  False: by search.
+// Fills in the table's range.  False: the edges are searched.
 bool use_lut(RelArgs& a) {
-  int32_t edges[REL_MAX_EDGES];
   const int64_t span = (int64_t)a.edges[a.ne - 1] - a.edges[0] + 1;
-  if (a.edges[0] == INT_MIN || span >= REL_LUT) return false;
-  for (int i = 0; i < a.ne; ++i) edges[i] = a.edges[i];
-  a.low = edges[0] - 1;
+  if (a.edges[0] == INT_MIN || span >= REL_SPAN) return false;
+  a.low = a.edges[0] - 1;
   a.span = (int32_t)span;  // difference low + span is the last edge
-  a.lut[0] = 0;
-  for (int i = 0; i < a.ne; ++i) {
-    const int from = edges[i] - a.low, to = i + 1 < a.ne ? edges[i + 1] - a.low : a.span + 1;
-    for (int d = from; d < to; ++d) a.lut[d] = (uint8_t)(i + 1);
+  if (span < REL_LUT) {
+    int32_t edges[REL_MAX_EDGES];
+    for (int i = 0; i < a.ne; ++i) edges[i] = a.edges[i];  // the table takes their place
+    a.lut[0] = 0;
+    for (int i = 0; i < a.ne; ++i) {
+      const int from = edges[i] - a.low, to = i + 1 < a.ne ? edges[i + 1] - a.low : a.span + 1;
+      for (int d = from; d < to; ++d) a.lut[d] = (uint8_t)(i + 1);
+    }
   }
   return true;
 }
@@ -358,10 +434,11 @@ hipError_t bwd(RelArgs a, hipStream_t s) {
     KernelTimer t(K_REL_BWD, s);
     const dim3 grid((unsigned)p.slabs(), (unsigned)p.groups), wg(64 * p.waves);
     const size_t lds = (size_t)p.waves * a.rows * 64 * sizeof(float);
-    if (lut && a.chain) hipLaunchKernelGGL((rel_bwd_kernel<T, true, true>), grid, wg, lds, s, a, p);
-    else if (lut) hipLaunchKernelGGL((rel_bwd_kernel<T, true, false>), grid, wg, lds, s, a, p);
-    else if (a.chain) hipLaunchKernelGGL((rel_bwd_kernel<T, false, true>), grid, wg, lds, s, a, p);
-    else hipLaunchKernelGGL((rel_bwd_kernel<T, false, false>), grid, wg, lds, s, a, p);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, wg, lds, s, a, p); };
+    if (p.hc == 64) go(lut ? rel_bwd_kernel<T, true, 64> : rel_bwd_kernel<T, false, 64>);
+    else if (p.hc == 16) go(lut ? rel_bwd_kernel<T, true, 16> : rel_bwd_kernel<T, false, 16>);
+    else if (p.hc == 4) go(lut ? rel_bwd_kernel<T, true, 4> : rel_bwd_kernel<T, false, 4>);
+    else go(lut ? rel_bwd_kernel<T, true, 0> : rel_bwd_kernel<T, false, 0>);
   }
   if (p.slabs() == 1) return hipGetLastError();
   KernelTimer t(K_REL_REDUCE, s);

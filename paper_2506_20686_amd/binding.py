@@ -783,11 +783,15 @@ def transition_bwd(x, gamma, beta, w1, w2, mean, rstd, dout,
 
 
 # ---- layer norm, linear projection with epilogue, relative position bias -------------------
+#
+# Their smallest calls take the GPU less time than Python needs to make them, so the
+# wrappers call the library's functions directly.
 
 def _on(dev, fn, *args):
     """fn(*args, stream) on torch's current stream of `dev`, with `dev` current."""
-    if dev.index is None or torch._C._cuda_getDevice() == dev.index:
-        return fn(*args, _stream(dev))
+    index = dev.index
+    if index is not None and torch._C._cuda_getDevice() == index:
+        return fn(*args, torch._C._cuda_getCurrentRawStream(index))
     with torch.cuda.device(dev):
         return fn(*args, _stream(dev))
 
@@ -800,36 +804,38 @@ def _workspace(workspace, need, dev):
             raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
         if workspace.numel() >= need:
             return workspace
-    return torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    return torch.empty(need, dtype=torch.uint8, device=dev)
 
 
 def _check_2d(name, t):
+    """t's dtype code, device and shape."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dim() != 2:
         raise ValueError(f"{name} must have two axes (got shape {tuple(t.shape)})")
-    if t.dtype not in _DTYPES:
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
         raise ValueError(f"unsupported dtype {t.dtype}")
-    _check(name, t, t.shape, t.dtype, t.device)
-    return _DTYPES[t.dtype]
+    dev = t.device
+    if dev.type != "cuda" or not t.is_contiguous():
+        _check(name, t, t.shape, t.dtype, dev)
+    m, n = t.shape
+    return dt, dev, m, n
 
 
 def layer_norm_fwd(x, gamma=None, beta=None, eps: float = 1e-5):
     """out = (x - mean) * rstd * gamma + beta over the rows of x [m, c] (fp32 or
     bf16; any c up to 8192); gamma and beta [c] may be None (ones, zeros).
     Returns (out, mean, rstd), the statistics [m] in fp32."""
-    dt = _check_2d("x", x)
-    m, c = x.shape
-    dev = x.device
-    if gamma is not None:
-        _check("gamma", gamma, (c,), x.dtype, dev)
-    if beta is not None:
-        _check("beta", beta, (c,), x.dtype, dev)
+    dt, dev, m, c = _check_2d("x", x)
+    for name, t in (("gamma", gamma), ("beta", beta)):
+        if t is not None:
+            _check(name, t, (c,), x.dtype, dev)
     out = torch.empty_like(x)
     mean = torch.empty(m, dtype=torch.float32, device=dev)
     rstd = torch.empty(m, dtype=torch.float32, device=dev)
-    st = _on(dev, tri_layer_norm_fwd, dt, m, c, float(eps), _ptr(x), _ptr(gamma), _ptr(beta),
-             _ptr(out), _ptr(mean), _ptr(rstd))
+    st = _on(dev, lib().tri_layer_norm_fwd, dt, m, c, eps, x.data_ptr(), _ptr(gamma),
+             _ptr(beta), out.data_ptr(), mean.data_ptr(), rstd.data_ptr())
     if st != OK:
         raise TriAttnError(st, "tri_layer_norm_fwd")
     return out, mean, rstd
@@ -838,9 +844,7 @@ def layer_norm_fwd(x, gamma=None, beta=None, eps: float = 1e-5):
 def layer_norm_bwd(x, gamma, mean, rstd, dout, workspace: Optional[torch.Tensor] = None):
     """Gradients of sum(dout * out) for layer_norm_fwd.  Returns (dx [m, c],
     dgamma [c] fp32, dbeta [c] fp32)."""
-    dt = _check_2d("x", x)
-    m, c = x.shape
-    dev = x.device
+    dt, dev, m, c = _check_2d("x", x)
     if gamma is not None:
         _check("gamma", gamma, (c,), x.dtype, dev)
     _check("mean", mean, (m,), torch.float32, dev)
@@ -850,9 +854,9 @@ def layer_norm_bwd(x, gamma, mean, rstd, dout, workspace: Optional[torch.Tensor]
     dgamma = torch.empty(c, dtype=torch.float32, device=dev)
     dbeta = torch.empty(c, dtype=torch.float32, device=dev)
     workspace = _workspace(workspace, tri_layer_norm_bwd_workspace_bytes(dt, m, c), dev)
-    st = _on(dev, tri_layer_norm_bwd, dt, m, c, _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd),
-             _ptr(dout), _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(workspace),
-             workspace.numel())
+    st = _on(dev, lib().tri_layer_norm_bwd, dt, m, c, x.data_ptr(), _ptr(gamma),
+             mean.data_ptr(), rstd.data_ptr(), dout.data_ptr(), dx.data_ptr(), dgamma.data_ptr(),
+             dbeta.data_ptr(), workspace.data_ptr(), workspace.numel())
     if st != OK:
         raise TriAttnError(st, "tri_layer_norm_bwd")
     return dx, dgamma, dbeta
@@ -864,11 +868,9 @@ def linear_fwd(x, w, bias=None, residual=None, act: int = ACT_NONE, save_z: bool
     ACT_RELU, ACT_GELU (error function), ACT_SILU.  Returns (out, z): z is the
     value before the activation, in x's dtype, if save_z (linear_bwd takes it
     when there is an activation), else None."""
-    dt = _check_2d("x", x)
-    m, k = x.shape
-    dev, dtype = x.device, x.dtype
-    _check_2d("w", w)
-    n = w.shape[1]
+    dt, dev, m, k = _check_2d("x", x)
+    n = _check_2d("w", w)[3]
+    dtype = x.dtype
     _check("w", w, (k, n), dtype, dev)
     if bias is not None:
         _check("bias", bias, (n,), dtype, dev)
@@ -876,8 +878,8 @@ def linear_fwd(x, w, bias=None, residual=None, act: int = ACT_NONE, save_z: bool
         _check("residual", residual, (m, n), dtype, dev)
     out = torch.empty((m, n), dtype=dtype, device=dev)
     z = torch.empty((m, n), dtype=dtype, device=dev) if save_z else None
-    st = _on(dev, tri_linear_fwd, dt, m, k, n, act, _ptr(x), _ptr(w), _ptr(bias),
-             _ptr(residual), _ptr(out), _ptr(z))
+    st = _on(dev, lib().tri_linear_fwd, dt, m, k, n, act, x.data_ptr(), w.data_ptr(),
+             _ptr(bias), _ptr(residual), out.data_ptr(), _ptr(z))
     if st != OK:
         raise TriAttnError(st, "tri_linear_fwd")
     return out, z
@@ -888,11 +890,9 @@ def linear_bwd(x, w, dout, z=None, act: int = ACT_NONE,
     """Gradients of sum(dout * out) for linear_fwd: z as it returned it (None
     without an activation).  Returns (dx [m, k] in x's dtype, dw [k, n] fp32,
     dbias [n] fp32); the residual's gradient is dout."""
-    dt = _check_2d("x", x)
-    m, k = x.shape
-    dev, dtype = x.device, x.dtype
-    _check_2d("w", w)
-    n = w.shape[1]
+    dt, dev, m, k = _check_2d("x", x)
+    n = _check_2d("w", w)[3]
+    dtype = x.dtype
     _check("w", w, (k, n), dtype, dev)
     _check("dout", dout, (m, n), dtype, dev)
     if z is not None:
@@ -901,8 +901,9 @@ def linear_bwd(x, w, dout, z=None, act: int = ACT_NONE,
     dw = torch.empty((k, n), dtype=torch.float32, device=dev)
     dbias = torch.empty(n, dtype=torch.float32, device=dev)
     workspace = _workspace(workspace, tri_linear_bwd_workspace_bytes(dt, m, k, n, act), dev)
-    st = _on(dev, tri_linear_bwd, dt, m, k, n, act, _ptr(x), _ptr(w), _ptr(z), _ptr(dout),
-             _ptr(dx), _ptr(dw), _ptr(dbias), _ptr(workspace), workspace.numel())
+    st = _on(dev, lib().tri_linear_bwd, dt, m, k, n, act, x.data_ptr(), w.data_ptr(), _ptr(z),
+             dout.data_ptr(), dx.data_ptr(), dw.data_ptr(), dbias.data_ptr(),
+             workspace.data_ptr(), workspace.numel())
     if st != OK:
         raise TriAttnError(st, "tri_linear_bwd")
     return dx, dw, dbias
@@ -956,8 +957,8 @@ def rel_bias_fwd(pos, edges, table, chain=None, base=None):
     if base is not None:
         _check("base", base, shape, table.dtype, dev)
     out = torch.empty(shape, dtype=table.dtype, device=dev)
-    st = _on(dev, tri_rel_bias_fwd, dt, batch, n, h, edges, _ptr(pos), _ptr(chain), _ptr(table),
-             _ptr(base), _ptr(out))
+    st = _on(dev, lib().tri_rel_bias_fwd, dt, batch, n, h, len(edges), _edges_arr(edges),
+             pos.data_ptr(), _ptr(chain), table.data_ptr(), _ptr(base), out.data_ptr())
     if st != OK:
         raise TriAttnError(st, "tri_rel_bias_fwd")
     return out
@@ -976,8 +977,9 @@ def rel_bias_bwd(pos, edges, dout, chain=None, workspace: Optional[torch.Tensor]
                          device=dev)
     need = tri_rel_bias_bwd_workspace_bytes(dt, batch, n, h, len(edges))
     workspace = _workspace(workspace, need, dev)
-    st = _on(dev, tri_rel_bias_bwd, dt, batch, n, h, edges, _ptr(pos), _ptr(chain), _ptr(dout),
-             _ptr(dtable), _ptr(workspace), workspace.numel())
+    st = _on(dev, lib().tri_rel_bias_bwd, dt, batch, n, h, len(edges), _edges_arr(edges),
+             pos.data_ptr(), _ptr(chain), dout.data_ptr(), dtable.data_ptr(),
+             workspace.data_ptr(), workspace.numel())
     if st != OK:
         raise TriAttnError(st, "tri_rel_bias_bwd")
     return dtable

@@ -79,6 +79,8 @@ struct Raw8 {
   u32x4 v[N];
 };
 template <typename T>
+constexpr int WORD = 16 / (int)sizeof(T);  // elements of a 16-byte word
+template <typename T>
 __device__ inline void unpack(const Raw8<T>& r, float (&f)[8]) {
   struct E {
     T x[8];
@@ -92,14 +94,15 @@ struct __attribute__((packed)) Any16 {
   u32x4 v;
 };
 
-// The first `have` of 8 values (zeros after them); ALIGNED: all of them, at 16 bytes.  A
+// The first `have` of 8 values (zeros after them); ALIGNED: whole words of them.  A
 // partial chunk is 8 loads at once, those past its end of its last element.
 template <typename T, bool ALIGNED>
 __device__ inline Raw8<T> get8(const T* p, int have) {
   Raw8<T> r{};
   if (ALIGNED) {
 #pragma unroll
-    for (int i = 0; i < Raw8<T>::N; ++i) r.v[i] = ((const u32x4*)p)[i];
+    for (int i = 0; i < Raw8<T>::N; ++i)
+      if (i * WORD<T> < have) r.v[i] = ((const u32x4*)p)[i];
   } else if (have >= 8) {
 #pragma unroll
     for (int i = 0; i < Raw8<T>::N; ++i) r.v[i] = ((const Any16*)p)[i].v;
@@ -125,9 +128,9 @@ struct Mat {
   int cols;
 };
 
-// Chunk (r, c .. c + 7) of the window at (r0, c0) of a matrix whose width is a multiple of
-// 8 elements, `lim` rows high: zeros outside.  A chunk is all in or all out, and the
-// buffer resource's range check gives the zeros.
+// Chunk (r, c .. c + 7) of the window at (r0, c0) of a matrix whose rows are whole 16-byte
+// words, `lim` rows high: zeros outside.  A word is all in or all out, and the buffer
+// resource's range check gives the zeros.
 template <typename T>
 __device__ inline Raw8<T> fetch(const Mat<T>& m, int64_t r0, int c0, int lim, int r, int c) {
   Raw8<T> x;
@@ -138,11 +141,13 @@ __device__ inline Raw8<T> fetch(const Mat<T>& m, int64_t r0, int c0, int lim, in
   const T* base = m.p + r0 * m.cols + c0;
   // the last row's end past the corner; a row is at most 32 KB, a window 4 MB
   const rsrc_t rs = buf_rsrc_n(base, rows ? (uint32_t)(rows * m.cols - c0) * sizeof(T) : 0u);
-  const uint32_t off = c0 + c < m.cols ? (uint32_t)(r * m.cols + c) * sizeof(T) : 0x80000000u;
 #pragma unroll
-  for (int i = 0; i < Raw8<T>::N; ++i)
-    x.v[i] = __builtin_bit_cast(
-        u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(off + 16 * i), 0, 0));
+  for (int i = 0; i < Raw8<T>::N; ++i) {
+    const int ci = c + i * WORD<T>;
+    const uint32_t off = c0 + ci < m.cols ? (uint32_t)(r * m.cols + ci) * sizeof(T) : 0x80000000u;
+    x.v[i] = __builtin_bit_cast(u32x4,
+                                __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, 0, 0));
+  }
   return x;
 }
 
@@ -155,7 +160,7 @@ __device__ inline Raw8<T> fetch(const Mat<T>& m, int64_t r0, int c0, int lim, in
 template <typename T>
 __device__ inline Raw8<T> fetch_any(const Mat<T>& m, int64_t r0, int c0, int lim, int r, int c,
                                     int& info) {
-  if (m.cols % 8 == 0) {  // this matrix's rows are whole chunks after all
+  if (m.cols % WORD<T> == 0) {  // this matrix's rows are whole words after all
     info = 8;
     return fetch<T>(m, r0, c0, lim, r, c);
   }
@@ -330,7 +335,7 @@ struct Product {
   using LB = typename SB::L;
   static constexpr int BUF = LA::BYTES + LB::BYTES;
   // steps whose loads are in flight: two where the registers allow three workgroups on a CU
-  static constexpr int D = R == 64 && ALIGNED ? 2 : 1;
+  static constexpr int D = R == 64 && (ALIGNED || sizeof(TA) == 4) ? 2 : 1;
   static constexpr int EPI = 4 * 32 * (R / 2 + 4) * 4;  // the result's staging
   static constexpr int LDS = 2 * BUF > EPI ? 2 * BUF : EPI;
 
@@ -452,12 +457,13 @@ struct Product {
   }
 };
 
-// Writes the first `have` of 8 values to p; ALIGNED: all of them, at 16 bytes.
+// Writes the first `have` of 8 values to p; ALIGNED: whole words of them.
 template <typename T, bool ALIGNED>
 __device__ inline void put_raw(T* p, int have, const Raw8<T>& r) {
   if (ALIGNED) {
 #pragma unroll
-    for (int i = 0; i < Raw8<T>::N; ++i) ((u32x4*)p)[i] = r.v[i];
+    for (int i = 0; i < Raw8<T>::N; ++i)
+      if (i * WORD<T> < have) ((u32x4*)p)[i] = r.v[i];
   } else if (have >= 8) {
 #pragma unroll
     for (int i = 0; i < Raw8<T>::N; ++i) ((Any16*)p)[i].v = r.v[i];
@@ -904,7 +910,11 @@ __global__ __launch_bounds__(256) void lin_reduce_kernel(LinBwdArgs a, int slice
   }
 }
 
-bool aligned8(int k, int n) { return k % 8 == 0 && n % 8 == 0; }
+// Rows of x, dx and of W, z, dout, out are whole 16-byte words.
+template <typename T>
+bool whole_words(int k, int n) {
+  return k % WORD<T> == 0 && n % WORD<T> == 0;
+}
 int64_t tiles_of(int64_t m, int64_t n, int r) { return (m + r - 1) / r * ((n + r - 1) / r); }
 
 // 128-wide tiles of an [m][width] result where there are enough of them for the 256 CUs and
@@ -922,7 +932,7 @@ hipError_t fwd(const LinArgs& a, hipStream_t s) {
   KernelTimer t(K_LIN_FWD, s);
   // ragged rows take 64-wide tiles throughout: in 128-wide ones the repair and what the
   // epilogue holds leave one workgroup on a CU (368,629 x 66 x 328: 286 against 220 us)
-  const bool al = aligned8(a.k, a.n), big = al && wide<T>(a.m, a.n, a.k);
+  const bool al = whole_words<T>(a.k, a.n), big = al && wide<T>(a.m, a.n, a.k);
   const dim3 grid((unsigned)tiles_of(a.m, a.n, big ? 128 : 64)), wg(256);
   if (big) hipLaunchKernelGGL((lin_fwd_kernel<T, 128, true>), grid, wg, 0, s, a);
   else if (al) hipLaunchKernelGGL((lin_fwd_kernel<T, 64, true>), grid, wg, 0, s, a);
@@ -963,7 +973,7 @@ void bwd_launch(const LinBwdArgs& a, hipStream_t s) {
 }
 template <typename T, int DZ>
 void bwd_align(const LinBwdArgs& a, hipStream_t s) {
-  if (aligned8(a.k, a.n)) bwd_launch<T, DZ, true>(a, s);
+  if (whole_words<T>(a.k, a.n)) bwd_launch<T, DZ, true>(a, s);
   else bwd_launch<T, DZ, false>(a, s);
 }
 template <typename T>
@@ -994,7 +1004,7 @@ bool narrow(int dtype, int k, int n) {
 }
 int narrow_parts(int64_t m, int k, int n, int act) {
   const int dz = act == TRIATTN_ACT_NONE ? DZ_X : act == TRIATTN_ACT_RELU ? DZ_RELU : DZ_ACT;
-  const int rows = narrow_rows(dz, aligned8(k, n));
+  const int rows = narrow_rows(dz, whole_words<bf16>(k, n));
   const int64_t blocks = (m + rows - 1) / rows;
   return (int)(blocks < 256 ? blocks : 256);  // one workgroup a CU
 }
@@ -1003,7 +1013,7 @@ hipError_t bwd_narrow(const LinBwdArgs& a, hipStream_t s) {
     KernelTimer t(K_LIN_NARROW, s);
     const dim3 grid(narrow_parts(a.m, a.k, a.n, a.act)), wg(NARROW_WG);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, wg, 0, s, a); };
-    const bool al = aligned8(a.k, a.n);
+    const bool al = whole_words<bf16>(a.k, a.n);
     if (a.act == TRIATTN_ACT_NONE) go(al ? lin_narrow_kernel<DZ_X, true> : lin_narrow_kernel<DZ_X, false>);
     else if (a.act == TRIATTN_ACT_RELU) go(al ? lin_narrow_kernel<DZ_RELU, true> : lin_narrow_kernel<DZ_RELU, false>);
     else go(al ? lin_narrow_kernel<DZ_ACT, true> : lin_narrow_kernel<DZ_ACT, false>);

@@ -50,7 +50,8 @@ def backward(t, act):
 SIZES = [(1, 1, 1), (1, 384, 1536), (2, 7, 3), (5, 128, 128), (16, 2048, 24), (17, 33, 65),
          (64, 64, 64), (100, 128, 128), (128, 256, 384), (129, 136, 72), (300, 449, 131),
          (257, 40, 200), (1000, 8, 8), (1500, 384, 520), (4001, 128, 128), (70, 1001, 16),
-         (33, 16, 1000), (513, 130, 257), (8, 8192, 32), (8, 24, 8192), (2500, 1, 5)]
+         (33, 16, 1000), (513, 130, 257), (8, 8192, 32), (8, 24, 8192), (2500, 1, 5),
+         (90, 132, 68), (70, 20, 12), (301, 129, 128), (140, 128, 129), (260, 4, 300)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F4])
@@ -111,7 +112,7 @@ def test_small_and_large_magnitudes_fp32():
 
 
 @pytest.mark.parametrize("dtype", [BF, F4])
-@pytest.mark.parametrize("m,k,n", [(130, 128, 136), (37, 45, 51)])
+@pytest.mark.parametrize("m,k,n", [(130, 128, 136), (37, 45, 51), (130, 128, 64), (77, 129, 140)])
 def test_nothing_outside_the_outputs_is_written(m, k, n, dtype):
     t = {a: dev(b) for a, b in inputs(m, k, n, dtype, 5).items()}
     ref = (*B.linear_fwd(t["x"], t["w"], t["bias"], t["residual"], B.ACT_GELU, True),
@@ -157,6 +158,27 @@ def test_bitwise_reproducible(dtype, act):
              *B.linear_bwd(t["x"], t["w"], t["dout"], z, act)) for _ in range(2))
     for s, r in zip(a, b):
         assert torch.equal(s, r)
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("m,k,n", [(40003, 128, 96), (33333, 77, 128), (70001, 5, 3),
+                                   (20000, 40, 200), (9000, 300, 33)])
+def test_many_rows(m, k, n, act):
+    # several rounds of every workgroup: sampled rows of the row-wise results, and the sums
+    # over rows by a dout that is zero elsewhere
+    t = inputs(m, k, n, BF, 3 * m + act)
+    rows = torch.unique(torch.cat([torch.arange(40), torch.arange(m - 40, m),
+                                   torch.linspace(40, m - 41, 300).long()]))
+    keep = torch.zeros(m, 1, dtype=BF)
+    keep[rows] = 1
+    t["dout"] = t["dout"] * keep
+    z = t["z"] if act else None
+    got = B.linear_bwd(dev(t["x"]), dev(t["w"]), dev(t["dout"]), dev(z), act)
+    ref, bound = R.lin_bwd(t["x"][rows], t["w"], t["dout"][rows], z[rows] if act else None, act)
+    R.check("dx", got[0][rows.to(DEV)], ref[0], bound[0])
+    R.check("dw", got[1], ref[1], bound[1])
+    R.check("dbias", got[2], ref[2], bound[2])
+    assert int(torch.count_nonzero(got[0])) == int(torch.count_nonzero(got[0][rows.to(DEV)]))
 
 
 def test_long_sum_over_rows():

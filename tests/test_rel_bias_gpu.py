@@ -43,6 +43,7 @@ def both(t, edges):
 
 CLIP = B.rel_bias_edges(32)
 FAR = B.rel_bias_edges(16, 512, 16)
+LONG = B.rel_bias_edges(80, 1760, 24)  # a table too long for the arguments
 WIDE = [-(1 << 31), -70000, -500, 0, 1, 3, 900, 12345, (1 << 31) - 1]
 
 
@@ -54,16 +55,18 @@ WIDE = [-(1 << 31), -70000, -500, 0, 1, 3, 900, 12345, (1 << 31) - 1]
     (1, 129, 4, CLIP, 3), (2, 33, 16, FAR, 2), (3, 17, 5, CLIP, 1), (1, 50, 128, CLIP, 2),
     (1, 31, 64, FAR, 1), (1, 12, 256, list(range(-127, 128)), 2), (2, 9, 255, WIDE, 1),
     (1, 200, 1, CLIP, 2), (1, 257, 2, FAR, 1), (1, 77, 24, list(range(-127, 128)), 2),
-    (1, 300, 8, CLIP, 1), (4, 64, 12, [-5, 9], 2)])
+    (1, 300, 8, CLIP, 1), (4, 64, 12, [-5, 9], 2), (1, 90, 16, LONG, 2), (1, 70, 4, LONG, 1),
+    (2, 40, 65, LONG, 1), (1, 37, 64, WIDE, 2), (1, 60, 16, WIDE, 1), (300, 5, 4, CLIP, 2),
+    (1, 130, 32, CLIP, 1), (1, 66, 200, FAR, 1)])
 def test_forward_and_backward(batch, n, h, edges, chains, dtype):
     both(inputs(batch, n, h, edges, chains, dtype, n + h), edges)
 
 
 @pytest.mark.parametrize("dtype", [BF, F4])
-@pytest.mark.parametrize("spread", [3, 100, 100000, (1 << 31) - 1])
+@pytest.mark.parametrize("spread", [3, 100, 2000, 100000, (1 << 31) - 1])
 def test_positions_in_any_order(spread, dtype):
     # the difference of two int32 does not fit one
-    edges = WIDE if spread > 1000 else CLIP
+    edges = WIDE if spread > 9000 else LONG if spread > 1000 else CLIP
     t = inputs(2, 70, 4, edges, 3, dtype, spread % 97, spread)
     t["pos"][0, 0], t["pos"][0, 1] = -(1 << 31), (1 << 31) - 1
     both(t, edges)

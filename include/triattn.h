@@ -327,7 +327,8 @@ int tri_layer_norm_bwd(int dtype, int64_t m, int64_t c, const void* x, const voi
  *   act: a triattn_act; gelu is z Phi(z) with the error function, silu is
  *        z sigmoid(z).
  *   dtype: TRIATTN_BF16 (bf16 products, fp32 sums, each output rounded once)
- *          or TRIATTN_F32 (fp32 throughout).
+ *          or TRIATTN_F32 (products of three bf16 parts of each value, which
+ *          keep its 24 bits, and fp32 sums; magnitudes up to 3.38e38).
  *   1 <= m <= 2^31, 1 <= k, n <= 8192 (TRIATTN_ERR_UNSUPPORTED above), any
  *   parity, and fewer than 2^24 tiles of 64 x 64 outputs
  *   (TRIATTN_ERR_UNSUPPORTED).  out may be residual itself.  No workspace.
@@ -353,8 +354,9 @@ int tri_linear_bwd_workspace_bytes(int dtype, int64_t m, int64_t k, int64_t n, i
  *   dx = dz W^T [m][k] (dtype),  dw = x^T dz [k][n] (fp32),
  *   dbias = sum over rows of dz [n] (fp32);
  * the residual's gradient is dout.  Sums over rows are taken in a fixed order
- * (bitwise reproducible).  dx, dw and dbias may each be NULL (not wanted; at
- * least one is not).  Sizes as the forward's, with [m][k] outputs too. */
+ * (bitwise reproducible).  dx, dw and dbias may each be NULL (not wanted), but
+ * not all three.  Sizes as the forward's, with [m][k] outputs too.  For gelu
+ * and silu with k > 128 the workspace holds dz in fp32 (4 m n bytes). */
 int tri_linear_bwd(int dtype, int64_t m, int64_t k, int64_t n, int act, const void* x,
                    const void* w, const void* z, const void* dout, void* dx, float* dw,
                    float* dbias, void* workspace, size_t workspace_bytes, void* stream);

@@ -495,7 +495,7 @@ constexpr int planes() {
 }
 
 template <typename T, int R, bool ALIGNED>
-__global__ __launch_bounds__(256) void lin_fwd_kernel(LinArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void lin_fwd_kernel(LinArgs a) {
   using G = Product<T, T, R, step_k(R, 2 * planes<T>()), true, false, planes<T>(), planes<T>(), DZ_X,
                     DZ_X, ALIGNED, false>;
   __shared__ __attribute__((aligned(16))) char lds[G::LDS];
@@ -505,9 +505,10 @@ __global__ __launch_bounds__(256) void lin_fwd_kernel(LinArgs a) {
   // what the epilogue reads is on its way before the product: the product of a narrow
   // projection is shorter than a memory access
   const int j = j0 + G::piece_col(), have = a.n - j;
-  Raw8<T> res[G::PIECES];
+  // (ragged rows have no registers to spare for the residual)
+  Raw8<T> res[ALIGNED ? G::PIECES : 1];
   float bias[8] = {};
-  if (a.residual) {
+  if (ALIGNED && a.residual) {
 #pragma unroll
     for (int t = 0; t < G::PIECES; ++t) {
       const int64_t i = i0 + G::piece_row(t);
@@ -531,7 +532,8 @@ __global__ __launch_bounds__(256) void lin_fwd_kernel(LinArgs a) {
     }
     if (a.residual) {
       float r[8];
-      unpack(res[t], r);
+      if constexpr (ALIGNED) unpack(res[t], r);
+      else unpack(get8<T, false>((const T*)a.residual + at, have), r);
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] += r[e];
     }
@@ -920,8 +922,8 @@ int64_t tiles_of(int64_t m, int64_t n, int r) { return (m + r - 1) / r * ((n + r
 // 128-wide tiles of an [m][width] result where there are enough of them for the 256 CUs and
 // a second half of a tile to fill, else 64-wide ones (four times as many, at half the reuse
 // of an operand).  fp32 tiles of 128 leave one workgroup on a CU (96 KB of planes), which
-// pays where the products and not the memory take the time: from 256 terms a sum on
-// (measured, 300,000 x 32 x 72 fp32: 73 us in tiles of 128, see the table of cases).
+// pays where the products and not the memory take the time, from 256 terms a sum on
+// (291,975 x 32 x 72 fp32 forward: 73 us in tiles of 128, 45 in tiles of 64).
 template <typename T>
 bool wide(int64_t m, int width, int terms) {
   return width > 64 && tiles_of(m, width, 128) >= 256 && (sizeof(T) == 2 || terms >= 256);
@@ -930,11 +932,12 @@ bool wide(int64_t m, int width, int terms) {
 template <typename T>
 hipError_t fwd(const LinArgs& a, hipStream_t s) {
   KernelTimer t(K_LIN_FWD, s);
-  // ragged rows take 64-wide tiles throughout: in 128-wide ones the repair and what the
-  // epilogue holds leave one workgroup on a CU (368,629 x 66 x 328: 286 against 220 us)
-  const bool al = whole_words<T>(a.k, a.n), big = al && wide<T>(a.m, a.n, a.k);
+  const bool al = whole_words<T>(a.k, a.n);
+  // ragged fp32 rows in tiles of 64 only: 25,152 x 453 x 1179 in 276 against 307 us
+  const bool big = (al || sizeof(T) == 2) && wide<T>(a.m, a.n, a.k);
   const dim3 grid((unsigned)tiles_of(a.m, a.n, big ? 128 : 64)), wg(256);
-  if (big) hipLaunchKernelGGL((lin_fwd_kernel<T, 128, true>), grid, wg, 0, s, a);
+  if (big && al) hipLaunchKernelGGL((lin_fwd_kernel<T, 128, true>), grid, wg, 0, s, a);
+  else if (big) hipLaunchKernelGGL((lin_fwd_kernel<bf16, 128, false>), grid, wg, 0, s, a);
   else if (al) hipLaunchKernelGGL((lin_fwd_kernel<T, 64, true>), grid, wg, 0, s, a);
   else hipLaunchKernelGGL((lin_fwd_kernel<T, 64, false>), grid, wg, 0, s, a);
   return hipGetLastError();
@@ -954,7 +957,8 @@ void bwd_launch(const LinBwdArgs& a, hipStream_t s) {
   const unsigned ndx = (unsigned)tiles_of(a.m, a.k, wx ? 128 : 64);
   const unsigned ndw = (unsigned)(tiles_of(a.k, a.n, ww ? 128 : 64) * a.splits);
   const dim3 wg(256), both(ndx + ndw);
-  if (a.dx && weights && !wx) {
+  // (and a launch holds fewer than 2^32 threads)
+  if (a.dx && weights && !wx && ndx < (1u << 20)) {
     KernelTimer t(K_LIN_BWD_W, s);
     if (ww) hipLaunchKernelGGL((lin_bwd_both_kernel<T, 128, DZ, AL>), both, wg, 0, s, a, (int)ndx);
     else hipLaunchKernelGGL((lin_bwd_both_kernel<T, 64, DZ, AL>), both, wg, 0, s, a, (int)ndx);

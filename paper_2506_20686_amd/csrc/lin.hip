@@ -1038,11 +1038,16 @@ hipError_t bwd(const LinBwdArgs& a, hipStream_t s) {
   return (a.dw || a.dbias) && a.splits > 1 ? reduce(a, s) : hipGetLastError();
 }
 
-// Splits of the rows for dW: enough workgroups for two rounds of the 256 CUs, each of at
-// least 128 rows; none, which needs no further sum, for up to 256 rows.
-int dw_splits(int64_t m, int k, int n) {
-  const int64_t tiles = tiles_of(k, n, wide_w(m, k, n) ? 128 : 64);
-  int64_t s = 512 / tiles, most = (m + 127) / 128;
+// Splits of the rows for dW: as many workgroups as the CUs hold at once beside those of dx
+// in the same launch (LDS and registers allow two or three on a CU, one of fp32 in tiles of
+// 128), each of at least 128 rows; none, which needs no further sum, for up to 256 rows.
+template <typename T>
+int dw_splits(int64_t m, int k, int n, int act) {
+  const bool ww = wide_w(m, k, n), smooth = act > TRIATTN_ACT_RELU;
+  const int64_t tiles = tiles_of(k, n, ww ? 128 : 64);
+  const int64_t fit = 256 * (ww ? (sizeof(T) == 4 ? 1 : 2) : sizeof(T) == 2 && smooth ? 2 : 3);
+  const int64_t ndx = wide<T>(m, k, n) ? 0 : tiles_of(m, k, 64);
+  int64_t s = (ndx < fit * 3 / 4 ? fit - ndx : fit) / tiles, most = (m + 127) / 128;
   if (s > most) s = most;
   if (s < 1 || m <= 256) s = 1;
   const int64_t per = split_rows(m, (int)s);
@@ -1053,7 +1058,9 @@ int dw_splits(int64_t m, int k, int n) {
 
 LinBwdPlan lin_bwd_plan(int dtype, int64_t m, int k, int n, int act) {
   LinBwdPlan p{};
-  p.splits = narrow(dtype, k, n) ? narrow_parts(m, k, n, act) : dw_splits(m, k, n);
+  p.splits = narrow(dtype, k, n) ? narrow_parts(m, k, n, act)
+             : dtype == TRIATTN_BF16 ? dw_splits<bf16>(m, k, n, act)
+                                     : dw_splits<float>(m, k, n, act);
   if (p.splits > 1) p.part = (size_t)p.splits * (size_t)slab_floats(k, n) * sizeof(float);
   if (make_dz(act, k) && !narrow(dtype, k, n)) p.dz = (size_t)m * n * sizeof(float);
   return p;

@@ -325,9 +325,10 @@ int64_t row_groups(int chunks, int64_t m) {
 template <typename T>
 hipError_t fwd(const LnArgs& a, hipStream_t s) {
   KernelTimer t(K_LN_FWD, s);
-  // eight workgroups fill a CU; each keeps its weights over its rounds
+  // eight workgroups fill a CU; with many rounds each keeps its weights over its own, with
+  // few the dispatcher evens them out
   const int64_t g = row_groups((a.c + Chunk<T>::N - 1) / Chunk<T>::N, a.m);
-  const dim3 grid((unsigned)(g < 256 * 8 ? g : 256 * 8));
+  const dim3 grid((unsigned)(g < 256 * 32 ? g : 256 * 8));
   dispatch<T>(a.c, [&](auto shape) {
     hipLaunchKernelGGL((ln_fwd_kernel<T, shape.lanes, shape.chunks>), grid, dim3(LN_WG), 0, s, a);
   });
@@ -365,7 +366,8 @@ int ln_bwd_parts(int dtype, int64_t m, int c) {
   const int64_t groups = row_groups((c * e + 15) / 16, m);
   int64_t most = m * e / 16;
   most = groups <= 4 ? 1 : most < 256 ? 256 : most > 1024 ? 1024 : most;
-  return (int)(groups < most ? groups : most);
+  const int64_t rounds = (groups + most - 1) / most;  // as many for every workgroup
+  return (int)((groups + rounds - 1) / rounds);
 }
 
 hipError_t launch_ln_fwd(int dtype, const LnArgs& a, hipStream_t s) {

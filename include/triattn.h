@@ -374,7 +374,7 @@ int tri_linear_bwd(int dtype, int64_t m, int64_t k, int64_t n, int act, const vo
  *          if one is not above the one before it), read during the call;
  *          1 <= n_edges <= 255 (TRIATTN_ERR_UNSUPPORTED above).
  *   1 <= batch <= 2^20, 1 <= n <= 8192, 1 <= h <= 256 (TRIATTN_ERR_UNSUPPORTED
- *   above).  The sum with base is rounded once.  base may hold -inf.  No
+ *   above), and fewer than 2^39 elements of out (TRIATTN_ERR_UNSUPPORTED).  The sum with base is rounded once.  base may hold -inf.  No
  *   workspace.  pos and chain need 4-byte alignment, the other pointers 16.
  *   Same stream and error rules as above. */
 int tri_rel_bias_fwd(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges,

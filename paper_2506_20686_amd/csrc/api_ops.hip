@@ -51,8 +51,8 @@ int rel_check(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges) {
   if (bad_dtype(dtype) || batch < 1 || batch > ((int64_t)1 << 20) || n < 1 || n > 8192 || h < 1 ||
       n_edges < 1)
     return TRIATTN_ERR_INVALID_ARG;
-  return h > triattn::REL_MAX_H || n_edges > triattn::REL_MAX_EDGES ? TRIATTN_ERR_UNSUPPORTED
-                                                                     : TRIATTN_OK;
+  if (h > triattn::REL_MAX_H || n_edges > triattn::REL_MAX_EDGES) return TRIATTN_ERR_UNSUPPORTED;
+  return batch * n * n * h >= (int64_t)1 << 39 ? TRIATTN_ERR_UNSUPPORTED : TRIATTN_OK;
 }
 
 // The workspace does not depend on whether there are chains: the larger need counts.

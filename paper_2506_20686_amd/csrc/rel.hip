@@ -103,18 +103,23 @@ __global__ __launch_bounds__(256) void rel_fwd_kernel(RelArgs a) {
   const Buckets buckets = load_buckets<LUT>(a, bucket_lds);
   const T* table = (const T*)a.table;
   if (LDS_TABLE) {
+    // in 16-byte words (the table starts at one), then what is left of it
     T* t = (T*)table_lds;
-    for (int i = threadIdx.x; i < a.rows * a.h; i += 256) t[i] = table[i];
+    const int all = a.rows * a.h, words = all / N;
+    for (int i = threadIdx.x; i < words; i += 256) ((u32x4*)t)[i] = ((const u32x4*)table)[i];
+    for (int i = words * N + threadIdx.x; i < all; i += 256) t[i] = table[i];
     table = t;
   }
   __syncthreads();
   const int len = a.n * a.h, chunks = (len + N - 1) / N;
   const int segs = (chunks + 64 * REL_U - 1) / (64 * REL_U), lane = threadIdx.x & 63;
-  const int64_t tasks = a.batch * a.n * segs;
-  for (int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); task < tasks;
-       task += (int64_t)gridDim.x * 4) {
-    const int64_t row = task / segs, b0 = row / a.n * a.n;  // row b n + q; its sample's first
-    const int seg = (int)(task - row * segs);
+  // below 2^31 for fewer than 2^39 elements; divided in 32 bits, as in 64 the two divisions
+  // took longer than the rest of a task
+  const uint32_t tasks = (uint32_t)(a.batch * a.n * segs);
+  for (uint32_t task = blockIdx.x * 4 + (threadIdx.x >> 6); task < tasks; task += gridDim.x * 4) {
+    const uint32_t r32 = task / (uint32_t)segs;  // row b n + q
+    const int seg = (int)(task - r32 * (uint32_t)segs);
+    const int64_t row = r32, b0 = (int64_t)(r32 / (uint32_t)a.n) * a.n;  // its sample's first
     const int32_t pq = a.pos[row], cq = a.chain ? a.chain[row] : 0;
     const T* base = a.base ? (const T*)a.base + row * len : nullptr;
     T* out = (T*)a.out + row * len;

@@ -98,6 +98,7 @@ REL = dict(PTR, dtype=B.BF16, batch=2, n=50, h=4, ne=3, edges=edges(-1, 0, 7), p
            table=P, base=P, out=P, dout=P, dtable=P)
 REL_SIZES = [(dict(dtype=-1), INV), (dict(batch=0), INV), (dict(batch=(1 << 20) + 1), INV),
              (dict(n=0), INV), (dict(n=8193), INV), (dict(h=0), INV), (dict(h=257), UNS),
+             (dict(batch=1 << 20, n=8192, h=256), UNS), (dict(batch=128, n=8192, h=64), UNS),
              (dict(ne=0), INV), (dict(ne=256), UNS), (dict(edges=None), INV),
              (dict(edges=edges(0, 0, 1)), INV), (dict(edges=edges(3, 2, 5)), INV),
              (dict(edges=edges(3, 4, -5)), INV), (dict(pos=None), INV), (dict(pos=P + 2), INV),
@@ -134,7 +135,7 @@ def test_workspace_sizes(lib):
             assert 0 < need and need % 256 == 0
             assert call(lib.tri_linear_bwd, LIN_BWD, LIN,
                         dict(dtype=dtype, m=m, k=k, n=n, wsb=need - 1)) == WS
-        for b, n, h, ne in ((1, 1, 1, 1), (1, 768, 4, 64), (1 << 20, 8192, 256, 255)):
+        for b, n, h, ne in ((1, 1, 1, 1), (1, 768, 4, 64), (64, 8192, 64, 255), (1 << 20, 300, 5, 64)):
             need = B.tri_rel_bias_bwd_workspace_bytes(dtype, b, n, h, ne)
             assert 0 < need and need % 256 == 0
             e = edges(*range(ne))

@@ -88,10 +88,13 @@ struct __attribute__((packed)) Any16 {
 // chunk and h) belong to one pair and take one bucket and one read of the table, which
 // lies in LDS if it has room.  Rows need not start at 16 bytes; a row's last, partial
 // chunk goes element by element.
-constexpr int REL_U = 2;
+template <typename T, int P>
+constexpr int task_chunks() {  // a lane's: more where a chunk is one piece
+  return P == 16 / (int)sizeof(T) ? 4 : 2;
+}
 template <typename T, int P, bool LUT, bool LDS_TABLE>
 __global__ __launch_bounds__(256) void rel_fwd_kernel(RelArgs a) {
-  constexpr int N = 16 / (int)sizeof(T);
+  constexpr int N = 16 / (int)sizeof(T), U = task_chunks<T, P>();
   struct Piece {
     T x[P];
   };
@@ -112,7 +115,7 @@ __global__ __launch_bounds__(256) void rel_fwd_kernel(RelArgs a) {
   }
   __syncthreads();
   const int len = a.n * a.h, chunks = (len + N - 1) / N;
-  const int segs = (chunks + 64 * REL_U - 1) / (64 * REL_U), lane = threadIdx.x & 63;
+  const int segs = (chunks + 64 * U - 1) / (64 * U), lane = threadIdx.x & 63;
   // below 2^31 for fewer than 2^39 elements; divided in 32 bits, as in 64 the two divisions
   // took longer than the rest of a task
   const uint32_t tasks = (uint32_t)(a.batch * a.n * segs);
@@ -123,33 +126,44 @@ __global__ __launch_bounds__(256) void rel_fwd_kernel(RelArgs a) {
     const int32_t pq = a.pos[row], cq = a.chain ? a.chain[row] : 0;
     const T* base = a.base ? (const T*)a.base + row * len : nullptr;
     T* out = (T*)a.out + row * len;
+    // all of the task's loads first; a piece past the row (never stored) takes the last one's
+    Elems add[U];
+    int32_t pk[U][N / P], ck[U][N / P];
+    int column[U][N / P];
 #pragma unroll
-    for (int u = 0; u < REL_U; ++u) {
-      const int e0 = ((seg * REL_U + u) * 64 + lane) * N;
-      if (e0 >= len) continue;
-      const bool whole = e0 + N <= len;
-      Elems add{}, o;
+    for (int u = 0; u < U; ++u) {
+      const int e0 = ((seg * U + u) * 64 + lane) * N;
       if (base) {
-        if (whole) {
-          add = __builtin_bit_cast(Elems, *(const Any16*)(base + e0));
+        if (e0 + N <= len) {
+          add[u] = __builtin_bit_cast(Elems, *(const Any16*)(base + e0));
         } else {
 #pragma unroll
-          for (int e = 0; e < N; ++e)
-            if (e0 + e < len) add.x[e] = base[e0 + e];
+          for (int e = 0; e < N; ++e) add[u].x[e] = base[min(e0 + e, len - 1)];
         }
       }
 #pragma unroll
-      for (int e = 0; e < N; e += P) {
-        const unsigned at = min(e0 + e, len - P);  // a piece past the row is not stored
+      for (int i = 0; i < N / P; ++i) {
+        const unsigned at = min(e0 + i * P, len - P);
         const int k = a.inv_h ? (int)__umulhi(at, a.inv_h) : (int)at;
-        int r = bucket_of<LUT>(a, buckets, pq, a.pos[b0 + k]);
-        if (a.chain && a.chain[b0 + k] != cq) r = a.ne + 1;
-        const Piece t = *(const Piece*)(table + r * a.h + ((int)at - k * a.h));
-#pragma unroll
-        for (int i = 0; i < P; ++i)
-          o.x[e + i] = base ? (T)((float)t.x[i] + (float)add.x[e + i]) : t.x[i];
+        column[u][i] = (int)at - k * a.h;
+        pk[u][i] = a.pos[b0 + k];
+        ck[u][i] = a.chain ? a.chain[b0 + k] : 0;
       }
-      if (whole) {
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int e0 = ((seg * U + u) * 64 + lane) * N;
+      Elems o;
+#pragma unroll
+      for (int i = 0; i < N / P; ++i) {
+        int r = bucket_of<LUT>(a, buckets, pq, pk[u][i]);
+        if (ck[u][i] != cq) r = a.ne + 1;
+        const Piece t = *(const Piece*)(table + r * a.h + column[u][i]);
+#pragma unroll
+        for (int e = 0; e < P; ++e)
+          o.x[i * P + e] = base ? (T)((float)t.x[e] + (float)add[u].x[i * P + e]) : t.x[e];
+      }
+      if (e0 + N <= len) {
         *(Any16*)(out + e0) = __builtin_bit_cast(Any16, o);
       } else {
 #pragma unroll
@@ -403,9 +417,12 @@ bool use_lut(RelArgs& a) {
 constexpr size_t REL_LDS_TABLE = 32 << 10;
 
 template <typename T, int P>
-void fwd_piece(const RelArgs& a, bool lut, unsigned grid, hipStream_t s) {
+void fwd_piece(const RelArgs& a, bool lut, hipStream_t s) {
+  constexpr int SEG = 64 * task_chunks<T, P>();
   const size_t table = (size_t)a.rows * a.h * sizeof(T);
-  const dim3 g(grid), wg(256);
+  const int64_t chunks = ((int64_t)a.n * a.h * sizeof(T) + 15) / 16;
+  const int64_t wgs = (a.batch * a.n * ((chunks + SEG - 1) / SEG) + 3) / 4;
+  const dim3 g((unsigned)(wgs < 256 * 8 ? wgs : 256 * 8)), wg(256);
   if (table <= REL_LDS_TABLE) {
     if (lut) hipLaunchKernelGGL((rel_fwd_kernel<T, P, true, true>), g, wg, table, s, a);
     else hipLaunchKernelGGL((rel_fwd_kernel<T, P, false, true>), g, wg, table, s, a);
@@ -420,14 +437,11 @@ hipError_t fwd(RelArgs a, hipStream_t s) {
   KernelTimer t(K_REL_FWD, s);
   const bool lut = use_lut(a);
   a.inv_h = a.h == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + a.h - 1) / a.h);
-  const int64_t chunks = ((int64_t)a.n * a.h * sizeof(T) + 15) / 16;
-  const int64_t wgs = (a.batch * a.n * ((chunks + 64 * REL_U - 1) / (64 * REL_U)) + 3) / 4;
-  const unsigned grid = (unsigned)(wgs < 256 * 8 ? wgs : 256 * 8);
   constexpr int N = 16 / (int)sizeof(T);
-  if (a.h % N == 0) fwd_piece<T, N>(a, lut, grid, s);
-  else if (N > 4 && a.h % 4 == 0) fwd_piece<T, 4>(a, lut, grid, s);
-  else if (a.h % 2 == 0) fwd_piece<T, 2>(a, lut, grid, s);
-  else fwd_piece<T, 1>(a, lut, grid, s);
+  if (a.h % N == 0) fwd_piece<T, N>(a, lut, s);
+  else if (N > 4 && a.h % 4 == 0) fwd_piece<T, 4>(a, lut, s);
+  else if (a.h % 2 == 0) fwd_piece<T, 2>(a, lut, s);
+  else fwd_piece<T, 1>(a, lut, s);
   return hipGetLastError();
 }
 

@@ -4,7 +4,7 @@
 #include <math.h>
 #include <stdint.h>
 
-#include "kernels.h"
+#include "ops.h"
 #include "triattn.h"
 
 namespace {

@@ -22,8 +22,8 @@
 //
 // Every sum over rows is split over workgroups; their partial sums, in the workspace, are
 // added in a fixed order.
-#include "kernels.h"
 #include "dma.h"
+#include "ops.h"
 #include "timing.h"
 #include "triattn.h"
 

@@ -13,7 +13,7 @@
 //
 // The variance is the mean square of the deviations from the mean (the row is at hand),
 // not a difference of squares, which would lose what a row far from zero has of it.
-#include "kernels.h"
+#include "ops.h"
 #include "slabs.h"
 #include "timing.h"
 #include "triattn.h"

@@ -10,7 +10,7 @@
 #include <limits.h>
 
 #include "dma.h"
-#include "kernels.h"
+#include "ops.h"
 #include "slabs.h"
 #include "timing.h"
 #include "triattn.h"

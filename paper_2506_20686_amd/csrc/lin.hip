@@ -264,7 +264,8 @@ struct Stage {
       const int c0 = (int)(KM ? k0 : i0);
       if constexpr (ALIGNED) {
         x[u] = fetch<T>(w, r0, c0, KM ? R : BK, line, c);
-        if constexpr (DZ != DZ_X) z[u] = fetch<T>(Mat<T>{zp, w.rows, w.cols}, r0, c0, KM ? R : BK, line, c);
+        if constexpr (DZ != DZ_X)
+          z[u] = fetch<T>(Mat<T>{zp, w.rows, w.cols}, r0, c0, KM ? R : BK, line, c);
       } else {
         const int lim = KM ? R : (int)(k1 - k0 < BK ? k1 - k0 : BK);
         x[u] = fetch_any<T>(w, r0, c0, lim, line, c, info[u]);
@@ -388,7 +389,8 @@ struct Product {
 #pragma unroll
       for (int p = 0; p < PA; ++p)
 #pragma unroll
-        for (int u = 0; u < NT; ++u) fa[p][u] = LA::frag(buf + p * LA::PLANE, ri + 32 * u, kk, lane);
+        for (int u = 0; u < NT; ++u)
+          fa[p][u] = LA::frag(buf + p * LA::PLANE, ri + 32 * u, kk, lane);
 #pragma unroll
       for (int p = 0; p < PB; ++p)
 #pragma unroll
@@ -494,6 +496,10 @@ constexpr int planes() {
   return sizeof(T) == 2 ? 1 : 3;
 }
 
+// Forward.  589,824 x 128 x 128 bf16 with residual: 87 us, 5.2 TB/s; 32,768 x 1024 x 512: 45
+// us, 750 TFLOP/s, LDS reads and staging beside the products; 16,384 x 1024 x 1024 fp32: 150
+// TFLOP/s.  Two workgroups on a CU (bf16) hide one's loads and epilogue behind the other's
+// products.
 template <typename T, int R, bool ALIGNED>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void lin_fwd_kernel(LinArgs a) {
   using G = Product<T, T, R, step_k(R, 2 * planes<T>()), true, false, planes<T>(), planes<T>(), DZ_X,
@@ -556,7 +562,8 @@ struct DzSource<T, DZ_MADE> {
 };
 
 // dz = dout act'(z) in fp32, where several column tiles of dx and dW would each form it
-// again from the two tensors (an exponential an element).
+// again from the two tensors (an exponential an element).  Bound by memory and a launch:
+// 1500 x 1536 in 9 us; 1500 x 384 x 1536 backward with it 49 us, without 126.
 template <typename T>
 __global__ __launch_bounds__(256) void lin_dz_kernel(LinBwdArgs a) {
   const int64_t all = a.m * a.n;
@@ -572,7 +579,10 @@ __global__ __launch_bounds__(256) void lin_dz_kernel(LinBwdArgs a) {
   }
 }
 
-// dx = dz W^T: W's rows are the columns of dx, its columns the contraction.
+// dx = dz W^T: W's rows are the columns of dx, its columns the contraction.  Bound by memory
+// for few columns (589,824 x 128 x 128 bf16 in 128-wide tiles: 61 us, 5.0 TB/s), by LDS reads
+// and, with planes, by the matrix cores for many (16,384 x 512 x 2048 with GELU, dx and dW
+// together: 240 us, 5 plane products for 2, 715 TFLOP/s of matrix instructions).
 template <typename T, int R, int DZ, bool ALIGNED>
 using DxProduct = Product<typename DzSource<T, DZ>::E, T, R,
                           step_k(R, DzSource<T, DZ>::P + planes<T>()), true, true,
@@ -608,7 +618,7 @@ __host__ __device__ inline int64_t slab_floats(int k, int n) {
 }
 
 // One split's dW tile and, in the first row of tiles, its dbias.  Without splits the
-// results themselves.
+// results themselves.  The rows are split so that the GPU is full although dW has few tiles.
 template <typename T, int R, int DZ, bool ALIGNED>
 using DwProduct = Product<T, typename DzSource<T, DZ>::E, R,
                           step_k(R, planes<T>() + DzSource<T, DZ>::Q), false, false, planes<T>(),
@@ -662,7 +672,7 @@ __global__ __launch_bounds__(256) void lin_bwd_w_kernel(LinBwdArgs a) {
   dw_tile<T, R, DZ, ALIGNED>(a, lds, xcd_swizzle(blockIdx.x, gridDim.x));
 }
 // Both in one launch, where dx does not fill the GPU: the first ndx workgroups make dx, the
-// others dW (in tiles of RW).
+// others dW (in tiles of RW).  1500 x 384 x 1536 with GELU: 23 us, where the two took 16 and 15.
 template <typename T, int RW, int DZ, bool ALIGNED>
 __global__ __launch_bounds__(256) void lin_bwd_both_kernel(LinBwdArgs a, int ndx) {
   constexpr int LX = DxProduct<T, 64, DZ, ALIGNED>::LDS, LW = DwProduct<T, RW, DZ, ALIGNED>::LDS;
@@ -686,7 +696,8 @@ __global__ __launch_bounds__(256) void lin_bwd_both_kernel(LinBwdArgs a, int ndx
 //
 // M = 128, or 64 where dz takes three planes (96 KB of LDS either way) or where the repair
 // of ragged rows would not fit the registers beside two times 128 rows.
-// 589,824 x 128 x 128: 143 us by the two kernels and their sums, see lin_narrow below.
+// 589,824 x 128 x 128: 85 us (5.3 TB/s of x, dout and dx) and 6 for the sums of 256 slabs, where
+// the two kernels above and their sums take 143.
 struct Square {  // lines of 128 bf16, read along and across
   // Both reads are free of bank conflicts: s differs between any 16 consecutive lines
   // (its low three bits between 8) for 16-byte reads down the lines, and its bits 3, 2 as
@@ -759,7 +770,8 @@ __global__ __launch_bounds__(NARROW_WG) void lin_narrow_kernel(LinBwdArgs a) {
   };
   // this wave's tiles: dx rows di .. + 31, columns dj .. + JW - 1; dW rows (of k) wi .. + 31,
   // columns wj .. + 63
-  const int di = M == 128 ? wave / 2 * 32 : wave / 4 * 32, dj = M == 128 ? wave % 2 * 64 : wave % 4 * 32;
+  const int di = M == 128 ? wave / 2 * 32 : wave / 4 * 32;
+  const int dj = M == 128 ? wave % 2 * 64 : wave % 4 * 32;
   const int wi = wave / 2 * 32, wj = wave % 2 * 64;
   f32x16 gw[2] = {};
   float col[8] = {};
@@ -883,8 +895,8 @@ __global__ __launch_bounds__(NARROW_WG) void lin_narrow_kernel(LinBwdArgs a) {
   }
 }
 
-// Sums of the splits' slabs: `slices` threads (a power of two) to 4 consecutive sums, each
-// every slices-th slab, then their sums through LDS, in a fixed order.
+// Sums of the splits' slabs (256 of 66 KB: 6 us): `slices` threads (a power of two) to 4
+// consecutive sums, each every slices-th slab, then their sums through LDS, in a fixed order.
 __global__ __launch_bounds__(256) void lin_reduce_kernel(LinBwdArgs a, int slices) {
   __shared__ f32x4 sum[256];
   const int cols = 256 / slices, slice = threadIdx.x / cols;
@@ -1018,9 +1030,12 @@ hipError_t bwd_narrow(const LinBwdArgs& a, hipStream_t s) {
     const dim3 grid(narrow_parts(a.m, a.k, a.n, a.act)), wg(NARROW_WG);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, wg, 0, s, a); };
     const bool al = whole_words<bf16>(a.k, a.n);
-    if (a.act == TRIATTN_ACT_NONE) go(al ? lin_narrow_kernel<DZ_X, true> : lin_narrow_kernel<DZ_X, false>);
-    else if (a.act == TRIATTN_ACT_RELU) go(al ? lin_narrow_kernel<DZ_RELU, true> : lin_narrow_kernel<DZ_RELU, false>);
-    else go(al ? lin_narrow_kernel<DZ_ACT, true> : lin_narrow_kernel<DZ_ACT, false>);
+    if (a.act == TRIATTN_ACT_NONE)
+      go(al ? lin_narrow_kernel<DZ_X, true> : lin_narrow_kernel<DZ_X, false>);
+    else if (a.act == TRIATTN_ACT_RELU)
+      go(al ? lin_narrow_kernel<DZ_RELU, true> : lin_narrow_kernel<DZ_RELU, false>);
+    else
+      go(al ? lin_narrow_kernel<DZ_ACT, true> : lin_narrow_kernel<DZ_ACT, false>);
   }
   return (a.dw || a.dbias) && a.splits > 1 ? reduce(a, s) : hipGetLastError();
 }

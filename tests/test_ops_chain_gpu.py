@@ -151,3 +151,38 @@ def test_two_streams_at_once():
     for g, w in zip(got, want):
         for k in w:
             assert torch.equal(g[k], w[k]), k
+
+
+def test_wrappers_refuse_what_the_library_cannot_take():
+    x = torch.randn(6, 16, device=DEV).to(BF)
+    w = torch.randn(16, 8, device=DEV).to(BF)
+    pos = torch.arange(6, dtype=torch.int32, device=DEV)
+    table = torch.randn(3, 4, device=DEV)
+    for call in (lambda: B.layer_norm_fwd(x.t()), lambda: B.layer_norm_fwd(x, x[0].float()),
+                 lambda: B.layer_norm_fwd(x, x[0, :8]), lambda: B.layer_norm_fwd(x.half()),
+                 lambda: B.linear_fwd(x, w.t()), lambda: B.linear_fwd(x, w.float()),
+                 lambda: B.linear_fwd(x, w, residual=x), lambda: B.linear_bwd(x, w, x),
+                 lambda: B.linear_fwd(x.cpu(), w.cpu()),
+                 lambda: B.linear_bwd(x, w, x[:, :8].contiguous(),
+                                      workspace=torch.empty(99, device=DEV)),
+                 lambda: B.rel_bias_fwd(pos.long(), [0, 1], table),
+                 lambda: B.rel_bias_fwd(pos, [0, 1, 2], table),
+                 lambda: B.rel_bias_fwd(pos, [0, 1], table, chain=pos),
+                 lambda: B.rel_bias_fwd(pos, [0, 1], table, base=table),
+                 lambda: B.rel_bias_bwd(pos, [0, 1], torch.zeros(6, 5, 4, device=DEV))):
+        with pytest.raises(ValueError):
+            call()
+    odd = torch.randn(50, 7, device=DEV)
+    for call, code in ((lambda: B.layer_norm_fwd(odd[1:]), B.ERR_INVALID_ARG),  # 28 bytes in
+                       (lambda: B.layer_norm_fwd(odd[:0]), B.ERR_INVALID_ARG),
+                       (lambda: B.layer_norm_fwd(torch.zeros(1, 8200, device=DEV)),
+                        B.ERR_UNSUPPORTED),
+                       (lambda: B.layer_norm_fwd(odd, eps=-1.0), B.ERR_INVALID_ARG),
+                       (lambda: B.linear_fwd(x, w, act=7), B.ERR_INVALID_ARG),
+                       (lambda: B.linear_bwd(x, w, x[:, :8].contiguous(), None, B.ACT_GELU),
+                        B.ERR_INVALID_ARG),
+                       (lambda: B.rel_bias_fwd(pos, [1, 1], table), B.ERR_INVALID_ARG),
+                       (lambda: B.rel_bias_fwd(pos, [], table[:1]), B.ERR_INVALID_ARG)):
+        with pytest.raises(B.TriAttnError) as e:
+            call()
+        assert e.value.status == code

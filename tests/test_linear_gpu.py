@@ -71,6 +71,17 @@ def test_backward(m, k, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F4])
+@pytest.mark.parametrize("m,k,n", [(1, 7, 130), (7, 1, 131), (130, 1, 7), (1, 130, 1), (2, 3, 129),
+                                   (3, 2, 1), (5, 1, 300), (1, 1, 1001), (6, 1, 2), (2, 2, 3)])
+def test_matrices_below_one_chunk(m, k, n, dtype):
+    # a matrix of 1 to 7 elements, on each side, beside short and wide ones
+    t = inputs(m, k, n, dtype, m + 3 * k + n)
+    forward(t, B.ACT_SILU)
+    backward(t, B.ACT_RELU)
+    backward(t, B.ACT_GELU)
+
+
+@pytest.mark.parametrize("dtype", [BF, F4])
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("bias,residual,save_z", [(True, False, False), (False, True, True),
                                                   (True, True, False)])

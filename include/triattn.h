@@ -350,7 +350,7 @@ int tri_linear_bwd_workspace_bytes(int dtype, int64_t m, int64_t k, int64_t n, i
 /* Backward of the projection for L = sum(dout * out): takes the forward's x
  * and W, z as the forward wrote it (NULL for TRIATTN_ACT_NONE) and dout
  * [m][n].  With dz = dout * act'(z), act' evaluated at the z given and dz
- * held in 24 bits (fp32 dw, dbias) or 16 bits (bf16 dx) in the products:
+ * held in 24 bits in the products:
  *   dx = dz W^T [m][k] (dtype),  dw = x^T dz [k][n] (fp32),
  *   dbias = sum over rows of dz [n] (fp32);
  * the residual's gradient is dout.  Sums over rows are taken in a fixed order

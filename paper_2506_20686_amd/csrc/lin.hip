@@ -17,8 +17,8 @@
 // fp32 operands are staged as three planes and a product is the six plane products above
 // 2^-24 of it; sums are fp32 throughout.  Six bf16 instructions for what would be 8 fp32
 // ones of four times the length each.  With bf16 tensors, dz of a smooth activation is
-// not a bf16 value: it enters dW (an fp32 result) as three planes and dx (a bf16 result)
-// as two, 16 bits, so that the result's own rounding is the only one that shows.
+// not a bf16 value: it enters dx and dW as three planes.  (dx is a bf16 result, but of
+// two planes, 16 bits, a difference of neighbouring dz keeps the cut and not the sum.)
 //
 // Every sum over rows is split over workgroups; their partial sums, in the workspace, are
 // added in a fixed order.
@@ -570,17 +570,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void lin_fwd_kernel(Li
 }
 
 // What dz is read from, and as what: the call's dout (and z) in its own type, or the fp32
-// dz that lin_dz_kernel made of them.  P: planes of dx's product, Q: of dW's.
+// dz that lin_dz_kernel made of them.  P: planes of dz.
 template <typename T, int DZ>
 struct DzSource {
   using E = T;
-  static constexpr int STAGE = DZ, P = sizeof(T) == 4 ? 3 : DZ == DZ_ACT ? 2 : 1,
-                       Q = sizeof(T) == 4 || DZ == DZ_ACT ? 3 : 1;
+  static constexpr int STAGE = DZ, P = sizeof(T) == 4 || DZ == DZ_ACT ? 3 : 1;
 };
 template <typename T>
 struct DzSource<T, DZ_MADE> {
   using E = float;
-  static constexpr int STAGE = DZ_X, P = sizeof(T) == 4 ? 3 : 2, Q = 3;
+  static constexpr int STAGE = DZ_X, P = 3;
 };
 
 // dz = dout act'(z) in fp32, where several column tiles of dx and dW would each form it
@@ -643,8 +642,8 @@ __host__ __device__ inline int64_t slab_floats(int k, int n) {
 // results themselves.  The rows are split so that the GPU is full although dW has few tiles.
 template <typename T, int R, int DZ, bool ALIGNED>
 using DwProduct = Product<T, typename DzSource<T, DZ>::E, R,
-                          step_k(R, planes<T>() + DzSource<T, DZ>::Q), false, false, planes<T>(),
-                          DzSource<T, DZ>::Q, DZ_X, DzSource<T, DZ>::STAGE, ALIGNED, true>;
+                          step_k(R, planes<T>() + DzSource<T, DZ>::P), false, false, planes<T>(),
+                          DzSource<T, DZ>::P, DZ_X, DzSource<T, DZ>::STAGE, ALIGNED, true>;
 template <typename T, int R, int DZ, bool ALIGNED>
 __device__ inline void dw_tile(const LinBwdArgs& a, char* lds, int wg) {
   using E = typename DzSource<T, DZ>::E;
@@ -756,7 +755,7 @@ __global__ __launch_bounds__(NARROW_WG) void lin_narrow_kernel(LinBwdArgs a) {
   constexpr int M = narrow_rows(DZ, ALIGNED), N = M / 32;       // chunks a thread stages of a tile
   constexpr int JT = M / 64, JW = 32 * JT;             // dx tiles, columns of a wave
   constexpr int TILE_BYTES = M * 256, W_BYTES = 128 * 256;
-  __shared__ __attribute__((aligned(16))) char lds[W_BYTES + (1 + S::Q) * TILE_BYTES];
+  __shared__ __attribute__((aligned(16))) char lds[W_BYTES + (1 + S::P) * TILE_BYTES];
   char *tw = lds, *tx = lds + W_BYTES, *tz = tx + TILE_BYTES;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const bool weights = a.dw || a.dbias;
@@ -816,12 +815,12 @@ __global__ __launch_bounds__(NARROW_WG) void lin_narrow_kernel(LinBwdArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) col[e] += f[e];
 #pragma unroll
-      for (int p = 0; p < S::Q; ++p) {
+      for (int p = 0; p < S::P; ++p) {
         bf16x8 b;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           b[e] = (bf16)f[e];
-          if (p + 1 < S::Q) f[e] -= (float)b[e];
+          if (p + 1 < S::P) f[e] -= (float)b[e];
         }
         *(bf16x8*)(tz + p * TILE_BYTES + at) = b;
       }
@@ -833,7 +832,7 @@ __global__ __launch_bounds__(NARROW_WG) void lin_narrow_kernel(LinBwdArgs a) {
       for (int kk = 0; kk < M; kk += 16) {
         const bf16x8 fx = Square::across(tx, wi, kk, lane);
 #pragma unroll
-        for (int p = S::Q - 1; p >= 0; --p)
+        for (int p = S::P - 1; p >= 0; --p)
 #pragma unroll
           for (int v = 0; v < 2; ++v)
             gw[v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(

@@ -1,5 +1,6 @@
 """How many bits the linear projection keeps where its bf16 outputs or random
-inputs would hide a loss (plain 64-bit forms in ops_ref.py)."""
+inputs would hide a loss: dz in the products of dx, the activations and their
+derivatives in the tails (plain 64-bit forms in ops_ref.py)."""
 import pytest
 import torch
 
@@ -8,7 +9,7 @@ from paper_2506_20686_amd import binding as B
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
-BF = torch.bfloat16
+BF, F4 = torch.bfloat16, torch.float32
 NAMES = {B.ACT_GELU: "gelu", B.ACT_SILU: "silu"}
 
 
@@ -43,3 +44,48 @@ def test_dx_takes_dz_in_24_bits(m, k, n, act):
     ref = dz[:, a] - dz[:, a + 1]
     e = 2 * 8 * R.U * dy[:, a] + 6 * R.U * torch.maximum(dz[:, a], dz[:, a + 1])
     R.check("dx", dx, ref, R.HALF[BF] * ref.abs() + 1.01 * e)
+
+
+def tail_points(limit):
+    """z over both tails, dense around zero, in fp32."""
+    g = torch.Generator().manual_seed(7)
+    return torch.cat([torch.linspace(-limit, limit, 20001), torch.randn(9000, generator=g),
+                      torch.randn(2000, generator=g) * 1e-3, torch.tensor([0.0, -0.0])])[:, None]
+
+
+# e^(-z^2/2) and e^z stay above 2^-126 up to here, the least normal fp32
+LIMIT = {B.ACT_GELU: 13.0, B.ACT_SILU: 87.0}
+
+
+@pytest.mark.parametrize("act", [B.ACT_GELU, B.ACT_SILU], ids=NAMES.get)
+def test_activation_values_in_the_tails_fp32(act):
+    # one weight of 1: the product gives z itself.  Of the value: the exponential is good to
+    # 4 roundings, the reciprocal to 2, the polynomial to 4, and there are 4 more products
+    # and sums
+    z = tail_points(LIMIT[act])
+    out, back = B.linear_fwd(z.to(DEV), torch.ones(1, 1, device=DEV), act=act, save_z=True)
+    assert torch.equal(back.cpu(), z)
+    ref = R.act(z.to(R.F8), act)
+    R.check("out", out, ref, 14 * R.U * ref.abs())
+
+
+# dz formed in the staging, and made beforehand (k above 128)
+@pytest.mark.parametrize("k", [1, 130])
+@pytest.mark.parametrize("act", [B.ACT_GELU, B.ACT_SILU], ids=NAMES.get)
+def test_activation_derivatives_in_the_tails_fp32(act, k):
+    # one column of ones: dx is dz, and with dout = 1 act'(z), in whose two terms the value's
+    # 14 roundings and those of a product and a sum enter (they cancel near its zero)
+    z = tail_points(LIMIT[act])
+    x = torch.zeros(z.shape[0], k)
+    dx, _, db = B.linear_bwd(x.to(DEV), torch.ones(k, 1, device=DEV),
+                             torch.ones(z.shape, device=DEV), z.to(DEV), act)
+    zd = z.to(R.F8)
+    ref = R.act_grad(zd, act)
+    if act == B.ACT_GELU:
+        parts = 0.5 * torch.erfc(-zd * R.SQRT_HALF) + (ref - 0.5 * torch.erfc(-zd * R.SQRT_HALF)).abs()
+    else:
+        parts = torch.sigmoid(zd) * (1 + zd.abs() * torch.sigmoid(-zd))
+    bound = 17 * R.U * parts
+    R.check("dx", dx, ref.expand(-1, k), bound.expand(-1, k))
+    # and the sum over the rows, in any order
+    R.check("dbias", db, ref.sum(0), bound.sum(0) + z.shape[0] * R.U * ref.abs().sum(0))

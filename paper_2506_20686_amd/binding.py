@@ -911,16 +911,27 @@ def linear_bwd(x, w, dout, z=None, act: int = ACT_NONE,
 
 def rel_bias_edges(exact: int, far: int = 0, steps: int = 0):
     """Ascending bucket borders for rel_bias_fwd, alike on both sides: the
-    differences -exact .. exact - 1 have buckets of their own, and beyond them
-    `steps` buckets a side grow geometrically up to `far` (fewer where two
+    differences 1 - exact .. exact - 1 have buckets of their own, and beyond
+    them `steps` buckets a side grow geometrically up to `far` (fewer where two
     borders would round to one); what is further shares the outermost bucket.
     With steps = 0, bucket i is the difference clipped to [-exact, exact],
     plus exact."""
     exact, far, steps = int(exact), int(far), int(steps)
     if exact < 1 or steps < 0 or (steps > 0 and far <= exact):
         raise ValueError("exact >= 1, steps >= 0 and, with steps, far > exact are needed")
-    up = list(range(1, exact + 1))
-    up += sorted({math.ceil(exact * (far / exact) ** ((i + 1) / steps)) for i in range(steps)})
+
+    def border(i):
+        """exact (far / exact)^(i / steps), rounded up; where it is an integer or close
+        to one, whole numbers decide, which nothing rounds."""
+        if i == steps:
+            return far
+        value = exact * (far / exact) ** (i / steps)
+        near = round(value)
+        if abs(value - near) > 1e-12 * value:
+            return math.ceil(value)
+        return near + (near ** steps < exact ** (steps - i) * far ** i)
+
+    up = list(range(1, exact + 1)) + sorted({border(i + 1) for i in range(steps)})
     return [1 - e for e in reversed(up)] + up
 
 

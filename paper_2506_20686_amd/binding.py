@@ -344,6 +344,8 @@ def tri_linear_bwd(dtype, m, k, n, act, x, w, z, dout, dx, dw, dbias, workspace,
 
 
 def _edges_arr(edges):
+    if isinstance(edges, (bytes, bytearray)):  # would be taken as the array's memory
+        raise TypeError("edges must be a sequence of integers")
     try:
         values = array.array("i", edges)  # 32 bits; checks every value
     except OverflowError as e:

@@ -43,3 +43,15 @@ def test_both_sides_alike(args):
     assert all(every.count(b) == 1 for b in own)
     assert all(bucket(d) + bucket(-d) == len(edges) for d in range(601))
     assert every[0] == 0 and every[-1] == len(edges)
+
+
+@pytest.mark.parametrize("raw", [bytes(8), bytearray(16), b"\x00\x01\x02\x03"])
+def test_raw_bytes_are_no_borders(raw):
+    # their length counts bytes: the library would read four times what there is
+    with pytest.raises(TypeError):
+        B._edges_arr(raw)
+    for call in (lambda: B.tri_rel_bias_fwd(B.F32, 1, 4, 4, raw, None, None, None, None, None, None),
+                 lambda: B.tri_rel_bias_bwd(B.F32, 1, 4, 4, raw, None, None, None, None, None, 0,
+                                            None)):
+        with pytest.raises(TypeError):
+            call()

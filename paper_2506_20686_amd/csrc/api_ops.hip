@@ -35,13 +35,14 @@ size_t ln_ws(int dtype, int64_t m, int64_t c) {
   return round256((size_t)triattn::ln_bwd_parts(dtype, m, (int)c) * 2 * c * sizeof(float));
 }
 
-int lin_check(int dtype, int64_t m, int64_t k, int64_t n, int act) {
+// `width`: of the widest result, n or (backward) the larger of k and n.
+int lin_check(int dtype, int64_t m, int64_t k, int64_t n, int act, int64_t width) {
   if (bad_dtype(dtype) || m < 1 || m > MAX_M || k < 1 || n < 1) return TRIATTN_ERR_INVALID_ARG;
   if (act < TRIATTN_ACT_NONE || act > TRIATTN_ACT_SILU) return TRIATTN_ERR_INVALID_ARG;
   if (k > triattn::LIN_MAX_K || n > triattn::LIN_MAX_K) return TRIATTN_ERR_UNSUPPORTED;
   // a launch holds fewer than 2^32 threads
-  const int64_t wide = ((k > n ? k : n) + 63) / 64;
-  return (m + 63) / 64 * wide >= (int64_t)1 << 24 ? TRIATTN_ERR_UNSUPPORTED : TRIATTN_OK;
+  const int64_t tiles = (m + 63) / 64 * ((width + 63) / 64);
+  return tiles >= (int64_t)1 << 24 ? TRIATTN_ERR_UNSUPPORTED : TRIATTN_OK;
 }
 
 // Partial sums, then dz; never 0, so that a workspace is always one.
@@ -148,7 +149,7 @@ int tri_layer_norm_bwd(int dtype, int64_t m, int64_t c, const void* x, const voi
 int tri_linear_fwd(int dtype, int64_t m, int64_t k, int64_t n, int act, const void* x,
                    const void* w, const void* bias, const void* residual, void* out, void* z,
                    void* stream) {
-  const int st = lin_check(dtype, m, k, n, act);
+  const int st = lin_check(dtype, m, k, n, act, n);
   if (st != TRIATTN_OK) return st;
   if (bad_pointers({x, w, out}, {bias, residual, z})) return TRIATTN_ERR_INVALID_ARG;
   triattn::LinArgs a{};
@@ -167,7 +168,7 @@ int tri_linear_fwd(int dtype, int64_t m, int64_t k, int64_t n, int act, const vo
 
 int tri_linear_bwd_workspace_bytes(int dtype, int64_t m, int64_t k, int64_t n, int act,
                                    size_t* bytes) {
-  const int st = lin_check(dtype, m, k, n, act);
+  const int st = lin_check(dtype, m, k, n, act, k > n ? k : n);
   if (st != TRIATTN_OK) return st;
   if (bytes == nullptr) return TRIATTN_ERR_INVALID_ARG;
   *bytes = lin_ws(triattn::lin_bwd_plan(dtype, m, (int)k, (int)n, act));
@@ -177,7 +178,7 @@ int tri_linear_bwd_workspace_bytes(int dtype, int64_t m, int64_t k, int64_t n, i
 int tri_linear_bwd(int dtype, int64_t m, int64_t k, int64_t n, int act, const void* x,
                    const void* w, const void* z, const void* dout, void* dx, float* dw,
                    float* dbias, void* workspace, size_t workspace_bytes, void* stream) {
-  const int st = lin_check(dtype, m, k, n, act);
+  const int st = lin_check(dtype, m, k, n, act, k > n ? k : n);
   if (st != TRIATTN_OK) return st;
   if (bad_pointers({x, w, dout}, {z, dx, dw, dbias})) return TRIATTN_ERR_INVALID_ARG;
   if (act != TRIATTN_ACT_NONE && z == nullptr) return TRIATTN_ERR_INVALID_ARG;

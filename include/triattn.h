@@ -328,7 +328,9 @@ int tri_layer_norm_bwd(int dtype, int64_t m, int64_t c, const void* x, const voi
  *        z sigmoid(z).
  *   dtype: TRIATTN_BF16 (bf16 products, fp32 sums, each output rounded once)
  *          or TRIATTN_F32 (products of three bf16 parts of each value, which
- *          keep its 24 bits, and fp32 sums; magnitudes up to 3.38e38).
+ *          keep its 24 bits from 2^-110 (7.7e-34) to 3.38e38 in magnitude, and
+ *          smaller values to 2^-134; fp32 sums).  Values must be finite, as
+ *          everywhere: the parts of an infinity are not numbers.
  *   1 <= m <= 2^31, 1 <= k, n <= 8192 (TRIATTN_ERR_UNSUPPORTED above), any
  *   parity, and fewer than 2^24 tiles of 64 x 64 outputs
  *   (TRIATTN_ERR_UNSUPPORTED).  out may be residual itself.  No workspace.

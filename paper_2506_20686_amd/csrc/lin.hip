@@ -15,7 +15,8 @@
 //
 // Precision: an fp32 value is the sum of three bf16 (8 bits each, rounded to nearest), so
 // fp32 operands are staged as three planes and a product is the six plane products above
-// 2^-24 of it; sums are fp32 throughout.  Six bf16 instructions for what would be 8 fp32
+// 2^-24 of it; sums are fp32 throughout.  (The matrix cores take subnormal bf16 as they
+// are, so the third plane ends at 2^-133: values below 2^-110 keep fewer bits.)  Six bf16 instructions for what would be 8 fp32
 // ones of four times the length each.  With bf16 tensors, dz of a smooth activation is
 // not a bf16 value: it enters dx and dW as three planes.  (dx is a bf16 result, but of
 // two planes, 16 bits, a difference of neighbouring dz keeps the cut and not the sum.)

@@ -89,3 +89,24 @@ def test_activation_derivatives_in_the_tails_fp32(act, k):
     R.check("dx", dx, ref.expand(-1, k), bound.expand(-1, k))
     # and the sum over the rows, in any order
     R.check("dbias", db, ref.sum(0), bound.sum(0) + z.shape[0] * R.U * ref.abs().sum(0))
+
+
+@pytest.mark.parametrize("m,k,n", [(300, 40, 24), (77, 33, 45)])
+def test_least_magnitudes_fp32(m, k, n):
+    # a value enters the products in three parts of 8 bits, the last of them no finer than
+    # bf16's least subnormal, 2^-133: to 24 bits, or to 2^-134 where that is more (below
+    # 2^-110); the other operand is scaled up, so that no result is itself that small
+    g = torch.Generator().manual_seed(m)
+    small = (torch.randn(m, k, generator=g) * torch.exp2(-95 - 35 * torch.rand(m, 1, generator=g)))
+    big = torch.randn(k, n, generator=g) * 2.0 ** 60
+    out, _ = B.linear_fwd(small.to(DEV), big.to(DEV))
+    (ref, _), (e, _) = R.lin_fwd(small, big, None, None, 0)
+    R.check("out", out, ref, e + 2.0 ** -134 * big.to(R.F8).abs().sum(0))
+    # dx = dz W^T of small dz; dW = x^T dz of small x
+    dx = B.linear_bwd(torch.zeros(m, n).to(DEV), big.t().contiguous().to(DEV), small.to(DEV))[0]
+    (ref, _, _), (e, _, _) = R.lin_bwd(torch.zeros(m, n), big.t().contiguous(), small, None, 0)
+    R.check("dx", dx, ref, e + 2.0 ** -134 * big.to(R.F8).abs().sum(0))
+    dz = torch.randn(m, n, generator=g) * 2.0 ** 60
+    dw = B.linear_bwd(small.to(DEV), torch.zeros(k, n).to(DEV), dz.to(DEV))[1]
+    (_, ref, _), (_, e, _) = R.lin_bwd(small, torch.zeros(k, n), dz, None, 0)
+    R.check("dw", dw, ref, e + 2.0 ** -134 * dz.to(R.F8).abs().sum(0))

@@ -1043,7 +1043,7 @@ void bwd_launch(const LinBwdArgs& a, hipStream_t s) {
   const dim3 wg(256), both(ndx + ndw);
   // (and a launch holds fewer than 2^32 threads)
   if (a.dx && weights && !wx && ndx < (1u << 20)) {
-    KernelTimer t(K_LIN_BWD_W, s);
+    KernelTimer t(K_LIN_BWD_BOTH, s);
     if (ww) hipLaunchKernelGGL((lin_bwd_both_kernel<T, 128, DZ, AL>), both, wg, 0, s, a, (int)ndx);
     else hipLaunchKernelGGL((lin_bwd_both_kernel<T, 64, DZ, AL>), both, wg, 0, s, a, (int)ndx);
     return;

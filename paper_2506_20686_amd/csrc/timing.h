@@ -44,6 +44,7 @@ enum KernelId {
   K_REL_FWD,
   K_REL_BWD,
   K_REL_REDUCE,
+  K_LIN_BWD_BOTH,
   K_COUNT
 };
 

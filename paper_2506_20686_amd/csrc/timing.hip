@@ -22,7 +22,7 @@ const char* const kNames[K_COUNT] = {"prep_bias",   "prep_kbits", "fwd",        
                                      "pad16",       "ln_fwd",     "ln_bwd",     "ln_reduce",
                                      "lin_fwd",     "lin_bwd_dx", "lin_bwd_w",  "lin_reduce", "lin_dz",
                                      "lin_narrow",
-                                     "rel_fwd",     "rel_bwd",    "rel_reduce"};
+                                     "rel_fwd",     "rel_bwd",    "rel_reduce", "lin_bwd_both"};
 
 struct Pending {
   int id;

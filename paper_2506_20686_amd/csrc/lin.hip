@@ -438,7 +438,12 @@ struct Product {
     };
 #pragma unroll
     for (int d = 0; d < D; ++d) load(d, d);
-    if constexpr (ALIGNED || sizeof(TA) == 2) {
+    // Ragged fp32 operands have the longest code by far (repair and split of both), so where
+    // few steps run it, one copy of a step and its loads instead of two.  One copy against two:
+    // gradients at 2777 x 449 x 131 (5 and 6 steps) 20.6 and 24.6 us; at 25,152 x 453 x 1179
+    // (37 and 132) 886 and 840, at 40 x 1001 x 1001 (32 and 2) 52 and 47.
+    constexpr bool LONG = !ALIGNED && sizeof(TA) == 4 && sizeof(TB) == 4;
+    if (!LONG || steps >= 16) {
       int it = 0;
       for (; it + 2 <= steps; it += 2) {
         step(0, lds, it);
@@ -446,9 +451,6 @@ struct Product {
       }
       if (it < steps) step(0, lds, it);
     } else {
-      // the longest code by far (repair and split of both operands), so one copy of a step and
-      // its loads instead of two: 24.6 -> 20.6 us for the gradients at 2777 x 449 x 131, against
-      // 737 -> 789 us at 25152 x 453 x 1179
       for (int it = 0; it < steps; ++it) step(0, lds + (it & 1) * BUF, it);
     }
   }

@@ -294,8 +294,9 @@ int tri_transition_bwd(int dtype, int64_t m, int64_t c, int64_t f, const void* x
  *   dtype: TRIATTN_F32 or TRIATTN_BF16; fp32 statistics and arithmetic, out
  *          rounded once.
  *   1 <= m <= 2^31, 1 <= c <= 8192 (TRIATTN_ERR_UNSUPPORTED above), any
- *   parity; eps finite and >= 0.  out may be x itself.  No workspace.  Same
- *   stream, pointer and error rules as above. */
+ *   parity; eps finite and >= 0 (with 0, a row of one value has no rstd and
+ *   unspecified outputs).  out may be x itself.  No workspace.  Same stream,
+ *   pointer and error rules as above. */
 int tri_layer_norm_fwd(int dtype, int64_t m, int64_t c, float eps, const void* x,
                        const void* gamma, const void* beta, void* out, float* mean, float* rstd,
                        void* stream);
@@ -376,9 +377,10 @@ int tri_linear_bwd(int dtype, int64_t m, int64_t k, int64_t n, int act, const vo
  *          if one is not above the one before it), read during the call;
  *          1 <= n_edges <= 255 (TRIATTN_ERR_UNSUPPORTED above).
  *   1 <= batch <= 2^20, 1 <= n <= 8192, 1 <= h <= 256 (TRIATTN_ERR_UNSUPPORTED
- *   above), and fewer than 2^39 elements of out (TRIATTN_ERR_UNSUPPORTED).  The sum with base is rounded once.  base may hold -inf.  No
- *   workspace.  pos and chain need 4-byte alignment, the other pointers 16.
- *   Same stream and error rules as above. */
+ *   above 256), and fewer than 2^39 elements of out (TRIATTN_ERR_UNSUPPORTED).
+ *   The sum with base is rounded once.  base may hold -inf.  No workspace.  pos
+ *   and chain need 4-byte alignment, the other pointers 16.  Same stream and
+ *   error rules as above. */
 int tri_rel_bias_fwd(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges,
                      const int32_t* edges, const int32_t* pos, const int32_t* chain,
                      const void* table, const void* base, void* out, void* stream);

@@ -109,3 +109,40 @@ def test_backward(dtype, m, k, n, act, wx, ww):
                                 ws.data_ptr(), need, s) == B.OK
         for a, b in zip(alone, got):
             assert a is None or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,m,k,n", [(BF, 33000, 128, 128), (BF, 33001, 77, 129),
+                                         (F4, 16500, 260, 132)])
+def test_output_over_the_residual(dtype, m, k, n):
+    assert wide(dtype, m, n, k)
+    t = {a: b.to(DEV) for a, b in inputs(m, k, n, dtype, 4).items()}
+    want, _ = B.linear_fwd(t["x"], t["w"], t["bias"], t["residual"], SILU)
+    r = t["residual"].data_ptr()
+    code = B.BF16 if dtype == BF else B.F32
+    assert B.tri_linear_fwd(code, m, k, n, SILU, t["x"].data_ptr(), t["w"].data_ptr(),
+                            t["bias"].data_ptr(), r, r, None,
+                            torch.cuda.current_stream().cuda_stream) == B.OK
+    assert torch.equal(t["residual"], want)
+
+
+def test_gelu_backward_in_a_graph():
+    # dz made beforehand, both products and the splits' sums, replayed on other inputs with
+    # eager work between; the workspace full of other values before each replay
+    m, k, n = 1700, 512, 512
+    assert wide_w(m, k, n) is False
+    sets = [{a: b.to(DEV) for a, b in inputs(m, k, n, BF, s).items()} for s in (1, 2)]
+    t = {a: b.clone() for a, b in sets[0].items()}
+    ws = torch.empty(B.tri_linear_bwd_workspace_bytes(B.BF16, m, k, n, GELU), dtype=torch.uint8,
+                     device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = B.linear_bwd(t["x"], t["w"], t["dout"], t["z"], GELU, ws)
+    for s in (1, 0, 1):
+        want = B.linear_bwd(*(sets[s][a] for a in ("x", "w", "dout", "z")), GELU)
+        for a in t:
+            t[a].copy_(sets[s][a])
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)

@@ -577,7 +577,7 @@ constexpr int planes() {
 }
 
 // Forward.  589,824 x 128 x 128 bf16 with residual: 87 us, 5.2 TB/s; 32,768 x 1024 x 512: 45
-// us, 750 TFLOP/s, LDS reads and staging beside the products; 16,384 x 1024 x 1024 fp32: 150
+// to 54 us on different cards, 640 to 750 TFLOP/s, LDS reads and staging beside the products; 16,384 x 1024 x 1024 fp32: 150
 // TFLOP/s.  Two workgroups on a CU (bf16) hide one's loads and epilogue behind the other's
 // products.
 template <typename T, int R, bool ALIGNED>
@@ -642,7 +642,8 @@ struct DzSource<T, DZ_MADE> {
 
 // dz = dout act'(z) in fp32, where several column tiles of dx and dW would each form it
 // again from the two tensors (an exponential an element).  Bound by memory and a launch:
-// 1500 x 1536 in 9 us; 1500 x 384 x 1536 backward with it 49 us, without 126.
+// 1500 x 1536 in 8.5 us; 1500 x 384 x 1536 backward with it 41 us, without 71; 16,384 x 512 x
+// 2048 with it 271, without 412.
 template <typename T>
 __global__ __launch_bounds__(256) void lin_dz_kernel(LinBwdArgs a) {
   const int64_t all = a.m * a.n;
@@ -659,9 +660,9 @@ __global__ __launch_bounds__(256) void lin_dz_kernel(LinBwdArgs a) {
 }
 
 // dx = dz W^T: W's rows are the columns of dx, its columns the contraction.  Bound by memory
-// for few columns (589,824 x 128 x 128 bf16 in 128-wide tiles: 61 us, 5.0 TB/s), by LDS reads
-// and, with planes, by the matrix cores for many (16,384 x 512 x 2048 with GELU, dx and dW
-// together: 240 us, 5 plane products for 2, 715 TFLOP/s of matrix instructions).
+// for few columns (294,912 x 256 x 128 bf16 in 128-wide tiles: 45 us, 5.0 TB/s), by LDS reads
+// and, with planes, by the matrix cores for many (16,384 x 512 x 2048 with GELU: 106 us, and dW
+// 106, three plane products each, 970 TFLOP/s of matrix instructions).
 template <typename T, int R, int DZ, bool ALIGNED>
 using DxProduct = Product<typename DzSource<T, DZ>::E, T, R,
                           step_k(R, DzSource<T, DZ>::P + planes<T>()), true, true,
@@ -751,7 +752,8 @@ __global__ __launch_bounds__(256) void lin_bwd_w_kernel(LinBwdArgs a) {
   dw_tile<T, R, DZ, ALIGNED>(a, lds, xcd_swizzle(blockIdx.x, gridDim.x));
 }
 // Both in one launch, where dx does not fill the GPU: the first ndx workgroups make dx, the
-// others dW (in tiles of RW).  1500 x 384 x 1536 with GELU: 23 us, where the two took 16 and 15.
+// others dW (in tiles of RW).  1500 x 384 x 1536 with GELU: 28 us, where the two take 27 and
+// 20.
 template <typename T, int RW, int DZ, bool ALIGNED>
 __global__ __launch_bounds__(256) void lin_bwd_both_kernel(LinBwdArgs a, int ndx) {
   constexpr int LX = DxProduct<T, 64, DZ, ALIGNED>::LDS, LW = DwProduct<T, RW, DZ, ALIGNED>::LDS;
@@ -1024,7 +1026,7 @@ template <typename T>
 hipError_t fwd(const LinArgs& a, hipStream_t s) {
   KernelTimer t(K_LIN_FWD, s);
   const bool al = whole_words<T>(a.k, a.n);
-  // ragged fp32 rows in tiles of 64 only: 25,152 x 453 x 1179 in 276 against 307 us
+  // ragged fp32 rows in tiles of 64 only: 25,152 x 453 x 1179 in 253 against 301 us
   const bool big = (al || sizeof(T) == 2) && wide<T>(a.m, a.n, a.k);
   const dim3 grid((unsigned)tiles_of(a.m, a.n, big ? 128 : 64)), wg(256);
   if (big && al) hipLaunchKernelGGL((lin_fwd_kernel<T, 128, true>), grid, wg, 0, s, a);
@@ -1134,7 +1136,8 @@ hipError_t bwd(const LinBwdArgs& a, hipStream_t s) {
 
 // Splits of the rows for dW: as many workgroups as the CUs hold at once beside those of dx
 // in the same launch (LDS and registers allow two or three on a CU, one of fp32 in tiles of
-// 128), each of at least 128 rows; none, which needs no further sum, for up to 256 rows.
+// 128, and one of ragged bf16 in tiles of 128 without planes, whose 193 + 64 registers are a
+// few too many for the two that are counted here: its grid runs in two turns), each of at least 128 rows; none, which needs no further sum, for up to 256 rows.
 template <typename T>
 int dw_splits(int64_t m, int k, int n, int act) {
   const bool ww = wide_w(m, k, n), smooth = act > TRIATTN_ACT_RELU;

@@ -107,8 +107,10 @@ __device__ inline float row_sum(float v, float (*slot)[4], int& turn) {
   return L == LN_WG ? wg_sum(v, slot, turn) : group_sum<L>(v);
 }
 
-// Forward.  589,824 x 128 bf16: 55 us, 5.5 TB/s of x and out (a large copy reaches 5.1); 9001 x
-// 833 bf16, rows at any element: 13 us, two rounds of a row's latency.
+// Forward.  589,824 x 128 bf16: 55 us, 5.5 TB/s of x and out (a large copy reaches 5.1); 65,536 x
+// 1024: 46, 5.9 TB/s; 9001 x 833 bf16, rows at any element: 14 us.  A chunk's load lies in the
+// branch of whole chunks, behind which the compiler waits for it, so with few rows a wave the
+// chunks' latencies (of gamma, beta and x) add up.
 template <typename T, int L, int V>
 __global__ __launch_bounds__(LN_WG) void ln_fwd_kernel(LnArgs a) {
   constexpr int N = Chunk<T>::N, G = LN_WG / L;
@@ -166,7 +168,8 @@ __global__ __launch_bounds__(LN_WG) void ln_fwd_kernel(LnArgs a) {
 // Backward: dx as in the forward, and each lane's terms of dgamma and dbeta kept in its
 // registers over all of its rows; the workgroup's totals go to its slab of the workspace
 // (fixed order: lanes, then waves), which ln_reduce_kernel adds up.  589,824 x 128 bf16: 99 us,
-// 4.6 TB/s of x, dout and dx, with 1024 slabs of 1 KB; 9001 x 833 bf16: 17 us.
+// 4.6 TB/s of x, dout and dx, with 1024 slabs of 1 KB; 100,000 x 384: 60, 3.9 TB/s; 9001 x 833
+// bf16: 17 to 19 us (a chunk's loads wait for each other as in the forward).
 template <typename T, int L, int V, bool WG>
 __global__ __launch_bounds__(LN_WG) void ln_bwd_kernel(LnBwdArgs a) {
   constexpr int N = Chunk<T>::N, G = LN_WG / L, ROW = (L < 64 ? L : 64) * V * N;

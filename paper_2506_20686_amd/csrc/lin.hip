@@ -13,13 +13,13 @@
 // fragments are 16-byte reads) or [contraction][row] (fragments are the LDS's transposing
 // reads), so neither W, W^T nor x^T is ever copied.
 //
-// Precision: an fp32 value is the sum of three bf16 (8 bits each, rounded to nearest), so
-// fp32 operands are staged as three planes and a product is the six plane products above
-// 2^-24 of it; sums are fp32 throughout.  (The matrix cores take subnormal bf16 as they
-// are, so the third plane ends at 2^-133: values below 2^-110 keep fewer bits.)  Six bf16 instructions for what would be 8 fp32
-// ones of four times the length each.  With bf16 tensors, dz of a smooth activation is
-// not a bf16 value: it enters dx and dW as three planes.  (dx is a bf16 result, but of
-// two planes, 16 bits, a difference of neighbouring dz keeps the cut and not the sum.)
+// Precision: an fp32 value is the sum of three bf16 (8 bits each, rounded to nearest), so fp32
+// operands are staged as three planes and a product is the six plane products above 2^-24 of it;
+// sums are fp32 throughout.  (The matrix cores take subnormal bf16 as they are, so the third plane
+// ends at 2^-133: values below 2^-110 keep fewer bits.)  Six bf16 instructions for what would be 8
+// fp32 ones of four times the length each.  With bf16 tensors, dz of a smooth activation is not a
+// bf16 value: it enters dx and dW as three planes.  (dx is rounded to bf16 itself, but where its
+// sum cancels, the cut of a dz to two planes, 16 bits, would show.)
 //
 // Every sum over rows is split over workgroups; their partial sums, in the workspace, are
 // added in a fixed order.
@@ -576,10 +576,10 @@ constexpr int planes() {
   return sizeof(T) == 2 ? 1 : 3;
 }
 
-// Forward.  589,824 x 128 x 128 bf16 with residual: 87 us, 5.2 TB/s; 32,768 x 1024 x 512: 45
-// to 54 us on different cards, 640 to 750 TFLOP/s, LDS reads and staging beside the products; 16,384 x 1024 x 1024 fp32: 150
-// TFLOP/s.  Two workgroups on a CU (bf16) hide one's loads and epilogue behind the other's
-// products.
+// Forward.  589,824 x 128 x 128 bf16 with residual: 87 us, 5.2 TB/s; 32,768 x 1024 x 512: 45 to 54
+// us on different cards, 640 to 750 TFLOP/s, LDS reads and staging beside the products; 16,384 x
+// 1024 x 1024 fp32: 150 TFLOP/s.  Two workgroups on a CU (bf16) hide one's loads and epilogue
+// behind the other's products.
 template <typename T, int R, bool ALIGNED>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void lin_fwd_kernel(LinArgs a) {
   using G = Product<T, T, R, step_k(R, 2 * planes<T>()), true, false, planes<T>(), planes<T>(), DZ_X,
@@ -640,10 +640,10 @@ struct DzSource<T, DZ_MADE> {
   static constexpr int STAGE = DZ_X, P = 3;
 };
 
-// dz = dout act'(z) in fp32, where several column tiles of dx and dW would each form it
-// again from the two tensors (an exponential an element).  Bound by memory and a launch:
-// 1500 x 1536 in 8.5 us; 1500 x 384 x 1536 backward with it 41 us, without 71; 16,384 x 512 x
-// 2048 with it 271, without 412.
+// dz = dout act'(z) in fp32, where several column tiles of dx and dW would each form it again from
+// the two tensors (an exponential an element).  Bound by memory and a launch: 1500 x 1536 in 8.5
+// us; 1500 x 384 x 1536 backward with it 41 us, without 71; 16,384 x 512 x 2048 with it 271,
+// without 412.
 template <typename T>
 __global__ __launch_bounds__(256) void lin_dz_kernel(LinBwdArgs a) {
   const int64_t all = a.m * a.n;
@@ -751,9 +751,8 @@ __global__ __launch_bounds__(256) void lin_bwd_w_kernel(LinBwdArgs a) {
   __shared__ __attribute__((aligned(16))) char lds[DwProduct<T, R, DZ, ALIGNED>::LDS];
   dw_tile<T, R, DZ, ALIGNED>(a, lds, xcd_swizzle(blockIdx.x, gridDim.x));
 }
-// Both in one launch, where dx does not fill the GPU: the first ndx workgroups make dx, the
-// others dW (in tiles of RW).  1500 x 384 x 1536 with GELU: 28 us, where the two take 27 and
-// 20.
+// Both in one launch, where dx does not fill the GPU: the first ndx workgroups make dx, the others
+// dW (in tiles of RW).  1500 x 384 x 1536 with GELU: 28 us, where the two take 27 and 20.
 template <typename T, int RW, int DZ, bool ALIGNED>
 __global__ __launch_bounds__(256) void lin_bwd_both_kernel(LinBwdArgs a, int ndx) {
   constexpr int LX = DxProduct<T, 64, DZ, ALIGNED>::LDS, LW = DwProduct<T, RW, DZ, ALIGNED>::LDS;
@@ -1134,10 +1133,11 @@ hipError_t bwd(const LinBwdArgs& a, hipStream_t s) {
   return (a.dw || a.dbias) && a.splits > 1 ? reduce(a, s) : hipGetLastError();
 }
 
-// Splits of the rows for dW: as many workgroups as the CUs hold at once beside those of dx
-// in the same launch (LDS and registers allow two or three on a CU, one of fp32 in tiles of
-// 128, and one of ragged bf16 in tiles of 128 without planes, whose 193 + 64 registers are a
-// few too many for the two that are counted here: its grid runs in two turns), each of at least 128 rows; none, which needs no further sum, for up to 256 rows.
+// Splits of the rows for dW: as many workgroups as the CUs hold at once beside those of dx in the
+// same launch (LDS and registers allow two or three on a CU, one of fp32 in tiles of 128, and one
+// of ragged bf16 in tiles of 128 without planes, whose 193 + 64 registers are a few too many for
+// the two that are counted here: its grid runs in two turns), each of at least 128 rows; none,
+// which needs no further sum, for up to 256 rows.
 template <typename T>
 int dw_splits(int64_t m, int k, int n, int act) {
   const bool ww = wide_w(m, k, n), smooth = act > TRIATTN_ACT_RELU;

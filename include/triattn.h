@@ -340,7 +340,8 @@ typedef enum {
   TRIATTN_ACT_NONE = 0,
   TRIATTN_ACT_RELU = 1,
   TRIATTN_ACT_GELU = 2,
-  TRIATTN_ACT_SILU = 3
+  TRIATTN_ACT_SILU = 3,
+  TRIATTN_ACT_SIGMOID = 4 /* the gated projection only */
 } triattn_act;
 int tri_linear_fwd(int dtype, int64_t m, int64_t k, int64_t n, int act, const void* x,
                    const void* w, const void* bias, const void* residual, void* out, void* z,
@@ -399,6 +400,112 @@ int tri_rel_bias_bwd(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges
                      const int32_t* edges, const int32_t* pos, const int32_t* chain,
                      const void* dout, float* dtable, void* workspace, size_t workspace_bytes,
                      void* stream);
+
+/* Attention of queries to keys and values of another length, with an additive pair bias
+ * and a key mask or without.  For every sample b, query i and head h, with kh = h / (heads /
+ * key_heads) the key head that head h reads:
+ *   s_j = scale * <Q[b][i][h], K[b][j][kh]> + bias[(b)][i][j][h],   j valid iff mask[b][j],
+ *   out[b][i][h] = sum_j softmax(s)_j V[b][j][kh].
+ * (One query a sample with key_heads = 1 is global attention; nq = nk with a bias is attention
+ * over the single representation.)
+ *   q, out, dout, dq : [batch][nq][heads][d]         (dtype)
+ *   k, v, dk, dv     : [batch][nk][key_heads][d]     (dtype)
+ *   bias, dbias      : [bias_batch][nq][nk][heads]   (dtype), the layout of the triangle
+ *                      attention's bias; bias_batch is 0 (no bias; bias NULL), 1 (one map for
+ *                      every sample) or batch
+ *   mask             : [batch][nk]                   (uint8, 0 = masked; NULL = all valid)
+ *   stat             : [batch][nq][heads][2]         (fp32): m = max_j s_j and
+ *                      ln sum_j exp(s_j - m) over the valid keys, saved for the backward (their
+ *                      sum is the log-sum-exp; apart, they also tell logits that all carry the
+ *                      type's lowest value); -inf and 0 for a query without a key
+ *   dtype: TRIATTN_F32 (fp32 throughout) or TRIATTN_BF16 (fp32 sums and statistics; the
+ *          weights P and their gradients dS rounded to bf16 for the second products).
+ *   d a multiple of 8, at most 128 (TRIATTN_ERR_UNSUPPORTED else); heads a multiple of
+ *   key_heads, at most 256 (TRIATTN_ERR_UNSUPPORTED above); 1 <= nq, nk <= 2^22;
+ *   1 <= batch <= 2^20; scale finite and positive; with g = heads / key_heads, (nq g + 256) g
+ *   < 2^32, and fewer than 2^24 workgroups and 2^34 elements a tensor of q's or k's shape
+ *   (TRIATTN_ERR_UNSUPPORTED).
+ *   bias entries may be -inf (the key is excluded) or as low as the type goes.  Masked keys
+ *   have no effect whatever they, or their bias entries, hold (NaN and infinities too), and
+ *   zero gradients.  A query without a valid key gets out = 0 and no gradient.  Everything
+ *   else must be finite.
+ *   The mask needs no alignment, stat and the other pointers 16 bytes.  Same workspace, stream
+ *   and error rules as above. */
+int tri_cross_attn_fwd_workspace_bytes(int dtype, int64_t batch, int64_t nq, int64_t nk,
+                                       int64_t heads, int64_t key_heads, int64_t d,
+                                       int64_t bias_batch, size_t* bytes);
+int tri_cross_attn_fwd(int dtype, int64_t batch, int64_t nq, int64_t nk, int64_t heads,
+                       int64_t key_heads, int64_t d, int64_t bias_batch, float scale,
+                       const void* q, const void* k, const void* v, const void* bias,
+                       const uint8_t* mask, void* out, float* stat, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* Backward of the cross attention for L = sum(dout * out): takes the forward's inputs, its out
+ * and stat, and dout; with P the weights, dP = dout V^T and D = sum_j P dP,
+ *   dS = P (dP - D),  dq = scale dS K,  dk = scale dS^T Q,  dv = P^T dout,  dbias = dS,
+ * dk and dv summed over the heads that share a key head and dbias over the samples that
+ * share a bias, in a fixed order (bitwise reproducible).  dbias may be NULL (not wanted).  The
+ * workspace holds dS in fp32 where there is a bias (4 batch nq nk heads bytes).  Same rules as
+ * the forward. */
+int tri_cross_attn_bwd_workspace_bytes(int dtype, int64_t batch, int64_t nq, int64_t nk,
+                                       int64_t heads, int64_t key_heads, int64_t d,
+                                       int64_t bias_batch, size_t* bytes);
+int tri_cross_attn_bwd(int dtype, int64_t batch, int64_t nq, int64_t nk, int64_t heads,
+                       int64_t key_heads, int64_t d, int64_t bias_batch, float scale,
+                       const void* q, const void* k, const void* v, const void* bias,
+                       const uint8_t* mask, const void* out, const float* stat,
+                       const void* dout, void* dq, void* dk, void* dv, void* dbias,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gated linear projection (the first half of a gated feed-forward block; the gated projections
+ * of a triangle update):
+ *   [a | b] = x W + bias,   out = act(a) * b,
+ * x [m][k], W [k][2 f] (a = columns 0 .. f-1, b = columns f .. 2 f-1, as W1 of the transition
+ * layer), bias [2 f] (NULL = zeros), out [m][f], all in dtype.  Neither a nor b is written.
+ *   act: a triattn_act, TRIATTN_ACT_SIGMOID too.
+ *   dtype: as tri_linear_fwd.  1 <= m <= 2^31, 1 <= k <= 8192, 1 <= f <= 4096
+ *   (TRIATTN_ERR_UNSUPPORTED above), any parity, and fewer than 2^24 tiles of 64 x 32 outputs
+ *   (TRIATTN_ERR_UNSUPPORTED).  No workspace.  Same stream, pointer and error rules as above. */
+int tri_gated_linear_fwd(int dtype, int64_t m, int64_t k, int64_t f, int act, const void* x,
+                         const void* w, const void* bias, void* out, void* stream);
+
+/* Bytes of device workspace tri_gated_linear_bwd needs for these sizes (8 m f for dz in fp32,
+ * and partial sums). */
+int tri_gated_linear_bwd_workspace_bytes(int dtype, int64_t m, int64_t k, int64_t f,
+                                         size_t* bytes);
+
+/* Backward of the gated projection for L = sum(dout * out): takes the forward's x, W, bias and
+ * act, and dout [m][f]; forms a and b again.  With
+ *   dz = [dout * b * act'(a) | dout * act(a)]   (24 bits in the products):
+ *   dx = dz W^T [m][k] (dtype),  dw = x^T dz [k][2 f] (fp32),
+ *   dbias = sum over rows of dz [2 f] (fp32),
+ * sums over rows in a fixed order (bitwise reproducible).  dx, dw and dbias may each be NULL
+ * (not wanted), but not all three.  Sizes as the forward's, with fewer than 2^24 tiles of
+ * 64 x 64 of [m][k] and [m][2 f]. */
+int tri_gated_linear_bwd(int dtype, int64_t m, int64_t k, int64_t f, int act, const void* x,
+                         const void* w, const void* bias, const void* dout, void* dx, float* dw,
+                         float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Norm of a list of gradients together, and the list scaled to a largest norm:
+ *   norm = sqrt(sum over the tensors of the sum of their squares)   (one fp32),
+ *   outs[i] = grads[i] * (norm > max_norm ? max_norm / norm : 1)    (rounded once).
+ * count tensors, grads[i] of sizes[i] elements of dtypes[i] (TRIATTN_F32 or TRIATTN_BF16, mixed
+ * as they come), contiguous, 16-byte aligned (a tensor of no elements may be NULL).  dtypes,
+ * sizes, grads and outs are HOST arrays, read during the call.  outs[i] may be grads[i] (then
+ * nothing is written where nothing is scaled); no other overlap.
+ *   The squares are summed in 64 bits in a fixed order (bitwise reproducible).  Elements may
+ * hold anything: NaN and infinities show in norm.  tri_grad_clip takes norm from device memory,
+ * so that it may be the norm over several GPUs; a norm that is not finite scales nothing.
+ *   1 <= count <= 2^20, sizes[i] >= 0, fewer than 2^39 elements in all (TRIATTN_ERR_UNSUPPORTED);
+ * max_norm finite and positive.  norm needs 4-byte alignment.  Same workspace, stream and
+ * error rules as above. */
+int tri_grad_norm_workspace_bytes(int64_t count, const int64_t* sizes, size_t* bytes);
+int tri_grad_norm(int64_t count, const int32_t* dtypes, const int64_t* sizes,
+                  const void* const* grads, float* norm, void* workspace, size_t workspace_bytes,
+                  void* stream);
+int tri_grad_clip(int64_t count, const int32_t* dtypes, const int64_t* sizes,
+                  const void* const* grads, const float* norm, float max_norm,
+                  void* const* outs, void* stream);
 
 /* Static, human-readable name of a status code ("unknown status" otherwise). */
 const char* tri_attn_status_string(int status);

@@ -25,6 +25,7 @@ STARTING, ENDING = 0, 1
 F32, BF16 = 0, 1
 HEAD_DIM = 32
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+ACT_SIGMOID = 4  # the gated projection only
 
 _LIB = None
 _vp, _i64, _f, _int, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_float, ctypes.c_int, ctypes.c_size_t
@@ -110,6 +111,23 @@ def lib():
                      "tri_layer_norm_bwd", "tri_linear_fwd", "tri_linear_bwd_workspace_bytes",
                      "tri_linear_bwd", "tri_rel_bias_fwd", "tri_rel_bias_bwd_workspace_bytes",
                      "tri_rel_bias_bwd"):
+            getattr(L, name).restype = _int
+        L.tri_cross_attn_fwd_workspace_bytes.argtypes = [_int] + [_i64] * 7 + [ctypes.POINTER(_sz)]
+        L.tri_cross_attn_bwd_workspace_bytes.argtypes = L.tri_cross_attn_fwd_workspace_bytes.argtypes
+        L.tri_cross_attn_fwd.argtypes = [_int] + [_i64] * 7 + [_f] + [_vp] * 8 + [_sz, _vp]
+        L.tri_cross_attn_bwd.argtypes = [_int] + [_i64] * 7 + [_f] + [_vp] * 13 + [_sz, _vp]
+        L.tri_gated_linear_fwd.argtypes = [_int, _i64, _i64, _i64, _int] + [_vp] * 5
+        L.tri_gated_linear_bwd_workspace_bytes.argtypes = [_int, _i64, _i64, _i64,
+                                                           ctypes.POINTER(_sz)]
+        L.tri_gated_linear_bwd.argtypes = [_int, _i64, _i64, _i64, _int] + [_vp] * 8 + [_sz, _vp]
+        # host arrays: ctypes arrays, or the address of an array.array
+        L.tri_grad_norm_workspace_bytes.argtypes = [_i64, _vp, ctypes.POINTER(_sz)]
+        L.tri_grad_norm.argtypes = [_i64] + [_vp] * 5 + [_sz, _vp]
+        L.tri_grad_clip.argtypes = [_i64] + [_vp] * 4 + [_f, _vp, _vp]
+        for name in ("tri_cross_attn_fwd_workspace_bytes", "tri_cross_attn_bwd_workspace_bytes",
+                     "tri_cross_attn_fwd", "tri_cross_attn_bwd", "tri_gated_linear_fwd",
+                     "tri_gated_linear_bwd_workspace_bytes", "tri_gated_linear_bwd",
+                     "tri_grad_norm_workspace_bytes", "tri_grad_norm", "tri_grad_clip"):
             getattr(L, name).restype = _int
         for name in ("tri_transition_fwd_workspace_bytes", "tri_transition_bwd_workspace_bytes",
                      "tri_transition_fwd", "tri_transition_bwd"):
@@ -996,3 +1014,206 @@ def rel_bias_bwd(pos, edges, dout, chain=None, workspace: Optional[torch.Tensor]
     if st != OK:
         raise TriAttnError(st, "tri_rel_bias_bwd")
     return dtable
+
+
+# ---- cross attention, gated linear projection, clipping of gradients --------------------------
+
+def _sized(name, *args) -> int:
+    """What a *_workspace_bytes function of the library says."""
+    n = _sz(0)
+    st = getattr(lib(), name)(*args, ctypes.byref(n))
+    if st != OK:
+        raise TriAttnError(st, name)
+    return n.value
+
+
+def _cross_common(q, k, v, bias, mask):
+    """Checks; returns the sizes as the library takes them, the device, the shapes of
+    the statistics."""
+    for name, t in (("q", q), ("k", k)):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+    if q.dim() not in (3, 4) or k.dim() != q.dim():
+        raise ValueError("q must be [nq, h, d] and k [nk, hk, d], or both with a batch axis")
+    dt = _DTYPES.get(q.dtype)
+    if dt is None:
+        raise ValueError(f"unsupported dtype {q.dtype}")
+    dev, dtype = q.device, q.dtype
+    lead = tuple(q.shape[:-3])
+    nq, h, d = q.shape[-3:]
+    nk, hk = k.shape[-3:-1]
+    _check("q", q, q.shape, dtype, dev)
+    _check("k", k, lead + (nk, hk, d), dtype, dev)
+    _check("v", v, k.shape, dtype, dev)
+    batch, bias_batch = lead[0] if lead else 1, 0
+    if bias is not None:
+        if not isinstance(bias, torch.Tensor):
+            raise TypeError("bias must be a torch.Tensor")
+        shared = bias.dim() == 3
+        _check("bias", bias, (() if shared else lead) + (nq, nk, h), dtype, dev)
+        bias_batch = 1 if shared else batch
+    if mask is not None:
+        _check("mask", mask, lead + (nk,), torch.uint8, dev)
+    return (dt, batch, nq, nk, h, hk, d, bias_batch), dev, lead + (nq, h, 2)
+
+
+def cross_attn_fwd(q, k, v, bias=None, mask=None, scale: Optional[float] = None,
+                   workspace: Optional[torch.Tensor] = None):
+    """Attention of the queries q [nq, h, d] to keys and values k, v [nk, hk, d] of
+    another length, fp32 or bf16 (hk divides h: head i reads key head i // (h //
+    hk)); bias [nq, nk, h] or None, mask [nk] uint8 (0 = masked) or None; scale
+    1/sqrt(d) if None.  With a leading batch axis on q, k, v and mask, a batch,
+    whose bias is [nq, nk, h] for every sample or [b, nq, nk, h].  Returns (out
+    [nq, h, d], stat [nq, h, 2] fp32: the logits' maximum and the log of the sum
+    of exponentials beside it)."""
+    sizes, dev, stat_shape = _cross_common(q, k, v, bias, mask)
+    scale = default_scale(sizes[6]) if scale is None else float(scale)
+    out = torch.empty_like(q)
+    stat = torch.empty(stat_shape, dtype=torch.float32, device=dev)
+    workspace = _workspace(workspace, _sized("tri_cross_attn_fwd_workspace_bytes", *sizes), dev)
+    st = _on(dev, lib().tri_cross_attn_fwd, *sizes, scale, q.data_ptr(), k.data_ptr(),
+             v.data_ptr(), _ptr(bias), _ptr(mask), out.data_ptr(), stat.data_ptr(),
+             workspace.data_ptr(), workspace.numel())
+    if st != OK:
+        raise TriAttnError(st, "tri_cross_attn_fwd")
+    return out, stat
+
+
+def cross_attn_bwd(q, k, v, out, stat, dout, bias=None, mask=None,
+                   scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradients of sum(dout * out) for cross_attn_fwd: out and stat as it returned
+    them.  Returns (dq, dk, dv, dbias) in q's dtype, dbias of bias's shape (summed
+    over the batch if that shares it), None without one."""
+    sizes, dev, stat_shape = _cross_common(q, k, v, bias, mask)
+    _check("out", out, q.shape, q.dtype, dev)
+    _check("stat", stat, stat_shape, torch.float32, dev)
+    _check("dout", dout, q.shape, q.dtype, dev)
+    scale = default_scale(sizes[6]) if scale is None else float(scale)
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    dbias = None if bias is None else torch.empty_like(bias)
+    workspace = _workspace(workspace, _sized("tri_cross_attn_bwd_workspace_bytes", *sizes), dev)
+    st = _on(dev, lib().tri_cross_attn_bwd, *sizes, scale, q.data_ptr(), k.data_ptr(),
+             v.data_ptr(), _ptr(bias), _ptr(mask), out.data_ptr(), stat.data_ptr(),
+             dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(dbias),
+             workspace.data_ptr(), workspace.numel())
+    if st != OK:
+        raise TriAttnError(st, "tri_cross_attn_bwd")
+    return dq, dk, dv, dbias
+
+
+def _gated_common(x, w, bias):
+    dt, dev, m, k = _check_2d("x", x)
+    n = _check_2d("w", w)[3]
+    if n % 2 != 0:
+        raise ValueError(f"w must have an even number of columns (got {n})")
+    _check("w", w, (k, n), x.dtype, dev)
+    if bias is not None:
+        _check("bias", bias, (n,), x.dtype, dev)
+    return dt, dev, m, k, n // 2
+
+
+def gated_linear_fwd(x, w, bias=None, act: int = ACT_SILU):
+    """out = act(a) * b with [a | b] = x @ w + bias: x [m, k], w [k, 2 f], bias [2 f]
+    or None, all fp32 or all bf16; act one of ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU,
+    ACT_SIGMOID.  Returns out [m, f]."""
+    dt, dev, m, k, f = _gated_common(x, w, bias)
+    out = torch.empty((m, f), dtype=x.dtype, device=dev)
+    st = _on(dev, lib().tri_gated_linear_fwd, dt, m, k, f, act, x.data_ptr(), w.data_ptr(),
+             _ptr(bias), out.data_ptr())
+    if st != OK:
+        raise TriAttnError(st, "tri_gated_linear_fwd")
+    return out
+
+
+def gated_linear_bwd(x, w, dout, bias=None, act: int = ACT_SILU,
+                     workspace: Optional[torch.Tensor] = None):
+    """Gradients of sum(dout * out) for gated_linear_fwd, a and b formed again.
+    Returns (dx [m, k] in x's dtype, dw [k, 2 f] fp32, dbias [2 f] fp32)."""
+    dt, dev, m, k, f = _gated_common(x, w, bias)
+    _check("dout", dout, (m, f), x.dtype, dev)
+    dx = torch.empty_like(x)
+    dw = torch.empty((k, 2 * f), dtype=torch.float32, device=dev)
+    dbias = torch.empty(2 * f, dtype=torch.float32, device=dev)
+    workspace = _workspace(workspace, _sized("tri_gated_linear_bwd_workspace_bytes", dt, m, k, f),
+                           dev)
+    st = _on(dev, lib().tri_gated_linear_bwd, dt, m, k, f, act, x.data_ptr(), w.data_ptr(),
+             _ptr(bias), dout.data_ptr(), dx.data_ptr(), dw.data_ptr(), dbias.data_ptr(),
+             workspace.data_ptr(), workspace.numel())
+    if st != OK:
+        raise TriAttnError(st, "tri_gated_linear_bwd")
+    return dx, dw, dbias
+
+
+class GradList:
+    """A list of gradients (fp32 and bf16 tensors of one GPU, of any shapes, contiguous),
+    checked once, for programs that clip the same ones step after step.  A call
+    looks up the tensors' addresses anew."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        if not self.tensors:
+            raise ValueError("at least one tensor is needed")
+        if not isinstance(self.tensors[0], torch.Tensor):
+            raise TypeError("tensors[0] must be a torch.Tensor")
+        self.device = self.tensors[0].device
+        for i, t in enumerate(self.tensors):
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"tensors[{i}] must be a torch.Tensor")
+            if t.dtype not in _DTYPES:
+                raise ValueError(f"tensors[{i}]: unsupported dtype {t.dtype}")
+            _check(f"tensors[{i}]", t, t.shape, t.dtype, self.device)
+        self.count = len(self.tensors)
+        self.shapes = [t.shape for t in self.tensors]
+        self.dtypes = array.array("i", [_DTYPES[t.dtype] for t in self.tensors])
+        self.sizes = array.array("q", [t.numel() for t in self.tensors])
+        self.workspace_bytes = _sized("tri_grad_norm_workspace_bytes", self.count,
+                                      self.sizes.buffer_info()[0])
+
+    def addresses(self):
+        """The tensors' addresses now; ValueError if one is not what was checked."""
+        for t, shape in zip(self.tensors, self.shapes):
+            if t.shape != shape or not t.is_contiguous():
+                raise ValueError(f"a tensor of the list has changed (was {tuple(shape)})")
+        return array.array("Q", [t.data_ptr() for t in self.tensors])
+
+
+def _grad_list(grads):
+    return grads if isinstance(grads, GradList) else GradList(grads)
+
+
+def grad_norm(grads, workspace: Optional[torch.Tensor] = None):
+    """The 2-norm of all gradients together (a GradList or tensors), summed in 64
+    bits.  Returns an fp32 tensor of no axes; nothing waits for the GPU."""
+    g = _grad_list(grads)
+    norm = torch.empty((), dtype=torch.float32, device=g.device)
+    workspace = _workspace(workspace, g.workspace_bytes, g.device)
+    at = g.addresses()
+    st = _on(g.device, lib().tri_grad_norm, g.count, g.dtypes.buffer_info()[0],
+             g.sizes.buffer_info()[0], at.buffer_info()[0], norm.data_ptr(),
+             workspace.data_ptr(), workspace.numel())
+    if st != OK:
+        raise TriAttnError(st, "tri_grad_norm")
+    return norm
+
+
+def grad_clip(grads, norm, max_norm: float, out=None):
+    """Scales the gradients (a GradList or tensors) by max_norm / norm where norm, as
+    grad_norm gives it, is above max_norm: into `out` (likewise, of the same
+    shapes and dtypes; the gradients themselves or no memory of theirs), in place
+    if None.  A norm that is not finite scales nothing.  Returns out's tensors."""
+    g = _grad_list(grads)
+    o = g if out is None else _grad_list(out)
+    if o is not g and (o.device != g.device or o.shapes != g.shapes or o.dtypes != g.dtypes):
+        raise ValueError("out must hold tensors of the gradients' shapes, dtypes and device")
+    _check("norm", norm, norm.shape if isinstance(norm, torch.Tensor) else (), torch.float32,
+           g.device)
+    if norm.numel() != 1:
+        raise ValueError("norm must have one element")
+    at = g.addresses()
+    to = at if o is g else o.addresses()
+    st = _on(g.device, lib().tri_grad_clip, g.count, g.dtypes.buffer_info()[0],
+             g.sizes.buffer_info()[0], at.buffer_info()[0], norm.data_ptr(), float(max_norm),
+             to.buffer_info()[0])
+    if st != OK:
+        raise TriAttnError(st, "tri_grad_clip")
+    return o.tensors

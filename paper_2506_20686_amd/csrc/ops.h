@@ -67,6 +67,46 @@ LinBwdPlan lin_bwd_plan(int dtype, int64_t m, int k, int n, int act);
 hipError_t launch_lin_fwd(int dtype, const LinArgs& a, hipStream_t s);
 hipError_t launch_lin_bwd(int dtype, const LinBwdArgs& a, hipStream_t s);
 
+// The products of a backward whose dz [m][n] is made already (a.dz; act, z and dout unused).
+LinBwdPlan lin_made_plan(int dtype, int64_t m, int k, int n);
+hipError_t launch_lin_made(int dtype, const LinBwdArgs& a, hipStream_t s);
+
+// ---- gated linear projection (glu.hip) -------------------------------------------------------
+constexpr int GLU_MAX_F = 4096;
+
+struct GluArgs {
+  int64_t m;
+  int k, f;
+  int act;                      // triattn_act
+  const void *x, *w, *bias;     // x [m][k], w [k][2 f], bias [2 f] or null
+  void* out;                    // [m][f]
+  const void* dout;             // backward
+  float* dz;                    // backward, workspace: [m][2 f]
+};
+hipError_t launch_glu_fwd(int dtype, const GluArgs& a, hipStream_t s);
+hipError_t launch_glu_dz(int dtype, const GluArgs& a, hipStream_t s);
+
+// ---- norm and clipping of gradients (grad.hip) ------------------------------------------------
+// Tensors of a launch: their addresses and sizes travel in its arguments.
+constexpr int GRAD_MAX = 96;
+
+struct GradArgs {
+  int count;
+  const void* src[GRAD_MAX];
+  void* dst[GRAD_MAX];
+  int64_t size[GRAD_MAX];
+  int first[GRAD_MAX + 1];      // first workgroup of each
+  uint8_t dtype[GRAD_MAX];
+  double* part;                 // workspace: a sum of squares a workgroup
+  int wg0;                      // workgroups of earlier launches
+  const float* norm;
+  float limit;
+};
+constexpr int64_t GRAD_SPAN = 1 << 15;  // elements of a workgroup
+hipError_t launch_grad_squares(const GradArgs& a, hipStream_t s);
+hipError_t launch_grad_root(const double* part, int64_t count, float* norm, hipStream_t s);
+hipError_t launch_grad_scale(const GradArgs& a, hipStream_t s);
+
 // ---- relative position bias (rel.hip) -------------------------------------------------------
 constexpr int REL_MAX_EDGES = 255;
 constexpr int REL_MAX_H = 256;
@@ -96,5 +136,43 @@ struct RelArgs {
 size_t rel_bwd_ws(int64_t batch, int n, int h, int rows);  // bytes of workspace
 hipError_t launch_rel_fwd(int dtype, const RelArgs& a, hipStream_t s);
 hipError_t launch_rel_bwd(int dtype, const RelArgs& a, hipStream_t s);
+
+// ---- cross attention (xat_fwd.hip, xat_bwd.hip) ----------------------------------------------
+struct XatArgs {
+  int64_t batch;
+  int nq, nk, h, hk, d;
+  int group;                  // heads that share a key head: h / hk
+  uint32_t inv_group;         // 2^32 / group rounded up
+  float scale;
+  const void *q, *k, *v;      // [batch][nq][h][d], [batch][nk][hk][d]
+  const void* bias;           // [nq][nk][h] or [batch][nq][nk][h], or null
+  int64_t bias_batch;         // 1 or batch
+  const uint8_t* mask;        // [batch][nk] or null
+  void* out;                  // [batch][nq][h][d]
+  float* stat;                // [batch][nq][h][2]
+  const void* dout;           // backward
+  void *dq, *dk, *dv, *dbias;
+  // workspace
+  void* planes;               // bias, [bias_batch][hk][nq * group][nkp] (dtype)
+  int nkp;                    // nk rounded up to whole tiles
+  int splits, splits_q;       // of the keys (forward, dq), of the rows (dk, dv)
+  float* part;                // partial results of the splits of the keys
+  float* part_q;              // and of the rows
+  float* dsum;                // [batch][nq][h]
+  int* single;                // [batch]: whether it has one valid key at most
+  float* dplanes;             // dbias of every sample, [batch][hk][nq * group][nkp]
+};
+
+struct XatPlan {
+  int nkp, splits, splits_q;
+  size_t planes, part, part_q, dsum, single, dplanes;  // bytes of workspace, 0 for none
+};
+XatPlan xat_fwd_plan(int dtype, const XatArgs& a);
+XatPlan xat_bwd_plan(int dtype, const XatArgs& a);
+hipError_t launch_xat_fwd(int dtype, const XatArgs& a, hipStream_t s);
+hipError_t launch_xat_bwd(int dtype, const XatArgs& a, hipStream_t s);
+// Bias to planes, one row of a plane after the other (xat_bias.hip).
+hipError_t launch_xat_planes(int dtype, const XatArgs& a, hipStream_t s);
+hipError_t launch_xat_dbias(int dtype, const XatArgs& a, hipStream_t s);
 
 }  // namespace triattn

@@ -45,6 +45,16 @@ enum KernelId {
   K_REL_BWD,
   K_REL_REDUCE,
   K_LIN_BWD_BOTH,
+  K_XAT_PLANES,
+  K_XAT_FWD,
+  K_XAT_JOIN,
+  K_XAT_DQ,
+  K_XAT_DKV,
+  K_XAT_DBIAS,
+  K_GLU_FWD,
+  K_GLU_DZ,
+  K_GRAD_NORM,
+  K_GRAD_CLIP,
   K_COUNT
 };
 

@@ -22,7 +22,10 @@ const char* const kNames[K_COUNT] = {"prep_bias",   "prep_kbits", "fwd",        
                                      "pad16",       "ln_fwd",     "ln_bwd",     "ln_reduce",
                                      "lin_fwd",     "lin_bwd_dx", "lin_bwd_w",  "lin_reduce", "lin_dz",
                                      "lin_narrow",
-                                     "rel_fwd",     "rel_bwd",    "rel_reduce", "lin_bwd_both"};
+                                     "rel_fwd",     "rel_bwd",    "rel_reduce", "lin_bwd_both",
+                                     "xat_planes",  "xat_fwd",    "xat_join",   "xat_dq",
+                                     "xat_dkv",     "xat_dbias",  "glu_fwd",    "glu_dz",
+                                     "grad_norm",   "grad_clip"};
 
 struct Pending {
   int id;

@@ -1,0 +1,310 @@
+// Cross attention: device pieces shared by its forward and backward kernels.
+//
+// For every sample and key head, the rows of the problem are the (query, head) pairs whose
+// heads read that key head: row r = query r / group, head hk * group + r % group.  So the
+// heads that share keys share the key tiles too, and the sums over them that dK and dV need
+// are sums over rows.
+//
+// Channels are padded to DP = 32, 64 or 128 in LDS and registers with zeros (exact: they add
+// nothing); memory is read and written as it is.
+#pragma once
+
+#include "dma.h"
+#include "ops.h"
+
+namespace triattn {
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// Eight consecutive elements as they lie in memory.
+template <typename T>
+struct Chunk {
+  static constexpr int N = (int)sizeof(T) / 2;  // 16-byte words
+  u32x4 v[N];
+};
+
+// A tile of rows x DP channels in LDS, read along rows (a fragment holds channels of one row
+// a lane) and across them (channels of 4 or 8 rows a lane).
+//
+// bf16: 16-byte chunks of a line permuted by XOR with a value s of the line's low bits (l0 ..
+// l3).  Both reads are free of bank conflicts whether the LDS serves 128 or 256 bytes a
+// cycle: s differs between any 8 consecutive lines that share banks, and between any 16; and
+// lines of a transposing read (4 lines x 2 or 4 chunks) that share banks differ in s's high
+// bits.  fp32: lines of DP + 4 floats, so that 8 consecutive lines start 4 banks apart; the
+// reads across take one float a lane, 32 lanes of a line.
+template <typename T, int DP>
+struct XTile;
+
+template <int DP>
+struct XTile<bf16, DP> {
+  static constexpr int LINE = DP * 2;
+  static constexpr int N = DP / 16;  // fragments of a row
+  using Row = bf16x8[N];
+  __device__ static inline int at(int line, int c) {
+    int s;
+    if constexpr (DP == 32) {
+      s = swz(line);
+    } else if constexpr (DP == 64) {
+      s = ((((line >> 1) & 1) << 2) | ((line & 1) << 1) | ((line >> 2) & 1)) ^
+          (((line >> 3) & 1) << 1);
+    } else {
+      const int e = line & 3;
+      s = ((e ^ (e << 1)) << 1) ^ ((line >> 2) & 3);
+    }
+    return line * LINE + 16 * (c ^ s);
+  }
+  __device__ static inline void put(char* t, int line, int c, const Chunk<bf16>& x) {
+    *(u32x4*)(t + at(line, c)) = x.v[0];
+  }
+  // sum over the channels of (line r0 + accumulator row) times (the row in `b`)
+  __device__ static inline f32x16 dot(const char* t, int r0, const Row& b, f32x16 acc) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bf16x8 a = *(const bf16x8*)(t + at(r0 + (lane & 31), 2 * i + (lane >> 5)));
+      acc = Mma<bf16>::mma(a, b[i], acc);
+    }
+    return acc;
+  }
+  // The 8 indices of a fragment of channels 32 n + lane % 32, lines r0 + 16 i + 4 g .. and
+  // r0 + 16 i + 8 + 4 g ..: the order of an accumulator fed back (acc_frags).
+  __device__ static inline bf16x8 across(const char* t, int r0, int n) {
+    const int lane = threadIdx.x & 63, i = lane & 15;
+    const int line = r0 + (i >> 2) + 4 * (lane >> 5), ch = 32 * n + (lane & 16) + 4 * (i & 3);
+    typedef TRIATTN_LDS s16x4* lds4;
+    const char* a = t + at(line, ch >> 3) + (ch & 4) * 2;
+    const char* b = t + at(line + 8, ch >> 3) + (ch & 4) * 2;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(uintptr_t)lds_addr(a));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(uintptr_t)lds_addr(b));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+  // out[n] += (lines r0 .. r0 + 31)^T p, contraction over the lines
+  using Frag = bf16x8[2];
+  __device__ static inline void add(const char* t, int r0, const Frag& p, f32x16 (&out)[DP / 32]) {
+#pragma unroll
+    for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) out[n] = Mma<bf16>::mma(across(t, r0 + 16 * i, n), p[i], out[n]);
+  }
+  // two products with the same lines
+  __device__ static inline void add2(const char* t, int r0, const Frag& p, f32x16 (&out)[DP / 32],
+                                     const Frag& p2, f32x16 (&out2)[DP / 32]) {
+#pragma unroll
+    for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const bf16x8 a = across(t, r0 + 16 * i, n);
+        out[n] = Mma<bf16>::mma(a, p[i], out[n]);
+        out2[n] = Mma<bf16>::mma(a, p2[i], out2[n]);
+      }
+  }
+  // the row's channels in registers; `p` its first, d a multiple of 8; zeros if !real
+  __device__ static inline void row(const bf16* p, int d, bool real, Row& r) {
+    const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      r[i] = bf16x8{};
+      if (real && 16 * i + 8 * g < d) r[i] = *(const bf16x8*)(p + 16 * i + 8 * g);
+    }
+  }
+  __device__ static inline float dot_regs(const Row& a, const Row& b) {  // this half's channels
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf((float)a[i][e], (float)b[i][e], s);
+    return s;
+  }
+};
+
+template <int DP>
+struct XTile<float, DP> {
+  static constexpr int LINE = (DP + 4) * 4;
+  static constexpr int N = DP / 2;
+  using Row = float[N];
+  __device__ static inline void put(char* t, int line, int c, const Chunk<float>& x) {
+    u32x4* p = (u32x4*)(t + line * LINE + 32 * c);
+    p[0] = x.v[0];
+    p[1] = x.v[1];
+  }
+  __device__ static inline f32x16 dot(const char* t, int r0, const Row& b, f32x16 acc) {
+    const int lane = threadIdx.x & 63;
+    const char* p = t + (r0 + (lane & 31)) * LINE + (lane >> 5) * N * 4;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const f32x4 a = *(const f32x4*)(p + 16 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc = Mma<float>::mma(a[e], b[4 * i + e], acc);
+    }
+    return acc;
+  }
+  using Frag = float[16];
+  __device__ static inline float across(const char* t, int r0, int v, int n) {
+    const int lane = threadIdx.x & 63;
+    return *(const float*)(t + (r0 + acc_row(v, lane >> 5)) * LINE + (32 * n + (lane & 31)) * 4);
+  }
+  __device__ static inline void add(const char* t, int r0, const Frag& p, f32x16 (&out)[DP / 32]) {
+#pragma unroll
+    for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) out[n] = Mma<float>::mma(across(t, r0, v, n), p[v], out[n]);
+  }
+  __device__ static inline void add2(const char* t, int r0, const Frag& p, f32x16 (&out)[DP / 32],
+                                     const Frag& p2, f32x16 (&out2)[DP / 32]) {
+#pragma unroll
+    for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const float a = across(t, r0, v, n);
+        out[n] = Mma<float>::mma(a, p[v], out[n]);
+        out2[n] = Mma<float>::mma(a, p2[v], out2[n]);
+      }
+  }
+  __device__ static inline void row(const float* p, int d, bool real, Row& r) {
+    const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      f32x4 x{};
+      if (real && N * g + 4 * i < d) x = *(const f32x4*)(p + N * g + 4 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[4 * i + e] = x[e];
+    }
+  }
+  __device__ static inline float dot_regs(const Row& a, const Row& b) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) s = fmaf(a[i], b[i], s);
+    return s;
+  }
+};
+
+// Quotient and remainder by the number of heads that share a key head; inv = 2^32 / group
+// rounded up, exact for r * group < 2^32.
+__device__ inline int row_query(const XatArgs& a, int r) {
+  return a.group == 1 ? r : (int)(((uint64_t)(uint32_t)r * a.inv_group) >> 32);
+}
+// First element of row r of sample b, key head kh in a tensor [batch][nq][h][c].
+__device__ inline int64_t row_at(const XatArgs& a, int64_t b, int kh, int r, int c) {
+  const int q = row_query(a, r);
+  return ((b * a.nq + q) * a.h + kh * a.group + (r - q * a.group)) * c;
+}
+
+// Chunks of `LINES` lines of DP channels, by the threads of NW waves: line() and col() of a
+// thread's chunk u.
+template <int DP, int LINES, int NW>
+struct Share {
+  static constexpr int PER = DP / 8, C = LINES * PER / (64 * NW);
+  static_assert(LINES * PER % (64 * NW) == 0, "whole chunks");
+  __device__ static inline int line(int u) { return ((int)threadIdx.x + 64 * NW * u) / PER; }
+  __device__ static inline int col(int u) { return ((int)threadIdx.x + 64 * NW * u) % PER; }
+};
+
+// Chunk at byte `off` of a resource (zeros past its end).
+template <typename T>
+__device__ inline Chunk<T> load_chunk(rsrc_t rs, uint32_t off) {
+  Chunk<T> x;
+#pragma unroll
+  for (int i = 0; i < Chunk<T>::N; ++i)
+    x.v[i] = __builtin_bit_cast(
+        u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(off + 16 * i), 0, 0));
+  return x;
+}
+constexpr uint32_t NOWHERE = 0x80000000u;  // past the end of any resource here
+
+// Staging of tiles of BK keys, keys and values: through registers, into LDS with the rows of
+// masked keys zeroed, so that nothing in them reaches a product.
+template <typename T, int DP, int BK, int NW>
+struct KvStage {
+  using S = Share<DP, BK, NW>;
+  using L = XTile<T, DP>;
+  static constexpr int BYTES = BK * L::LINE;
+  Chunk<T> k[S::C], v[S::C];
+  int valid;  // of key k0 + lane
+  __device__ inline void load(const XatArgs& a, int64_t b, int kh, int k0) {
+    const int rows = a.nk - k0 < BK ? a.nk - k0 : BK, stride = a.hk * a.d;
+    const uint32_t n = rows > 0 ? (uint32_t)((rows - 1) * stride + a.d) * sizeof(T) : 0u;
+    const int64_t at = ((b * a.nk + k0) * a.hk + kh) * a.d;
+    const rsrc_t rk = buf_rsrc_n((const T*)a.k + at, n), rv = buf_rsrc_n((const T*)a.v + at, n);
+#pragma unroll
+    for (int u = 0; u < S::C; ++u) {
+      const int line = S::line(u), c = 8 * S::col(u);
+      const uint32_t off =
+          c < a.d && line < rows ? (uint32_t)(line * stride + c) * sizeof(T) : NOWHERE;
+      k[u] = load_chunk<T>(rk, off);
+      v[u] = load_chunk<T>(rv, off);
+    }
+    const int lane = threadIdx.x & 63;
+    valid = lane < rows && lane < BK;
+    if (a.mask && valid) valid = a.mask[b * a.nk + k0 + lane];
+  }
+  // Which of the tile's keys are valid.
+  __device__ inline uint64_t bits() const { return __ballot(valid != 0); }
+  __device__ inline void store(char* tk, char* tv, uint64_t ok) const {
+    constexpr uint64_t ALL = BK == 64 ? ~0ull : (1ull << BK) - 1;
+#pragma unroll
+    for (int u = 0; u < S::C; ++u) {
+      const int line = S::line(u), c = S::col(u);
+      Chunk<T> x = k[u], y = v[u];
+      if (ok != ALL && !((ok >> line) & 1)) x = Chunk<T>{}, y = Chunk<T>{};
+      L::put(tk, line, c, x);
+      L::put(tv, line, c, y);
+    }
+  }
+};
+
+// Keys of a tile: 64 for workgroups of four waves where the two buffers leave room for several
+// on a CU, else 32.
+template <typename T, int DP, int NW>
+constexpr int xat_keys() {
+  return NW == 4 && (sizeof(T) == 2 || DP == 32) ? 64 : 32;
+}
+
+// Waves of a workgroup that share staged tiles: 32 rows each.  Few rows take a wave to
+// themselves, which needs no barrier.
+inline int xat_row_waves(const XatArgs& a) { return (int64_t)a.nq * a.group <= 32 ? 1 : 4; }
+inline int xat_key_waves(const XatArgs& a) { return a.nk <= 32 ? 1 : 4; }
+inline int xat_row_tiles(const XatArgs& a, int nw) {
+  return (int)(((int64_t)a.nq * a.group + 32 * nw - 1) / (32 * nw));
+}
+inline int xat_key_tiles(const XatArgs& a, int nw) { return (a.nk + 32 * nw - 1) / (32 * nw); }
+
+// Splits of a long loop: so that the workgroups (of nw waves) fill the GPU, each of at least
+// `least` steps.
+inline int xat_splits(int64_t wgs, int nw, int64_t steps, int64_t least) {
+  const int64_t want = nw == 1 ? 2048 : 512;
+  int64_t s = (want + wgs - 1) / wgs;
+  if (wgs >= want) s = 1;
+  if (s > steps / least) s = steps / least;
+  return s < 1 ? 1 : (s > 64 ? 64 : (int)s);
+}
+inline int xat_key_splits(const XatArgs& a) {
+  const int nw = xat_row_waves(a);
+  return xat_splits(a.batch * a.hk * xat_row_tiles(a, nw), nw, (a.nk + 63) / 64, 4);
+}
+inline int xat_row_splits(const XatArgs& a) {
+  const int nw = xat_key_waves(a);
+  return xat_splits(a.batch * a.hk * xat_key_tiles(a, nw), nw,
+                    ((int64_t)a.nq * a.group + 63) / 64, 4);
+}
+
+// Four consecutive keys' bias of a lane's row.
+__device__ inline f32x4 bias4(const bf16* p) { return load4(p); }
+__device__ inline f32x4 bias4(const float* p) { return load4(p); }
+
+// Work items are numbered so that the ones that read the same keys (or rows) are neighbours.
+struct Item {
+  int64_t b;
+  int kh, tile, split;
+};
+__device__ inline Item item_of(const XatArgs& a, int wg, int tiles, int splits) {
+  Item t;
+  t.split = wg % splits;
+  wg /= splits;
+  t.tile = wg % tiles;
+  wg /= tiles;
+  t.kh = wg % a.hk;
+  t.b = wg / a.hk;
+  return t;
+}
+
+}  // namespace triattn

@@ -1,0 +1,421 @@
+// Cross attention, backward.  With P and dP = dO V^T recomputed from the saved maximum and sum
+// of each row:
+//   D = sum over keys of P dP,  dS = P (dP - D),
+//   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO,  dbias = dS.
+//
+// Two passes, neither of which writes P or dS but for dbias:
+//   dq   a wave owns 32 rows and walks the keys, as the forward does;
+//   dkv  a wave owns 32 keys and walks the rows (of all heads that share them).
+//
+// D: the row's sum of P dP equals dO . out, but out is rounded.  Taken from it as it is, D
+// would leave sum(dS) off zero by that rounding: where one key takes all the weight, that is all
+// there is of dS.  So the first pass takes d = dO . out only as a shift, dS' = P (dP - d), sums
+// dS' in fp32 (e), and ends with
+//   dQ = scale (dS' K - e P K),  D = d + e,
+// one more product for an exact D, where a pass of its own over the keys would take two and the
+// exponentials again.  A sample with one valid key has P = 1 and dS = 0 whatever its logits, which
+// no rounded P and D give exactly: its dS are set to 0.
+#include "timing.h"
+#include "triattn.h"
+#include "xat.h"
+
+namespace triattn {
+namespace {
+
+// P of logits s (accumulator values): exp2(s c + add), or with a bias exp2((s - m) c + add).
+template <bool BIAS>
+__device__ inline float weight(float s, float c, float m, float add) {
+  return __builtin_amdgcn_exp2f(BIAS ? fmaf(s - m, c, add) : fmaf(s, c, add));
+}
+
+// A row's statistics as weight() takes them: its maximum (with a bias), and the addend, -inf
+// for a row without keys (P = 0).
+template <bool BIAS>
+__device__ inline void row_stat(const XatArgs& a, int64_t R, float& m, float& add) {
+  const f32x2 x = *(const f32x2*)(a.stat + 2 * R);
+  const bool none = x[0] == neg_inf();
+  m = none ? 0.f : x[0];
+  add = none ? neg_inf() : -LOG2E * (BIAS ? x[1] : x[0] + x[1]);
+}
+
+// Partial results of a split of the keys: dS' K and P K of every row, then e.
+__device__ inline float* part_ab(const XatArgs& a, int split, int64_t R, int which) {
+  const int64_t all = a.batch * a.nq * a.h;
+  return a.part + (((int64_t)split * all + R) * 2 + which) * a.d;
+}
+__device__ inline float* part_e(const XatArgs& a, int split, int64_t R) {
+  const int64_t all = a.batch * a.nq * a.h;
+  return a.part + (int64_t)a.splits * all * 2 * a.d + (int64_t)split * all + R;
+}
+
+template <typename T, int DP, int NW, bool BIAS>
+__global__ __launch_bounds__(64 * NW) void xat_dq_kernel(XatArgs a, int tiles) {
+  constexpr int BK = xat_keys<T, DP, NW>(), J = BK / 32;
+  constexpr uint64_t ALL = BK == 64 ? ~0ull : (1ull << BK) - 1;
+  using St = KvStage<T, DP, BK, NW>;
+  using L = XTile<T, DP>;
+  __shared__ __attribute__((aligned(16))) char lds[2 * 2 * St::BYTES];
+  const Item w = item_of(a, xcd_swizzle(blockIdx.x, gridDim.x), tiles, a.splits);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
+  const int rows = a.nq * a.group, first = (w.tile * NW + wave) * 32;
+  const int r = first + (lane & 31), in = r < rows ? r : rows - 1;
+  const int64_t R = row_at(a, w.b, w.kh, in, 1);
+  typename L::Row q, dy;
+  L::row((const T*)a.q + R * a.d, a.d, r < rows, q);
+  L::row((const T*)a.dout + R * a.d, a.d, r < rows, dy);
+  float shift;
+  {
+    typename L::Row o;
+    L::row((const T*)a.out + R * a.d, a.d, r < rows, o);
+    shift = wave_xor32_sum(L::dot_regs(dy, o));
+  }
+  float m, add;
+  row_stat<BIAS>(a, R, m, add);
+  const T* bias = nullptr;
+  if (BIAS)
+    bias = (const T*)a.planes +
+           (((a.bias_batch == 1 ? 0 : w.b) * a.hk + w.kh) * rows + in) * a.nkp + 4 * g;
+  const int nt = (a.nk + BK - 1) / BK;
+  const int t0 = (int)((int64_t)nt * w.split / a.splits);
+  const int t1 = (int)((int64_t)nt * (w.split + 1) / a.splits);
+  const float c = BIAS ? LOG2E : a.scale * LOG2E;
+  f32x16 sk[DP / 32] = {}, pk[DP / 32] = {};
+  float e = 0.f;
+  int valid = 0;  // keys
+  St st;
+  st.load(a, w.b, w.kh, t0 * BK);
+  for (int t = t0; t < t1; ++t) {
+    char* tk = lds + (t & 1) * 2 * St::BYTES;
+    char* tv = tk + St::BYTES;
+    const uint64_t ok = st.bits();
+    st.store(tk, tv, ok);
+    valid += __popcll(ok);
+    st.load(a, w.b, w.kh, (t + 1) * BK);
+    __syncthreads();
+    if (ok == 0 || first >= rows) continue;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      f32x16 s = L::dot(tk, 32 * j, q, f32x16{});
+      f32x16 dp = L::dot(tv, 32 * j, dy, f32x16{});
+      if constexpr (BIAS) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 x = bias4(bias + (int64_t)t * BK + 32 * j + 8 * i);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) s[4 * i + u] = fmaf(s[4 * i + u], a.scale, x[u]);
+        }
+      }
+      if (ok != ALL) mask_rows(s, (uint32_t)(ok >> (32 * j)), g);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        s[v] = weight<BIAS>(s[v], c, m, add);
+        dp[v] = s[v] * (dp[v] - shift);
+      }
+      typename L::Frag fp, fs;
+      acc_frags(s, fp);
+      acc_frags(dp, fs);
+      e += sum16(dp);
+      L::add2(tk, 32 * j, fs, sk, fp, pk);
+    }
+  }
+  const bool single = a.splits == 1 && valid <= 1;
+  if (w.tile == 0 && w.kh == 0 && w.split == 0 && threadIdx.x == 0) a.single[w.b] = single;
+  if (r >= rows) return;
+  const float sum = wave_xor32_sum(e);
+  if (a.splits > 1) {
+    float *ps = part_ab(a, w.split, R, 0), *pp = part_ab(a, w.split, R, 1);
+#pragma unroll
+    for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int ch = 32 * n + 8 * i + 4 * g;
+        if (ch < a.d) {
+          store4(ps + ch, f32x4{sk[n][4 * i], sk[n][4 * i + 1], sk[n][4 * i + 2], sk[n][4 * i + 3]});
+          store4(pp + ch, f32x4{pk[n][4 * i], pk[n][4 * i + 1], pk[n][4 * i + 2], pk[n][4 * i + 3]});
+        }
+      }
+    if (g == 0) {
+      *part_e(a, w.split, R) = sum;
+      if (w.split == 0) a.dsum[R] = shift;
+    }
+    return;
+  }
+  T* dq = (T*)a.dq + R * a.d;
+#pragma unroll
+  for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int ch = 32 * n + 8 * i + 4 * g;
+      f32x4 x;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        x[u] = single ? 0.f : a.scale * fmaf(-sum, pk[n][4 * i + u], sk[n][4 * i + u]);
+      if (ch < a.d) store4(dq + ch, x);
+    }
+  if (g == 0) a.dsum[R] = shift + sum;
+}
+
+// Joins the splits of the keys: four channels of a row a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void xat_dq_join_kernel(XatArgs a) {
+  const int64_t all = a.batch * a.nq * a.h, quads = a.d / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= all * quads) return;
+  const int64_t R = i / quads;
+  const int ch = 4 * (int)(i % quads);
+  f32x4 sk{}, pk{};
+  float e = 0.f;
+  for (int s = 0; s < a.splits; ++s) {
+    sk += *(const f32x4*)(part_ab(a, s, R, 0) + ch);
+    pk += *(const f32x4*)(part_ab(a, s, R, 1) + ch);
+    e += *part_e(a, s, R);
+  }
+  f32x4 x;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) x[u] = a.scale * fmaf(-e, pk[u], sk[u]);
+  store4((T*)a.dq + R * a.d + ch, x);
+  if (ch == 0) a.dsum[R] += e;
+}
+
+// Tiles of BQ rows of q and dout, and the rows' statistics.
+template <typename T, int DP, int BQ, int NW, bool BIAS>
+struct RowStage {
+  using S = Share<DP, BQ, NW>;
+  using L = XTile<T, DP>;
+  static constexpr int TILE = BQ * L::LINE, BYTES = 2 * TILE + 3 * BQ * 4;
+  Chunk<T> q[S::C], dy[S::C];
+  float m, add, d;
+  __device__ inline void load(const XatArgs& a, int64_t b, int kh, int r0) {
+    const int rows = a.nq * a.group, q0 = row_query(a, r0 < rows ? r0 : 0);
+    const int64_t at = ((b * a.nq + q0) * a.h + kh * a.group) * a.d;
+    const uint32_t n = 0x7fffffffu;  // rows are checked here
+    const rsrc_t rq = buf_rsrc_n((const T*)a.q + at, n), rd = buf_rsrc_n((const T*)a.dout + at, n);
+#pragma unroll
+    for (int u = 0; u < S::C; ++u) {
+      const int r = r0 + S::line(u), c = 8 * S::col(u), qi = row_query(a, r);
+      const uint32_t off =
+          r < rows && c < a.d
+              ? (uint32_t)(((qi - q0) * a.h + r - qi * a.group) * a.d + c) * sizeof(T)
+              : NOWHERE;
+      q[u] = load_chunk<T>(rq, off);
+      dy[u] = load_chunk<T>(rd, off);
+    }
+    const int r = r0 + (int)threadIdx.x;
+    m = 0.f, add = neg_inf(), d = 0.f;
+    if ((int)threadIdx.x < BQ && r < rows) {
+      const int64_t R = row_at(a, b, kh, r, 1);
+      row_stat<BIAS>(a, R, m, add);
+      d = a.dsum[R];
+    }
+  }
+  __device__ inline void store(char* t) const {
+#pragma unroll
+    for (int u = 0; u < S::C; ++u) {
+      L::put(t, S::line(u), S::col(u), q[u]);
+      L::put(t + TILE, S::line(u), S::col(u), dy[u]);
+    }
+    if ((int)threadIdx.x < BQ) {
+      float* p = (float*)(t + 2 * TILE) + threadIdx.x;
+      p[0] = m;
+      p[BQ] = add;
+      p[2 * BQ] = d;
+    }
+  }
+};
+
+template <typename T, int DP, int NW, bool BIAS>
+__global__ __launch_bounds__(64 * NW) void xat_dkv_kernel(XatArgs a, int tiles) {
+  constexpr int BQ = xat_keys<T, DP, NW>(), J = BQ / 32;
+  using St = RowStage<T, DP, BQ, NW, BIAS>;
+  using L = XTile<T, DP>;
+  __shared__ __attribute__((aligned(16))) char lds[2 * St::BYTES];
+  const Item w = item_of(a, xcd_swizzle(blockIdx.x, gridDim.x), tiles, a.splits_q);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
+  const int rows = a.nq * a.group, first = (w.tile * NW + wave) * 32, key = first + (lane & 31);
+  const bool valid = key < a.nk && (a.mask == nullptr || a.mask[w.b * a.nk + key] != 0);
+  const int64_t K = (w.b * a.nk + (key < a.nk ? key : a.nk - 1)) * a.hk + w.kh;
+  typename L::Row kf, vf;
+  L::row((const T*)a.k + K * a.d, a.d, valid, kf);
+  L::row((const T*)a.v + K * a.d, a.d, valid, vf);
+  const T* bias = nullptr;
+  float* ds = nullptr;
+  if (BIAS) {
+    bias = (const T*)a.planes + ((a.bias_batch == 1 ? 0 : w.b) * a.hk + w.kh) * rows * a.nkp + key;
+    if (a.dbias) ds = a.dplanes + (w.b * a.hk + w.kh) * rows * a.nkp + key;
+  }
+  const int nt = (rows + BQ - 1) / BQ;
+  const int t0 = (int)((int64_t)nt * w.split / a.splits_q);
+  const int t1 = (int)((int64_t)nt * (w.split + 1) / a.splits_q);
+  const float c = BIAS ? LOG2E : a.scale * LOG2E;
+  f32x16 dv[DP / 32] = {}, dk[DP / 32] = {};
+  const bool single = a.single[w.b] != 0;
+  St st;
+  st.load(a, w.b, w.kh, t0 * BQ);
+  for (int t = t0; t < t1; ++t) {
+    char* tq = lds + (t & 1) * St::BYTES;
+    char* td = tq + St::TILE;
+    const float* stat = (const float*)(tq + 2 * St::TILE);
+    st.store(tq);
+    st.load(a, w.b, w.kh, (t + 1) * BQ);
+    __syncthreads();
+    if (first >= a.nk) continue;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int r0 = t * BQ + 32 * j;
+      if (r0 >= rows) break;
+      float x[16];
+      if constexpr (BIAS) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int r = r0 + acc_row(v, g);
+          x[v] = key < a.nk && r < rows ? (float)bias[(int64_t)r * a.nkp] : 0.f;
+        }
+      }
+      f32x16 s = L::dot(tq, 32 * j, kf, f32x16{});
+      f32x16 dp = L::dot(td, 32 * j, vf, f32x16{});
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int line = 32 * j + 8 * i + 4 * g;
+        f32x4 m{};
+        if (BIAS) m = *(const f32x4*)(stat + line);
+        const f32x4 add = *(const f32x4*)(stat + BQ + line);
+        const f32x4 sum = *(const f32x4*)(stat + 2 * BQ + line);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int v = 4 * i + u;
+          if constexpr (BIAS) s[v] = fmaf(s[v], a.scale, x[v]);
+          s[v] = weight<BIAS>(s[v], c, m[u], add[u]);
+          dp[v] = s[v] * (dp[v] - sum[u]);
+        }
+      }
+      if (single) dp = f32x16{};
+      if (BIAS && ds) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int r = r0 + acc_row(v, g);
+          if (key < a.nk && r < rows) ds[(int64_t)r * a.nkp] = valid ? dp[v] : 0.f;
+        }
+      }
+      typename L::Frag f;
+      acc_frags(s, f);
+      L::add(td, 32 * j, f, dv);
+      acc_frags(dp, f);
+      L::add(tq, 32 * j, f, dk);
+    }
+  }
+  if (key >= a.nk) return;
+  // whatever the column of a masked key holds, its gradients are zeros
+  const int64_t all = a.batch * a.nk * a.hk * a.d;
+  float* part = a.part_q + (int64_t)w.split * 2 * all + K * a.d;
+#pragma unroll
+  for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int ch = 32 * n + 8 * i + 4 * g;
+      f32x4 x{}, y{};
+      if (valid) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = a.scale * dk[n][4 * i + u], y[u] = dv[n][4 * i + u];
+      }
+      if (ch >= a.d) continue;
+      if (a.splits_q > 1) {
+        store4(part + ch, x);
+        store4(part + all + ch, y);
+      } else {
+        store4((T*)a.dk + K * a.d + ch, x);
+        store4((T*)a.dv + K * a.d + ch, y);
+      }
+    }
+}
+
+// Sums of the splits of the rows: four channels of dk and of dv a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void xat_dkv_join_kernel(XatArgs a) {
+  const int64_t all = a.batch * a.nk * a.hk * a.d;
+  const int64_t i = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+  if (i >= all) return;
+  f32x4 x{}, y{};
+  for (int s = 0; s < a.splits_q; ++s) {
+    x += *(const f32x4*)(a.part_q + (int64_t)s * 2 * all + i);
+    y += *(const f32x4*)(a.part_q + (int64_t)s * 2 * all + all + i);
+  }
+  store4((T*)a.dk + i, x);
+  store4((T*)a.dv + i, y);
+}
+
+template <typename T, int DP, int NW>
+void dq_launch(const XatArgs& a, hipStream_t s) {
+  const int tiles = xat_row_tiles(a, NW);
+  const dim3 grid((unsigned)(a.batch * a.hk * tiles * a.splits)), wg(64 * NW);
+  if (a.bias) hipLaunchKernelGGL((xat_dq_kernel<T, DP, NW, true>), grid, wg, 0, s, a, tiles);
+  else hipLaunchKernelGGL((xat_dq_kernel<T, DP, NW, false>), grid, wg, 0, s, a, tiles);
+}
+template <typename T, int DP, int NW>
+void dkv_launch(const XatArgs& a, hipStream_t s) {
+  const int tiles = xat_key_tiles(a, NW);
+  const dim3 grid((unsigned)(a.batch * a.hk * tiles * a.splits_q)), wg(64 * NW);
+  if (a.bias) hipLaunchKernelGGL((xat_dkv_kernel<T, DP, NW, true>), grid, wg, 0, s, a, tiles);
+  else hipLaunchKernelGGL((xat_dkv_kernel<T, DP, NW, false>), grid, wg, 0, s, a, tiles);
+}
+
+template <typename T>
+hipError_t bwd(const XatArgs& a, hipStream_t s) {
+  const int dtype = sizeof(T) == 2 ? TRIATTN_BF16 : TRIATTN_F32;
+  if (a.bias) {
+    const hipError_t e = launch_xat_planes(dtype, a, s);
+    if (e != hipSuccess) return e;
+  }
+  {
+    KernelTimer t(K_XAT_DQ, s);
+    const int nw = xat_row_waves(a);
+    if (a.d <= 32) nw == 1 ? dq_launch<T, 32, 1>(a, s) : dq_launch<T, 32, 4>(a, s);
+    else if (a.d <= 64) nw == 1 ? dq_launch<T, 64, 1>(a, s) : dq_launch<T, 64, 4>(a, s);
+    else nw == 1 ? dq_launch<T, 128, 1>(a, s) : dq_launch<T, 128, 4>(a, s);
+  }
+  if (a.splits > 1) {
+    KernelTimer t(K_XAT_JOIN, s);
+    const int64_t n = a.batch * a.nq * a.h * (a.d / 4);
+    hipLaunchKernelGGL(xat_dq_join_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a);
+  }
+  {
+    KernelTimer t(K_XAT_DKV, s);
+    const int nw = xat_key_waves(a);
+    if (a.d <= 32) nw == 1 ? dkv_launch<T, 32, 1>(a, s) : dkv_launch<T, 32, 4>(a, s);
+    else if (a.d <= 64) nw == 1 ? dkv_launch<T, 64, 1>(a, s) : dkv_launch<T, 64, 4>(a, s);
+    else nw == 1 ? dkv_launch<T, 128, 1>(a, s) : dkv_launch<T, 128, 4>(a, s);
+  }
+  if (a.splits_q > 1) {
+    KernelTimer t(K_XAT_JOIN, s);
+    const int64_t n = a.batch * a.nk * a.hk * (a.d / 4);
+    hipLaunchKernelGGL(xat_dkv_join_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s,
+                       a);
+  }
+  if (a.dbias) return launch_xat_dbias(dtype, a, s);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+XatPlan xat_bwd_plan(int dtype, const XatArgs& a) {
+  XatPlan p{};
+  const int64_t all = a.batch * a.nq * a.h, keys = a.batch * a.nk * a.hk;
+  p.nkp = (a.nk + 63) / 64 * 64;
+  p.splits = xat_key_splits(a);
+  p.splits_q = xat_row_splits(a);
+  const size_t e = dtype == TRIATTN_BF16 ? 2 : 4;
+  if (a.bias_batch) {
+    p.planes = (size_t)a.bias_batch * a.h * a.nq * p.nkp * e;
+    p.dplanes = (size_t)a.batch * a.h * a.nq * p.nkp * sizeof(float);  // unused without dbias
+  }
+  p.dsum = (size_t)all * sizeof(float);
+  p.single = (size_t)a.batch * sizeof(int);
+  if (p.splits > 1) p.part = (size_t)p.splits * all * (2 * a.d + 1) * sizeof(float);
+  if (p.splits_q > 1) p.part_q = (size_t)p.splits_q * keys * 2 * a.d * sizeof(float);
+  return p;
+}
+
+hipError_t launch_xat_bwd(int dtype, const XatArgs& a, hipStream_t s) {
+  return dtype == TRIATTN_BF16 ? bwd<bf16>(a, s) : bwd<float>(a, s);
+}
+
+}  // namespace triattn

@@ -1,0 +1,194 @@
+// Cross attention, forward: out = softmax(scale q k^T + bias over the valid keys) v.
+//
+// One pass over the keys with a running maximum and sum a row.  A wave owns 32 rows (a row a
+// lane, its keys over the accumulator's registers: S^T = K Q^T), so the row's statistics are a
+// lane's own; P^T feeds back as an operand of O^T = V^T P^T.  Tiles of keys and values go
+// through registers into LDS, the next tile's loads in flight while one is multiplied.
+//
+// Logits stay in natural units where there is a bias: a bias of the type's lowest value would
+// overflow in base 2.  P is rounded to bf16 for its product (bf16 tensors): half a step of each
+// weight, as much as the output's own rounding, beside twice the matrix instructions for 16 bits
+// of it.
+#include "timing.h"
+#include "triattn.h"
+#include "xat.h"
+
+namespace triattn {
+namespace {
+
+template <typename T, int DP, int NW, bool BIAS>
+__global__ __launch_bounds__(64 * NW) void xat_fwd_kernel(XatArgs a, int tiles) {
+  constexpr int BK = xat_keys<T, DP, NW>(), J = BK / 32;
+  constexpr uint64_t ALL = BK == 64 ? ~0ull : (1ull << BK) - 1;
+  using St = KvStage<T, DP, BK, NW>;
+  using L = XTile<T, DP>;
+  __shared__ __attribute__((aligned(16))) char lds[2 * 2 * St::BYTES];
+  const Item w = item_of(a, xcd_swizzle(blockIdx.x, gridDim.x), tiles, a.splits);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
+  const int rows = a.nq * a.group, first = (w.tile * NW + wave) * 32;
+  const int r = first + (lane & 31), in = r < rows ? r : rows - 1;
+  typename L::Row q;
+  L::row((const T*)a.q + row_at(a, w.b, w.kh, in, a.d), a.d, r < rows, q);
+  const T* bias = nullptr;
+  if (BIAS)
+    bias = (const T*)a.planes +
+           (((a.bias_batch == 1 ? 0 : w.b) * a.hk + w.kh) * rows + in) * a.nkp + 4 * g;
+  const int nt = (a.nk + BK - 1) / BK;
+  const int t0 = (int)((int64_t)nt * w.split / a.splits);
+  const int t1 = (int)((int64_t)nt * (w.split + 1) / a.splits);
+  const float c = BIAS ? LOG2E : a.scale * LOG2E;
+  float m = neg_inf(), l = 0.f;
+  f32x16 o[DP / 32] = {};
+  St st;
+  st.load(a, w.b, w.kh, t0 * BK);
+  for (int t = t0; t < t1; ++t) {
+    char* tk = lds + (t & 1) * 2 * St::BYTES;
+    char* tv = tk + St::BYTES;
+    const uint64_t ok = st.bits();
+    st.store(tk, tv, ok);
+    st.load(a, w.b, w.kh, (t + 1) * BK);
+    // this buffer was last read two steps ago, before the barrier of the last step
+    __syncthreads();
+    if (ok == 0 || first >= rows) continue;
+    f32x16 s[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      s[j] = L::dot(tk, 32 * j, q, f32x16{});
+      if constexpr (BIAS) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 x = bias4(bias + (int64_t)t * BK + 32 * j + 8 * i);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[j][4 * i + e] = fmaf(s[j][4 * i + e], a.scale, x[e]);
+        }
+      }
+      if (ok != ALL) mask_rows(s[j], (uint32_t)(ok >> (32 * j)), g);
+    }
+    float top = max16(s[0]);
+    if constexpr (J == 2) top = fmaxf(top, max16(s[J - 1]));
+    top = fmaxf(m, wave_xor32_max(top));
+    if (__any(top > m)) {
+      const float f = top > m ? __builtin_amdgcn_exp2f((m - top) * c) : 1.f;
+      l *= f;
+#pragma unroll
+      for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[n][v] *= f;
+      m = top;
+    }
+    const float base = m == neg_inf() ? 0.f : m, shift = -base * c;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        s[j][v] = __builtin_amdgcn_exp2f(BIAS ? (s[j][v] - base) * c : fmaf(s[j][v], c, shift));
+      l += sum16(s[j]);
+      typename L::Frag p;
+      acc_frags(s[j], p);
+      L::add(tv, 32 * j, p, o);
+    }
+  }
+  l = wave_xor32_sum(l);
+  if (r >= rows) return;
+  if (!BIAS) m *= a.scale;  // scale > 0: -inf stays
+  const int64_t R = row_at(a, w.b, w.kh, r, 1);
+  const int64_t all = a.batch * a.nq * a.h;
+  if (a.splits > 1) {
+    float* po = a.part + ((int64_t)w.split * all + R) * a.d;
+    float* pm = a.part + (int64_t)a.splits * all * a.d + ((int64_t)w.split * all + R) * 2;
+#pragma unroll
+    for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int ch = 32 * n + 8 * i + 4 * g;
+        if (ch < a.d) store4(po + ch, f32x4{o[n][4 * i], o[n][4 * i + 1], o[n][4 * i + 2],
+                                            o[n][4 * i + 3]});
+      }
+    if (g == 0) *(f32x2*)pm = f32x2{m, l};
+    return;
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  T* out = (T*)a.out + R * a.d;
+#pragma unroll
+  for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int ch = 32 * n + 8 * i + 4 * g;
+      if (ch < a.d) store4(out + ch, f32x4{o[n][4 * i] * inv, o[n][4 * i + 1] * inv,
+                                           o[n][4 * i + 2] * inv, o[n][4 * i + 3] * inv});
+    }
+  if (g == 0) *(f32x2*)(a.stat + 2 * R) = f32x2{m, l > 0.f ? __logf(l) : 0.f};
+}
+
+// Joins the splits: four channels of a row a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void xat_join_kernel(XatArgs a) {
+  const int64_t all = a.batch * a.nq * a.h, quads = a.d / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= all * quads) return;
+  const int64_t R = i / quads;
+  const int ch = 4 * (int)(i % quads);
+  const float* pm = a.part + (int64_t)a.splits * all * a.d;
+  float m = neg_inf();
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, pm[((int64_t)s * all + R) * 2]);
+  const float base = m == neg_inf() ? 0.f : m;
+  float l = 0.f;
+  f32x4 o{};
+  for (int s = 0; s < a.splits; ++s) {
+    const f32x2 x = *(const f32x2*)(pm + ((int64_t)s * all + R) * 2);
+    const float f = __builtin_amdgcn_exp2f((x[0] - base) * LOG2E);
+    l = fmaf(x[1], f, l);
+    o += *(const f32x4*)(a.part + ((int64_t)s * all + R) * a.d + ch) * f;
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  store4((T*)a.out + R * a.d + ch, o * inv);
+  if (ch == 0) *(f32x2*)(a.stat + 2 * R) = f32x2{m, l > 0.f ? __logf(l) : 0.f};
+}
+
+template <typename T, int DP, int NW>
+void fwd_launch(const XatArgs& a, hipStream_t s) {
+  const int tiles = xat_row_tiles(a, NW);
+  const dim3 grid((unsigned)(a.batch * a.hk * tiles * a.splits)), wg(64 * NW);
+  if (a.bias) hipLaunchKernelGGL((xat_fwd_kernel<T, DP, NW, true>), grid, wg, 0, s, a, tiles);
+  else hipLaunchKernelGGL((xat_fwd_kernel<T, DP, NW, false>), grid, wg, 0, s, a, tiles);
+}
+
+template <typename T>
+hipError_t fwd(const XatArgs& a, hipStream_t s) {
+  if (a.bias) {
+    const hipError_t e = launch_xat_planes(sizeof(T) == 2 ? TRIATTN_BF16 : TRIATTN_F32, a, s);
+    if (e != hipSuccess) return e;
+  }
+  {
+    KernelTimer t(K_XAT_FWD, s);
+    const int nw = xat_row_waves(a);
+    if (a.d <= 32) nw == 1 ? fwd_launch<T, 32, 1>(a, s) : fwd_launch<T, 32, 4>(a, s);
+    else if (a.d <= 64) nw == 1 ? fwd_launch<T, 64, 1>(a, s) : fwd_launch<T, 64, 4>(a, s);
+    else nw == 1 ? fwd_launch<T, 128, 1>(a, s) : fwd_launch<T, 128, 4>(a, s);
+  }
+  if (a.splits > 1) {
+    KernelTimer t(K_XAT_JOIN, s);
+    const int64_t n = a.batch * a.nq * a.h * (a.d / 4);
+    hipLaunchKernelGGL(xat_join_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+XatPlan xat_fwd_plan(int dtype, const XatArgs& a) {
+  XatPlan p{};
+  const int64_t all = a.batch * a.nq * a.h;
+  p.nkp = (a.nk + 63) / 64 * 64;
+  p.splits = xat_key_splits(a);
+  const size_t e = dtype == TRIATTN_BF16 ? 2 : 4;
+  if (a.bias_batch) p.planes = (size_t)a.bias_batch * a.h * a.nq * p.nkp * e;
+  if (p.splits > 1) p.part = (size_t)p.splits * all * (a.d + 2) * sizeof(float);
+  return p;
+}
+
+hipError_t launch_xat_fwd(int dtype, const XatArgs& a, hipStream_t s) {
+  return dtype == TRIATTN_BF16 ? fwd<bf16>(a, s) : fwd<float>(a, s);
+}
+
+}  // namespace triattn

@@ -423,8 +423,8 @@ int tri_rel_bias_bwd(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges
  *   d a multiple of 8, at most 128 (TRIATTN_ERR_UNSUPPORTED else); heads a multiple of
  *   key_heads, at most 256 (TRIATTN_ERR_UNSUPPORTED above); 1 <= nq, nk <= 2^22;
  *   1 <= batch <= 2^20; scale finite and positive; with g = heads / key_heads, (nq g + 256) g
- *   < 2^32, and fewer than 2^24 workgroups and 2^34 elements a tensor of q's or k's shape
- *   (TRIATTN_ERR_UNSUPPORTED).
+ *   < 2^32, and fewer than 2^24 workgroups and at most 2^34 elements in q, in k and in a map of
+ *   the bias (TRIATTN_ERR_UNSUPPORTED).
  *   bias entries may be -inf (the key is excluded) or as low as the type goes.  Masked keys
  *   have no effect whatever they, or their bias entries, hold (NaN and infinities too), and
  *   zero gradients.  A query without a valid key gets out = 0 and no gradient.  Everything

@@ -160,7 +160,7 @@ struct XatArgs {
   float* part_q;              // and of the rows
   float* dsum;                // [batch][nq][h]
   int* single;                // [batch]: whether it has one valid key at most
-  float* dplanes;             // dbias of every sample, [batch][hk][nq * group][nkp]
+  float* dplanes;             // dbias of every sample, [batch][hk][nq * group][nkp] or as dbias
 };
 
 struct XatPlan {
@@ -173,6 +173,7 @@ hipError_t launch_xat_fwd(int dtype, const XatArgs& a, hipStream_t s);
 hipError_t launch_xat_bwd(int dtype, const XatArgs& a, hipStream_t s);
 // Bias to planes, one row of a plane after the other (xat_bias.hip).
 hipError_t launch_xat_planes(int dtype, const XatArgs& a, hipStream_t s);
-hipError_t launch_xat_dbias(int dtype, const XatArgs& a, hipStream_t s);
+// The other way; heads: from [batch][nq][nk][h] as it is, summed over the samples.
+hipError_t launch_xat_dbias(int dtype, const XatArgs& a, bool heads, hipStream_t s);
 
 }  // namespace triattn

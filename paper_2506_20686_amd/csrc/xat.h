@@ -11,6 +11,7 @@
 
 #include "dma.h"
 #include "ops.h"
+#include "triattn.h"
 
 namespace triattn {
 
@@ -195,8 +196,9 @@ template <int DP, int LINES, int NW>
 struct Share {
   static constexpr int PER = DP / 8, C = LINES * PER / (64 * NW);
   static_assert(LINES * PER % (64 * NW) == 0, "whole chunks");
-  __device__ static inline int line(int u) { return ((int)threadIdx.x + 64 * NW * u) / PER; }
-  __device__ static inline int col(int u) { return ((int)threadIdx.x + 64 * NW * u) % PER; }
+  __device__ static inline int id(int u) { return (int)(threadIdx.x % (64 * NW)) + 64 * NW * u; }
+  __device__ static inline int line(int u) { return id(u) / PER; }
+  __device__ static inline int col(int u) { return id(u) % PER; }
 };
 
 // Chunk at byte `off` of a resource (zeros past its end).
@@ -263,6 +265,7 @@ constexpr int xat_keys() {
 // themselves, which needs no barrier.
 inline int xat_row_waves(const XatArgs& a) { return (int64_t)a.nq * a.group <= 32 ? 1 : 4; }
 inline int xat_key_waves(const XatArgs& a) { return a.nk <= 32 ? 1 : 4; }
+// (with the heads side by side, a wave has 32 rows or keys and a workgroup's others the same)
 inline int xat_row_tiles(const XatArgs& a, int nw) {
   return (int)(((int64_t)a.nq * a.group + 32 * nw - 1) / (32 * nw));
 }
@@ -277,19 +280,72 @@ inline int xat_splits(int64_t wgs, int nw, int64_t steps, int64_t least) {
   if (s > steps / least) s = steps / least;
   return s < 1 ? 1 : (s > 64 ? 64 : (int)s);
 }
-inline int xat_key_splits(const XatArgs& a) {
+// Whether a bias is taken as it lies, four heads a workgroup: the heads' tiles and the bias tile fit LDS, and 4 heads a load.
+inline bool xat_by_heads(int dtype, const XatArgs& a) {
+  return a.bias_batch > 0 && a.group == 1 && a.h % 4 == 0 &&
+         a.d <= (dtype == TRIATTN_BF16 ? 64 : 32);
+}
+
+inline int xat_key_splits(int dtype, const XatArgs& a) {
+  if (xat_by_heads(dtype, a))
+    return xat_splits(a.batch * (a.h / 4) * xat_row_tiles(a, 1), 4, (a.nk + 31) / 32, 6);
   const int nw = xat_row_waves(a);
   return xat_splits(a.batch * a.hk * xat_row_tiles(a, nw), nw, (a.nk + 63) / 64, 4);
 }
-inline int xat_row_splits(const XatArgs& a) {
+inline int xat_row_splits(int dtype, const XatArgs& a) {
+  if (xat_by_heads(dtype, a))
+    return xat_splits(a.batch * (a.h / 4) * xat_key_tiles(a, 1), 4, (a.nq + 31) / 32, 6);
   const int nw = xat_key_waves(a);
   return xat_splits(a.batch * a.hk * xat_key_tiles(a, nw), nw,
                     ((int64_t)a.nq * a.group + 63) / 64, 4);
 }
 
-// Four consecutive keys' bias of a lane's row.
-__device__ inline f32x4 bias4(const bf16* p) { return load4(p); }
-__device__ inline f32x4 bias4(const float* p) { return load4(p); }
+// Where the bias comes from: none; planes of it, a head each, that a launch before made; or, for
+// four heads at a time, as it lies (heads fastest).  In the last case a workgroup's four waves
+// take four heads of the same 32 rows (or keys): each stages its own head's tiles, and they
+// share the bias tile of 32 queries x 32 keys x 4 heads, whose 4 heads are one load.
+enum XatBias { XB_NONE, XB_PLANES, XB_HEADS };
+
+template <typename T>
+struct BiasTile {
+  typedef T V __attribute__((__vector_size__(4 * sizeof(T))));
+  // lines of 32 keys x 4 heads, 8 or 16 bytes apart from the banks of the next: reads of a
+  // head of one key a line (32 lanes, bf16) fall on distinct banks, those of a line's keys too
+  static constexpr int LINE = 32 * 4 * (int)sizeof(T) + 4 * (int)sizeof(T), BYTES = 32 * LINE;
+  static constexpr int C = 4;  // entries of a thread
+  V x[C];
+  __device__ static inline int q(int u) { return (int)threadIdx.x / 32 + 8 * u; }
+  __device__ static inline int k() { return threadIdx.x % 32; }
+  __device__ static inline int64_t at(const XatArgs& a, int64_t b, int q, int k) {
+    return ((b * a.nq + q) * a.nk + k) * a.h;
+  }
+  // The tile at query q0, key k0, heads h0 .. h0 + 3; 0 past the ends.
+  __device__ inline void load(const XatArgs& a, int64_t b, int h0, int q0, int k0) {
+#pragma unroll
+    for (int u = 0; u < C; ++u) {
+      x[u] = V{};
+      if (q0 + q(u) < a.nq && k0 + k() < a.nk)
+        x[u] = *(const V*)((const T*)a.bias + at(a, b, q0 + q(u), k0 + k()) + h0);
+    }
+  }
+  __device__ inline void store(char* t) const {
+#pragma unroll
+    for (int u = 0; u < C; ++u) *(V*)(t + q(u) * LINE + k() * 4 * (int)sizeof(T)) = x[u];
+  }
+  __device__ static inline T* entry(char* t, int q, int k, int head) {
+    return (T*)(t + q * LINE + (k * 4 + head) * (int)sizeof(T));
+  }
+  // Writes the tile (as T holds it) to `to`, of the bias's layout.
+  __device__ static inline void write(const XatArgs& a, T* to, int64_t b, int h0, int q0, int k0,
+                                      const char* t) {
+#pragma unroll
+    for (int u = 0; u < C; ++u)
+      if (q0 + q(u) < a.nq && k0 + k() < a.nk)
+        *(V*)(to + at(a, b, q0 + q(u), k0 + k()) + h0) =
+            *(const V*)(t + q(u) * LINE + k() * 4 * (int)sizeof(T));
+  }
+};
+
 
 // Work items are numbered so that the ones that read the same keys (or rows) are neighbours.
 struct Item {
@@ -304,6 +360,18 @@ __device__ inline Item item_of(const XatArgs& a, int wg, int tiles, int splits) 
   wg /= tiles;
   t.kh = wg % a.hk;
   t.b = wg / a.hk;
+  return t;
+}
+// The same of four heads side by side: neighbours read the same bias lines.
+__device__ inline Item heads_item(const XatArgs& a, int wg, int tiles, int splits) {
+  Item t;
+  const int quads = a.h / 4;
+  t.kh = 4 * (wg % quads) + (threadIdx.x >> 6);
+  wg /= quads;
+  t.split = wg % splits;
+  wg /= splits;
+  t.tile = wg % tiles;
+  t.b = wg / tiles;
   return t;
 }
 

@@ -52,6 +52,19 @@ __global__ __launch_bounds__(256) void xat_dbias_kernel(XatArgs a, int chunks) {
   for (int i = threadIdx.x; i < keys * a.h; i += 256) dst[i] = (T)x[i % a.h * line + i / a.h];
 }
 
+// Sum over the samples of maps of dbias's layout, 4 elements a thread (their number is a
+// multiple of 4).
+template <typename T>
+__global__ __launch_bounds__(256) void xat_dbias_sum_kernel(XatArgs a) {
+  const int64_t all = (int64_t)a.nq * a.nk * a.h;
+  const int64_t i = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+  if (i >= all) return;
+  f32x4 s{};
+#pragma unroll 4
+  for (int64_t b = 0; b < a.batch; ++b) s += *(const f32x4*)(a.dplanes + b * all + i);
+  store4((T*)a.dbias + i, s);
+}
+
 int64_t groups(const XatArgs& a, int& chunks) {
   const int kc = plane_keys(a.h);
   chunks = (a.nkp + kc - 1) / kc;
@@ -69,8 +82,14 @@ hipError_t launch_xat_planes(int dtype, const XatArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_xat_dbias(int dtype, const XatArgs& a, hipStream_t s) {
+hipError_t launch_xat_dbias(int dtype, const XatArgs& a, bool heads, hipStream_t s) {
   KernelTimer t(K_XAT_DBIAS, s);
+  if (heads) {
+    const dim3 grid((unsigned)(((int64_t)a.nq * a.nk * a.h / 4 + 255) / 256)), wg(256);
+    if (dtype == TRIATTN_BF16) hipLaunchKernelGGL(xat_dbias_sum_kernel<bf16>, grid, wg, 0, s, a);
+    else hipLaunchKernelGGL(xat_dbias_sum_kernel<float>, grid, wg, 0, s, a);
+    return hipGetLastError();
+  }
   int chunks;
   const dim3 grid((unsigned)groups(a, chunks)), wg(256);
   if (dtype == TRIATTN_BF16) hipLaunchKernelGGL(xat_dbias_kernel<bf16>, grid, wg, 0, s, a, chunks);

@@ -48,16 +48,22 @@ __device__ inline float* part_e(const XatArgs& a, int split, int64_t R) {
   return a.part + (int64_t)a.splits * all * 2 * a.d + (int64_t)split * all + R;
 }
 
-template <typename T, int DP, int NW, bool BIAS>
+template <typename T, int DP, int NW, int MODE>
 __global__ __launch_bounds__(64 * NW) void xat_dq_kernel(XatArgs a, int tiles) {
-  constexpr int BK = xat_keys<T, DP, NW>(), J = BK / 32;
+  constexpr bool BIAS = MODE != XB_NONE, HEADS = MODE == XB_HEADS;
+  constexpr int SW = HEADS ? 1 : NW;  // waves that share a tile
+  constexpr int BK = xat_keys<T, DP, SW>(), J = BK / 32;
   constexpr uint64_t ALL = BK == 64 ? ~0ull : (1ull << BK) - 1;
-  using St = KvStage<T, DP, BK, NW>;
+  using St = KvStage<T, DP, BK, SW>;
+  using Bt = BiasTile<T>;
   using L = XTile<T, DP>;
-  __shared__ __attribute__((aligned(16))) char lds[2 * 2 * St::BYTES];
-  const Item w = item_of(a, xcd_swizzle(blockIdx.x, gridDim.x), tiles, a.splits);
+  __shared__ __attribute__((aligned(16))) char lds[2 * 2 * St::BYTES * (NW / SW)];
+  __shared__ __attribute__((aligned(16))) char blds[HEADS ? 2 * Bt::BYTES : 16];
+  const int wg = xcd_swizzle(blockIdx.x, gridDim.x);
+  const Item w = HEADS ? heads_item(a, wg, tiles, a.splits) : item_of(a, wg, tiles, a.splits);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
-  const int rows = a.nq * a.group, first = (w.tile * NW + wave) * 32;
+  const int rows = a.nq * a.group, first = (w.tile * SW + (HEADS ? 0 : wave)) * 32;
+  const int64_t bb = a.bias_batch == 1 ? 0 : w.b;
   const int r = first + (lane & 31), in = r < rows ? r : rows - 1;
   const int64_t R = row_at(a, w.b, w.kh, in, 1);
   typename L::Row q, dy;
@@ -72,9 +78,7 @@ __global__ __launch_bounds__(64 * NW) void xat_dq_kernel(XatArgs a, int tiles) {
   float m, add;
   row_stat<BIAS>(a, R, m, add);
   const T* bias = nullptr;
-  if (BIAS)
-    bias = (const T*)a.planes +
-           (((a.bias_batch == 1 ? 0 : w.b) * a.hk + w.kh) * rows + in) * a.nkp + 4 * g;
+  if (MODE == XB_PLANES) bias = (const T*)a.planes + ((bb * a.hk + w.kh) * rows + in) * a.nkp + 4 * g;
   const int nt = (a.nk + BK - 1) / BK;
   const int t0 = (int)((int64_t)nt * w.split / a.splits);
   const int t1 = (int)((int64_t)nt * (w.split + 1) / a.splits);
@@ -83,14 +87,19 @@ __global__ __launch_bounds__(64 * NW) void xat_dq_kernel(XatArgs a, int tiles) {
   float e = 0.f;
   int valid = 0;  // keys
   St st;
+  Bt bt;
   st.load(a, w.b, w.kh, t0 * BK);
+  if (HEADS) bt.load(a, bb, w.kh & ~3, first, t0 * BK);
   for (int t = t0; t < t1; ++t) {
-    char* tk = lds + (t & 1) * 2 * St::BYTES;
+    char* tk = lds + ((t & 1) + (HEADS ? 2 * wave : 0)) * 2 * St::BYTES;
     char* tv = tk + St::BYTES;
+    char* tb = blds + (HEADS ? (t & 1) * Bt::BYTES : 0);
     const uint64_t ok = st.bits();
     st.store(tk, tv, ok);
+    if (HEADS) bt.store(tb);
     valid += __popcll(ok);
     st.load(a, w.b, w.kh, (t + 1) * BK);
+    if (HEADS) bt.load(a, bb, w.kh & ~3, first, (t + 1) * BK);
     __syncthreads();
     if (ok == 0 || first >= rows) continue;
 #pragma unroll
@@ -100,7 +109,14 @@ __global__ __launch_bounds__(64 * NW) void xat_dq_kernel(XatArgs a, int tiles) {
       if constexpr (BIAS) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const f32x4 x = bias4(bias + (int64_t)t * BK + 32 * j + 8 * i);
+          f32x4 x;
+          if constexpr (HEADS) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              x[u] = (float)*Bt::entry(tb, lane & 31, 8 * i + 4 * g + u, wave);
+          } else {
+            x = load4(bias + (int64_t)t * BK + 32 * j + 8 * i);
+          }
 #pragma unroll
           for (int u = 0; u < 4; ++u) s[4 * i + u] = fmaf(s[4 * i + u], a.scale, x[u]);
         }
@@ -200,9 +216,9 @@ struct RowStage {
       q[u] = load_chunk<T>(rq, off);
       dy[u] = load_chunk<T>(rd, off);
     }
-    const int r = r0 + (int)threadIdx.x;
+    const int id = threadIdx.x % (64 * NW), r = r0 + id;
     m = 0.f, add = neg_inf(), d = 0.f;
-    if ((int)threadIdx.x < BQ && r < rows) {
+    if (id < BQ && r < rows) {
       const int64_t R = row_at(a, b, kh, r, 1);
       row_stat<BIAS>(a, R, m, add);
       d = a.dsum[R];
@@ -214,8 +230,9 @@ struct RowStage {
       L::put(t, S::line(u), S::col(u), q[u]);
       L::put(t + TILE, S::line(u), S::col(u), dy[u]);
     }
-    if ((int)threadIdx.x < BQ) {
-      float* p = (float*)(t + 2 * TILE) + threadIdx.x;
+    const int id = threadIdx.x % (64 * NW);
+    if (id < BQ) {
+      float* p = (float*)(t + 2 * TILE) + id;
       p[0] = m;
       p[BQ] = add;
       p[2 * BQ] = d;
@@ -223,15 +240,26 @@ struct RowStage {
   }
 };
 
-template <typename T, int DP, int NW, bool BIAS>
+template <typename T, int DP, int NW, int MODE, typename DS = float>
 __global__ __launch_bounds__(64 * NW) void xat_dkv_kernel(XatArgs a, int tiles) {
-  constexpr int BQ = xat_keys<T, DP, NW>(), J = BQ / 32;
-  using St = RowStage<T, DP, BQ, NW, BIAS>;
+  constexpr bool BIAS = MODE != XB_NONE, HEADS = MODE == XB_HEADS;
+  constexpr int SW = HEADS ? 1 : NW;  // waves that share a tile
+  constexpr int BQ = xat_keys<T, DP, SW>(), J = BQ / 32;
+  using St = RowStage<T, DP, BQ, SW, BIAS>;
+  using Bt = BiasTile<T>;
+  using Dt = BiasTile<DS>;
   using L = XTile<T, DP>;
-  __shared__ __attribute__((aligned(16))) char lds[2 * St::BYTES];
-  const Item w = item_of(a, xcd_swizzle(blockIdx.x, gridDim.x), tiles, a.splits_q);
+  // dS of the four heads leaves through LDS: in the bias's place where it has the bias's type
+  constexpr bool SAME = sizeof(T) == sizeof(DS);
+  __shared__ __attribute__((aligned(16))) char lds[2 * St::BYTES * (NW / SW)];
+  __shared__ __attribute__((aligned(16))) char blds[HEADS ? 2 * Bt::BYTES : 16];
+  __shared__ __attribute__((aligned(16))) char dlds[HEADS && !SAME ? 2 * Dt::BYTES : 16];
+  const int wg = xcd_swizzle(blockIdx.x, gridDim.x);
+  const Item w = HEADS ? heads_item(a, wg, tiles, a.splits_q) : item_of(a, wg, tiles, a.splits_q);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
-  const int rows = a.nq * a.group, first = (w.tile * NW + wave) * 32, key = first + (lane & 31);
+  const int rows = a.nq * a.group, first = (w.tile * SW + (HEADS ? 0 : wave)) * 32;
+  const int key = first + (lane & 31);
+  const int64_t bb = a.bias_batch == 1 ? 0 : w.b;
   const bool valid = key < a.nk && (a.mask == nullptr || a.mask[w.b * a.nk + key] != 0);
   const int64_t K = (w.b * a.nk + (key < a.nk ? key : a.nk - 1)) * a.hk + w.kh;
   typename L::Row kf, vf;
@@ -239,8 +267,8 @@ __global__ __launch_bounds__(64 * NW) void xat_dkv_kernel(XatArgs a, int tiles) 
   L::row((const T*)a.v + K * a.d, a.d, valid, vf);
   const T* bias = nullptr;
   float* ds = nullptr;
-  if (BIAS) {
-    bias = (const T*)a.planes + ((a.bias_batch == 1 ? 0 : w.b) * a.hk + w.kh) * rows * a.nkp + key;
+  if (MODE == XB_PLANES) {
+    bias = (const T*)a.planes + (bb * a.hk + w.kh) * rows * a.nkp + key;
     if (a.dbias) ds = a.dplanes + (w.b * a.hk + w.kh) * rows * a.nkp + key;
   }
   const int nt = (rows + BQ - 1) / BQ;
@@ -250,13 +278,19 @@ __global__ __launch_bounds__(64 * NW) void xat_dkv_kernel(XatArgs a, int tiles) 
   f32x16 dv[DP / 32] = {}, dk[DP / 32] = {};
   const bool single = a.single[w.b] != 0;
   St st;
+  Bt bt;
   st.load(a, w.b, w.kh, t0 * BQ);
+  if (HEADS) bt.load(a, bb, w.kh & ~3, t0 * BQ, first);
   for (int t = t0; t < t1; ++t) {
-    char* tq = lds + (t & 1) * St::BYTES;
+    char* tq = lds + ((t & 1) + (HEADS ? 2 * wave : 0)) * St::BYTES;
     char* td = tq + St::TILE;
+    char* tb = blds + (HEADS ? (t & 1) * Bt::BYTES : 0);
+    char* ts = SAME ? tb : dlds + (HEADS ? (t & 1) * Dt::BYTES : 0);
     const float* stat = (const float*)(tq + 2 * St::TILE);
     st.store(tq);
+    if (HEADS) bt.store(tb);
     st.load(a, w.b, w.kh, (t + 1) * BQ);
+    if (HEADS) bt.load(a, bb, w.kh & ~3, (t + 1) * BQ, first);
     __syncthreads();
     if (first >= a.nk) continue;
 #pragma unroll
@@ -268,7 +302,8 @@ __global__ __launch_bounds__(64 * NW) void xat_dkv_kernel(XatArgs a, int tiles) 
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           const int r = r0 + acc_row(v, g);
-          x[v] = key < a.nk && r < rows ? (float)bias[(int64_t)r * a.nkp] : 0.f;
+          if (HEADS) x[v] = (float)*Bt::entry(tb, acc_row(v, g), lane & 31, wave);
+          else x[v] = key < a.nk && r < rows ? (float)bias[(int64_t)r * a.nkp] : 0.f;
         }
       }
       f32x16 s = L::dot(tq, 32 * j, kf, f32x16{});
@@ -289,7 +324,16 @@ __global__ __launch_bounds__(64 * NW) void xat_dkv_kernel(XatArgs a, int tiles) 
         }
       }
       if (single) dp = f32x16{};
-      if (BIAS && ds) {
+      if (HEADS && a.dbias) {
+        // a wave writes where it alone has read; all four before the entries leave
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          *Dt::entry(ts, acc_row(v, g), lane & 31, wave) = (DS)(valid ? dp[v] : 0.f);
+        __syncthreads();
+        Dt::write(a, a.bias_batch == a.batch ? (DS*)a.dbias : (DS*)a.dplanes, w.b, w.kh & ~3, r0,
+                  first, ts);
+      }
+      if (MODE == XB_PLANES && ds) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           const int r = r0 + acc_row(v, g);
@@ -347,28 +391,47 @@ template <typename T, int DP, int NW>
 void dq_launch(const XatArgs& a, hipStream_t s) {
   const int tiles = xat_row_tiles(a, NW);
   const dim3 grid((unsigned)(a.batch * a.hk * tiles * a.splits)), wg(64 * NW);
-  if (a.bias) hipLaunchKernelGGL((xat_dq_kernel<T, DP, NW, true>), grid, wg, 0, s, a, tiles);
-  else hipLaunchKernelGGL((xat_dq_kernel<T, DP, NW, false>), grid, wg, 0, s, a, tiles);
+  if (a.bias) hipLaunchKernelGGL((xat_dq_kernel<T, DP, NW, XB_PLANES>), grid, wg, 0, s, a, tiles);
+  else hipLaunchKernelGGL((xat_dq_kernel<T, DP, NW, XB_NONE>), grid, wg, 0, s, a, tiles);
+}
+template <typename T, int DP>
+void dq_heads(const XatArgs& a, hipStream_t s) {
+  const int tiles = xat_row_tiles(a, 1);
+  const dim3 grid((unsigned)(a.batch * (a.h / 4) * tiles * a.splits)), wg(256);
+  hipLaunchKernelGGL((xat_dq_kernel<T, DP, 4, XB_HEADS>), grid, wg, 0, s, a, tiles);
+}
+template <typename T, int DP>
+void dkv_heads(const XatArgs& a, hipStream_t s) {
+  const int tiles = xat_key_tiles(a, 1);
+  const dim3 grid((unsigned)(a.batch * (a.h / 4) * tiles * a.splits_q)), wg(256);
+  // samples that share a bias: dS in fp32, to be summed over them
+  if (a.bias_batch == a.batch)
+    hipLaunchKernelGGL((xat_dkv_kernel<T, DP, 4, XB_HEADS, T>), grid, wg, 0, s, a, tiles);
+  else
+    hipLaunchKernelGGL((xat_dkv_kernel<T, DP, 4, XB_HEADS, float>), grid, wg, 0, s, a, tiles);
 }
 template <typename T, int DP, int NW>
 void dkv_launch(const XatArgs& a, hipStream_t s) {
   const int tiles = xat_key_tiles(a, NW);
   const dim3 grid((unsigned)(a.batch * a.hk * tiles * a.splits_q)), wg(64 * NW);
-  if (a.bias) hipLaunchKernelGGL((xat_dkv_kernel<T, DP, NW, true>), grid, wg, 0, s, a, tiles);
-  else hipLaunchKernelGGL((xat_dkv_kernel<T, DP, NW, false>), grid, wg, 0, s, a, tiles);
+  if (a.bias) hipLaunchKernelGGL((xat_dkv_kernel<T, DP, NW, XB_PLANES>), grid, wg, 0, s, a, tiles);
+  else hipLaunchKernelGGL((xat_dkv_kernel<T, DP, NW, XB_NONE>), grid, wg, 0, s, a, tiles);
 }
 
 template <typename T>
 hipError_t bwd(const XatArgs& a, hipStream_t s) {
   const int dtype = sizeof(T) == 2 ? TRIATTN_BF16 : TRIATTN_F32;
-  if (a.bias) {
+  const bool heads = xat_by_heads(dtype, a);
+  if (a.bias && !heads) {
     const hipError_t e = launch_xat_planes(dtype, a, s);
     if (e != hipSuccess) return e;
   }
   {
     KernelTimer t(K_XAT_DQ, s);
     const int nw = xat_row_waves(a);
-    if (a.d <= 32) nw == 1 ? dq_launch<T, 32, 1>(a, s) : dq_launch<T, 32, 4>(a, s);
+    if (heads && a.d <= 32) dq_heads<T, 32>(a, s);
+    else if (heads) dq_heads<bf16, 64>(a, s);
+    else if (a.d <= 32) nw == 1 ? dq_launch<T, 32, 1>(a, s) : dq_launch<T, 32, 4>(a, s);
     else if (a.d <= 64) nw == 1 ? dq_launch<T, 64, 1>(a, s) : dq_launch<T, 64, 4>(a, s);
     else nw == 1 ? dq_launch<T, 128, 1>(a, s) : dq_launch<T, 128, 4>(a, s);
   }
@@ -380,7 +443,9 @@ hipError_t bwd(const XatArgs& a, hipStream_t s) {
   {
     KernelTimer t(K_XAT_DKV, s);
     const int nw = xat_key_waves(a);
-    if (a.d <= 32) nw == 1 ? dkv_launch<T, 32, 1>(a, s) : dkv_launch<T, 32, 4>(a, s);
+    if (heads && a.d <= 32) dkv_heads<T, 32>(a, s);
+    else if (heads) dkv_heads<bf16, 64>(a, s);
+    else if (a.d <= 32) nw == 1 ? dkv_launch<T, 32, 1>(a, s) : dkv_launch<T, 32, 4>(a, s);
     else if (a.d <= 64) nw == 1 ? dkv_launch<T, 64, 1>(a, s) : dkv_launch<T, 64, 4>(a, s);
     else nw == 1 ? dkv_launch<T, 128, 1>(a, s) : dkv_launch<T, 128, 4>(a, s);
   }
@@ -390,7 +455,7 @@ hipError_t bwd(const XatArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(xat_dkv_join_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s,
                        a);
   }
-  if (a.dbias) return launch_xat_dbias(dtype, a, s);
+  if (a.dbias && !(heads && a.bias_batch == a.batch)) return launch_xat_dbias(dtype, a, heads, s);
   return hipGetLastError();
 }
 
@@ -400,12 +465,16 @@ XatPlan xat_bwd_plan(int dtype, const XatArgs& a) {
   XatPlan p{};
   const int64_t all = a.batch * a.nq * a.h, keys = a.batch * a.nk * a.hk;
   p.nkp = (a.nk + 63) / 64 * 64;
-  p.splits = xat_key_splits(a);
-  p.splits_q = xat_row_splits(a);
+  p.splits = xat_key_splits(dtype, a);
+  p.splits_q = xat_row_splits(dtype, a);
   const size_t e = dtype == TRIATTN_BF16 ? 2 : 4;
   if (a.bias_batch) {
-    p.planes = (size_t)a.bias_batch * a.h * a.nq * p.nkp * e;
-    p.dplanes = (size_t)a.batch * a.h * a.nq * p.nkp * sizeof(float);  // unused without dbias
+    const bool heads = xat_by_heads(dtype, a);
+    const size_t maps = (size_t)a.batch * a.h * a.nq;
+    if (!heads) p.planes = (size_t)a.bias_batch * a.h * a.nq * p.nkp * e;
+    // (unused without dbias)
+    if (!heads) p.dplanes = maps * p.nkp * sizeof(float);
+    else if (a.bias_batch != a.batch) p.dplanes = maps * a.nk * sizeof(float);
   }
   p.dsum = (size_t)all * sizeof(float);
   p.single = (size_t)a.batch * sizeof(int);

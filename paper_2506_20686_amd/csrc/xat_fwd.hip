@@ -16,23 +16,27 @@
 namespace triattn {
 namespace {
 
-template <typename T, int DP, int NW, bool BIAS>
+template <typename T, int DP, int NW, int MODE>
 __global__ __launch_bounds__(64 * NW) void xat_fwd_kernel(XatArgs a, int tiles) {
-  constexpr int BK = xat_keys<T, DP, NW>(), J = BK / 32;
+  constexpr bool BIAS = MODE != XB_NONE, HEADS = MODE == XB_HEADS;
+  constexpr int SW = HEADS ? 1 : NW;  // waves that share a tile
+  constexpr int BK = xat_keys<T, DP, SW>(), J = BK / 32;
   constexpr uint64_t ALL = BK == 64 ? ~0ull : (1ull << BK) - 1;
-  using St = KvStage<T, DP, BK, NW>;
+  using St = KvStage<T, DP, BK, SW>;
+  using Bt = BiasTile<T>;
   using L = XTile<T, DP>;
-  __shared__ __attribute__((aligned(16))) char lds[2 * 2 * St::BYTES];
-  const Item w = item_of(a, xcd_swizzle(blockIdx.x, gridDim.x), tiles, a.splits);
+  __shared__ __attribute__((aligned(16))) char lds[2 * 2 * St::BYTES * (NW / SW)];
+  __shared__ __attribute__((aligned(16))) char blds[HEADS ? 2 * Bt::BYTES : 16];
+  const int wg = xcd_swizzle(blockIdx.x, gridDim.x);
+  const Item w = HEADS ? heads_item(a, wg, tiles, a.splits) : item_of(a, wg, tiles, a.splits);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
-  const int rows = a.nq * a.group, first = (w.tile * NW + wave) * 32;
+  const int rows = a.nq * a.group, first = (w.tile * SW + (HEADS ? 0 : wave)) * 32;
   const int r = first + (lane & 31), in = r < rows ? r : rows - 1;
+  const int64_t bb = a.bias_batch == 1 ? 0 : w.b;
   typename L::Row q;
   L::row((const T*)a.q + row_at(a, w.b, w.kh, in, a.d), a.d, r < rows, q);
   const T* bias = nullptr;
-  if (BIAS)
-    bias = (const T*)a.planes +
-           (((a.bias_batch == 1 ? 0 : w.b) * a.hk + w.kh) * rows + in) * a.nkp + 4 * g;
+  if (MODE == XB_PLANES) bias = (const T*)a.planes + ((bb * a.hk + w.kh) * rows + in) * a.nkp + 4 * g;
   const int nt = (a.nk + BK - 1) / BK;
   const int t0 = (int)((int64_t)nt * w.split / a.splits);
   const int t1 = (int)((int64_t)nt * (w.split + 1) / a.splits);
@@ -40,13 +44,18 @@ __global__ __launch_bounds__(64 * NW) void xat_fwd_kernel(XatArgs a, int tiles) 
   float m = neg_inf(), l = 0.f;
   f32x16 o[DP / 32] = {};
   St st;
+  Bt bt;
   st.load(a, w.b, w.kh, t0 * BK);
+  if (HEADS) bt.load(a, bb, w.kh & ~3, first, t0 * BK);
   for (int t = t0; t < t1; ++t) {
-    char* tk = lds + (t & 1) * 2 * St::BYTES;
+    char* tk = lds + ((t & 1) + (HEADS ? 2 * wave : 0)) * 2 * St::BYTES;
     char* tv = tk + St::BYTES;
+    char* tb = blds + (HEADS ? (t & 1) * Bt::BYTES : 0);
     const uint64_t ok = st.bits();
     st.store(tk, tv, ok);
+    if (HEADS) bt.store(tb);
     st.load(a, w.b, w.kh, (t + 1) * BK);
+    if (HEADS) bt.load(a, bb, w.kh & ~3, first, (t + 1) * BK);
     // this buffer was last read two steps ago, before the barrier of the last step
     __syncthreads();
     if (ok == 0 || first >= rows) continue;
@@ -57,7 +66,14 @@ __global__ __launch_bounds__(64 * NW) void xat_fwd_kernel(XatArgs a, int tiles) 
       if constexpr (BIAS) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const f32x4 x = bias4(bias + (int64_t)t * BK + 32 * j + 8 * i);
+          f32x4 x;
+          if constexpr (HEADS) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              x[e] = (float)*Bt::entry(tb, lane & 31, 8 * i + 4 * g + e, wave);
+          } else {
+            x = load4(bias + (int64_t)t * BK + 32 * j + 8 * i);
+          }
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[j][4 * i + e] = fmaf(s[j][4 * i + e], a.scale, x[e]);
         }
@@ -149,20 +165,30 @@ template <typename T, int DP, int NW>
 void fwd_launch(const XatArgs& a, hipStream_t s) {
   const int tiles = xat_row_tiles(a, NW);
   const dim3 grid((unsigned)(a.batch * a.hk * tiles * a.splits)), wg(64 * NW);
-  if (a.bias) hipLaunchKernelGGL((xat_fwd_kernel<T, DP, NW, true>), grid, wg, 0, s, a, tiles);
-  else hipLaunchKernelGGL((xat_fwd_kernel<T, DP, NW, false>), grid, wg, 0, s, a, tiles);
+  if (a.bias) hipLaunchKernelGGL((xat_fwd_kernel<T, DP, NW, XB_PLANES>), grid, wg, 0, s, a, tiles);
+  else hipLaunchKernelGGL((xat_fwd_kernel<T, DP, NW, XB_NONE>), grid, wg, 0, s, a, tiles);
+}
+template <typename T, int DP>
+void fwd_heads(const XatArgs& a, hipStream_t s) {
+  const int tiles = xat_row_tiles(a, 1);
+  const dim3 grid((unsigned)(a.batch * (a.h / 4) * tiles * a.splits)), wg(256);
+  hipLaunchKernelGGL((xat_fwd_kernel<T, DP, 4, XB_HEADS>), grid, wg, 0, s, a, tiles);
 }
 
 template <typename T>
 hipError_t fwd(const XatArgs& a, hipStream_t s) {
-  if (a.bias) {
-    const hipError_t e = launch_xat_planes(sizeof(T) == 2 ? TRIATTN_BF16 : TRIATTN_F32, a, s);
+  const int dtype = sizeof(T) == 2 ? TRIATTN_BF16 : TRIATTN_F32;
+  const bool heads = xat_by_heads(dtype, a);
+  if (a.bias && !heads) {
+    const hipError_t e = launch_xat_planes(dtype, a, s);
     if (e != hipSuccess) return e;
   }
   {
     KernelTimer t(K_XAT_FWD, s);
     const int nw = xat_row_waves(a);
-    if (a.d <= 32) nw == 1 ? fwd_launch<T, 32, 1>(a, s) : fwd_launch<T, 32, 4>(a, s);
+    if (heads && a.d <= 32) fwd_heads<T, 32>(a, s);
+    else if (heads) fwd_heads<bf16, 64>(a, s);
+    else if (a.d <= 32) nw == 1 ? fwd_launch<T, 32, 1>(a, s) : fwd_launch<T, 32, 4>(a, s);
     else if (a.d <= 64) nw == 1 ? fwd_launch<T, 64, 1>(a, s) : fwd_launch<T, 64, 4>(a, s);
     else nw == 1 ? fwd_launch<T, 128, 1>(a, s) : fwd_launch<T, 128, 4>(a, s);
   }
@@ -180,9 +206,9 @@ XatPlan xat_fwd_plan(int dtype, const XatArgs& a) {
   XatPlan p{};
   const int64_t all = a.batch * a.nq * a.h;
   p.nkp = (a.nk + 63) / 64 * 64;
-  p.splits = xat_key_splits(a);
+  p.splits = xat_key_splits(dtype, a);
   const size_t e = dtype == TRIATTN_BF16 ? 2 : 4;
-  if (a.bias_batch) p.planes = (size_t)a.bias_batch * a.h * a.nq * p.nkp * e;
+  if (a.bias_batch && !xat_by_heads(dtype, a)) p.planes = (size_t)a.bias_batch * a.h * a.nq * p.nkp * e;
   if (p.splits > 1) p.part = (size_t)p.splits * all * (a.d + 2) * sizeof(float);
   return p;
 }

@@ -57,7 +57,8 @@ SIZES = [(1, 1, 1, 1, 1, 8), (1, 1, 1, 2, 1, 16), (2, 7, 33, 4, 4, 32), (1, 33, 
          (1, 5, 2100, 8, 1, 16), (2, 300, 20, 4, 4, 40), (1, 129, 257, 2, 1, 128),
          (1, 40, 100, 2, 2, 96), (1, 700, 90, 1, 1, 72), (5, 32, 128, 4, 4, 32),
          (2, 11, 32, 6, 2, 8), (1, 1500, 3, 2, 2, 32), (1, 3, 1500, 1, 1, 128),
-         (2, 1, 130, 7, 1, 56), (1, 97, 640, 5, 5, 24)]
+         (2, 1, 130, 7, 1, 56), (1, 97, 640, 5, 5, 24), (1, 45, 70, 16, 16, 24),
+         (3, 50, 40, 8, 8, 64), (1, 1, 1, 4, 4, 8)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F4])
@@ -73,9 +74,11 @@ def test_mask_without_bias_and_scale(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F4])
-@pytest.mark.parametrize("bias", ["none", "each"])
-def test_nothing_masked_has_an_effect(dtype, bias):
-    q, k, v, x, m, y = inputs(2, 70, 100, 4, 2, 32, dtype, bias, True, seed=7)
+@pytest.mark.parametrize("bias,hk", [("none", 2), ("each", 2), ("each", 4), ("shared", 4)])
+def test_nothing_masked_has_an_effect(dtype, bias, hk):
+    q, k, v, x, m, y = inputs(2, 70, 100, 4, hk, 32, dtype, bias, True, seed=7)
+    if bias == "shared":
+        m[1] = m[0]
     want = both(q, k, v, x, m, y)
     off = (m == 0)
     for value in (math.nan, math.inf, -math.inf):
@@ -83,7 +86,10 @@ def test_nothing_masked_has_an_effect(dtype, bias):
         k2[off], v2[off] = value, value
         x2 = None if x is None else x.clone()
         if x2 is not None:
-            x2.permute(0, 2, 1, 3)[off] = value
+            if bias == "shared":
+                x2.permute(1, 0, 2)[off[0]] = value
+            else:
+                x2.permute(0, 2, 1, 3)[off] = value
         out, stat = B.cross_attn_fwd(dev(q), dev(k2), dev(v2), dev(x2), dev(m))
         got = (out, stat, *B.cross_attn_bwd(dev(q), dev(k2), dev(v2), out, stat, dev(y), dev(x2),
                                             dev(m)))
@@ -179,7 +185,8 @@ def test_sharp_weights():
 
 
 @pytest.mark.parametrize("dtype", [BF, F4])
-@pytest.mark.parametrize("size", [(2, 37, 70, 4, 2, 24), (1, 3, 900, 4, 1, 64), (1, 900, 5, 2, 2, 8)],
+@pytest.mark.parametrize("size", [(2, 37, 70, 4, 2, 24), (1, 3, 900, 4, 1, 64), (1, 900, 5, 2, 2, 8),
+                                  (2, 37, 70, 8, 8, 24)],
                          ids=str)
 def test_nothing_outside_the_outputs_is_written(size, dtype):
     b, nq, nk, h, hk, d = size

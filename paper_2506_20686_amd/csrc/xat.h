@@ -300,6 +300,12 @@ inline int xat_row_splits(int dtype, const XatArgs& a) {
                     ((int64_t)a.nq * a.group + 63) / 64, 4);
 }
 
+// Waves a SIMD that a backward kernel's registers have to leave room for.
+template <typename T, int DP>
+constexpr int xat_waves() {
+  return sizeof(T) == 2 && DP <= 64 ? 2 : 1;
+}
+
 // Where the bias comes from: none; planes of it, a head each, that a launch before made; or, for
 // four heads at a time, as it lies (heads fastest).  In the last case a workgroup's four waves
 // take four heads of the same 32 rows (or keys): each stages its own head's tiles, and they

@@ -49,7 +49,7 @@ __device__ inline float* part_e(const XatArgs& a, int split, int64_t R) {
 }
 
 template <typename T, int DP, int NW, int MODE>
-__global__ __launch_bounds__(64 * NW) void xat_dq_kernel(XatArgs a, int tiles) {
+__global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dq_kernel(XatArgs a, int tiles) {
   constexpr bool BIAS = MODE != XB_NONE, HEADS = MODE == XB_HEADS;
   constexpr int SW = HEADS ? 1 : NW;  // waves that share a tile
   constexpr int BK = xat_keys<T, DP, SW>(), J = BK / 32;
@@ -241,7 +241,7 @@ struct RowStage {
 };
 
 template <typename T, int DP, int NW, int MODE, typename DS = float>
-__global__ __launch_bounds__(64 * NW) void xat_dkv_kernel(XatArgs a, int tiles) {
+__global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dkv_kernel(XatArgs a, int tiles) {
   constexpr bool BIAS = MODE != XB_NONE, HEADS = MODE == XB_HEADS;
   constexpr int SW = HEADS ? 1 : NW;  // waves that share a tile
   constexpr int BQ = xat_keys<T, DP, SW>(), J = BQ / 32;

@@ -306,6 +306,24 @@ constexpr int xat_waves() {
   return sizeof(T) == 2 && DP <= 64 ? 2 : 1;
 }
 
+template <typename T, int DP, int NW>
+constexpr int xat_fwd_waves() {
+  return sizeof(T) == 2 ? (DP == 32 ? 4 : DP == 64 ? 3 : NW == 4 ? 2 : 1) : 1;
+}
+
+// The logits' (or weights') values of a tile's masked keys set to `value`, for the few tiles that
+// need it.  The empty statement keeps it in a branch of its own: without, its comparisons and
+// selects run for every tile.  The caller has used every value it passes in ordinary
+// instructions before the branch: the compiler counts the wait states after a matrix instruction
+// along one path to a join only, and that may be the longer one.
+__device__ inline void mask_tile(f32x16& s, uint32_t bits, int g, float value) {
+  asm volatile("");
+  const uint32_t b = bits >> (4 * g);
+#pragma unroll
+  for (int v = 0; v < 16; ++v)
+    if (!((b >> (8 * (v >> 2) + (v & 3))) & 1u)) s[v] = value;
+}
+
 // Where the bias comes from: none; planes of it, a head each, that a launch before made; or, for
 // four heads at a time, as it lies (heads fastest).  In the last case a workgroup's four waves
 // take four heads of the same 32 rows (or keys): each stages its own head's tiles, and they

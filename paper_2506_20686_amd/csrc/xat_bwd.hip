@@ -121,12 +121,14 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dq_kernel(X
           for (int u = 0; u < 4; ++u) s[4 * i + u] = fmaf(s[4 * i + u], a.scale, x[u]);
         }
       }
-      if (ok != ALL) mask_rows(s, (uint32_t)(ok >> (32 * j)), g);
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         s[v] = weight<BIAS>(s[v], c, m, add);
-        dp[v] = s[v] * (dp[v] - shift);
+        dp[v] -= shift;
+        asm volatile("" : "+v"(s[v]), "+v"(dp[v]));  // made before the branch
       }
+      if (ok != ALL) mask_tile(s, (uint32_t)(ok >> (32 * j)), g, 0.f);
+      dp *= s;
       typename L::Frag fp, fs;
       acc_frags(s, fp);
       acc_frags(dp, fs);

@@ -17,7 +17,7 @@ namespace triattn {
 namespace {
 
 template <typename T, int DP, int NW, int MODE>
-__global__ __launch_bounds__(64 * NW) void xat_fwd_kernel(XatArgs a, int tiles) {
+__global__ __launch_bounds__(64 * NW, (xat_fwd_waves<T, DP, NW>())) void xat_fwd_kernel(XatArgs a, int tiles) {
   constexpr bool BIAS = MODE != XB_NONE, HEADS = MODE == XB_HEADS;
   constexpr int SW = HEADS ? 1 : NW;  // waves that share a tile
   constexpr int BK = xat_keys<T, DP, SW>(), J = BK / 32;
@@ -78,10 +78,16 @@ __global__ __launch_bounds__(64 * NW) void xat_fwd_kernel(XatArgs a, int tiles) 
           for (int e = 0; e < 4; ++e) s[j][4 * i + e] = fmaf(s[j][4 * i + e], a.scale, x[e]);
         }
       }
-      if (ok != ALL) mask_rows(s[j], (uint32_t)(ok >> (32 * j)), g);
     }
     float top = max16(s[0]);
     if constexpr (J == 2) top = fmaxf(top, max16(s[J - 1]));
+    asm volatile("" : "+v"(top));  // made before the branch
+    if (ok != ALL) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) mask_tile(s[j], (uint32_t)(ok >> (32 * j)), g, neg_inf());
+      top = max16(s[0]);
+      if constexpr (J == 2) top = fmaxf(top, max16(s[J - 1]));
+    }
     top = fmaxf(m, wave_xor32_max(top));
     if (__any(top > m)) {
       const float f = top > m ? __builtin_amdgcn_exp2f((m - top) * c) : 1.f;

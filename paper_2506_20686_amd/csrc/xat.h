@@ -99,14 +99,15 @@ struct XTile<bf16, DP> {
         out2[n] = Mma<bf16>::mma(a, p2[i], out2[n]);
       }
   }
-  // the row's channels in registers; `p` its first, d a multiple of 8; zeros if !real
+  // The row's channels in registers; `p` its first, d a multiple of 8; zeros if !real.  All
+  // loads at once, without conditions: one inside a branch is waited for at its end.
   __device__ static inline void row(const bf16* p, int d, bool real, Row& r) {
     const int g = (threadIdx.x & 63) >> 5;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      r[i] = bf16x8{};
-      if (real && 16 * i + 8 * g < d) r[i] = *(const bf16x8*)(p + 16 * i + 8 * g);
-    }
+    for (int i = 0; i < N; ++i) r[i] = *(const bf16x8*)(p + min(16 * i + 8 * g, d - 8));
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (!real || 16 * i + 8 * g >= d) r[i] = bf16x8{};
   }
   __device__ static inline float dot_regs(const Row& a, const Row& b) {  // this half's channels
     float s = 0.f;
@@ -165,11 +166,13 @@ struct XTile<float, DP> {
     const int g = (threadIdx.x & 63) >> 5;
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
-      f32x4 x{};
-      if (real && N * g + 4 * i < d) x = *(const f32x4*)(p + N * g + 4 * i);
+      const f32x4 x = *(const f32x4*)(p + min(N * g + 4 * i, d - 4));
 #pragma unroll
       for (int e = 0; e < 4; ++e) r[4 * i + e] = x[e];
     }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (!real || N * g + i >= d) r[i] = 0.f;
   }
   __device__ static inline float dot_regs(const Row& a, const Row& b) {
     float s = 0.f;
@@ -235,9 +238,11 @@ struct KvStage {
       k[u] = load_chunk<T>(rk, off);
       v[u] = load_chunk<T>(rv, off);
     }
-    const int lane = threadIdx.x & 63;
-    valid = lane < rows && lane < BK;
-    if (a.mask && valid) valid = a.mask[b * a.nk + k0 + lane];
+    const int lane = threadIdx.x & 63, in = rows > 0 ? rows : 0;
+    valid = lane < in;
+    if (a.mask)  // bytes past the tile's keys read as zeros
+      valid = __builtin_amdgcn_raw_buffer_load_b8(buf_rsrc_n(a.mask + b * a.nk + k0, (uint32_t)in),
+                                                  lane, 0, 0);
   }
   // Which of the tile's keys are valid.
   __device__ inline uint64_t bits() const { return __ballot(valid != 0); }
@@ -271,6 +276,11 @@ inline int xat_row_tiles(const XatArgs& a, int nw) {
 }
 inline int xat_key_tiles(const XatArgs& a, int nw) { return (a.nk + 32 * nw - 1) / (32 * nw); }
 
+constexpr int XAT_SPLITS = 128;
+
+// Tiles whose loads are in flight: two where a wave stages for itself.
+constexpr int xat_ahead(int sharing) { return sharing == 1 ? 2 : 1; }
+
 // Splits of a long loop: so that the workgroups (of nw waves) fill the GPU, each of at least
 // `least` steps.
 inline int xat_splits(int64_t wgs, int nw, int64_t steps, int64_t least) {
@@ -278,12 +288,13 @@ inline int xat_splits(int64_t wgs, int nw, int64_t steps, int64_t least) {
   int64_t s = (want + wgs - 1) / wgs;
   if (wgs >= want) s = 1;
   if (s > steps / least) s = steps / least;
-  return s < 1 ? 1 : (s > 64 ? 64 : (int)s);
+  return s < 1 ? 1 : (s > XAT_SPLITS ? XAT_SPLITS : (int)s);
 }
 // Whether a bias is taken as it lies, four heads a workgroup: the heads' tiles and the bias tile fit LDS, and 4 heads a load.
 inline bool xat_by_heads(int dtype, const XatArgs& a) {
-  return a.bias_batch > 0 && a.group == 1 && a.h % 4 == 0 &&
-         a.d <= (dtype == TRIATTN_BF16 ? 64 : 32);
+  const int64_t e = dtype == TRIATTN_BF16 ? 2 : 4;
+  return a.bias_batch > 0 && a.group == 1 && a.h % 4 == 0 && a.d <= (e == 2 ? 64 : 32) &&
+         32 * e * a.nk * a.h < (int64_t)1 << 31;  // offsets within a tile
 }
 
 inline int xat_key_splits(int dtype, const XatArgs& a) {
@@ -306,9 +317,10 @@ constexpr int xat_waves() {
   return sizeof(T) == 2 && DP <= 64 ? 2 : 1;
 }
 
-template <typename T, int DP, int NW>
+template <typename T, int DP, int NW, int MODE>
 constexpr int xat_fwd_waves() {
-  return sizeof(T) == 2 ? (DP == 32 ? 4 : DP == 64 ? 3 : NW == 4 ? 2 : 1) : 1;
+  const int most = DP == 32 ? 4 : DP == 64 ? 3 : 2;  // without a bias, tiles shared
+  return sizeof(T) == 4 ? 1 : NW == 1 || MODE != 0 ? most - 1 : most;
 }
 
 // The logits' (or weights') values of a tile's masked keys set to `value`, for the few tiles that
@@ -345,11 +357,16 @@ struct BiasTile {
   }
   // The tile at query q0, key k0, heads h0 .. h0 + 3; 0 past the ends.
   __device__ inline void load(const XatArgs& a, int64_t b, int h0, int q0, int k0) {
+    const rsrc_t rs = buf_rsrc_n((const T*)a.bias + at(a, b, q0, k0) + h0, 0x7fffffffu);
 #pragma unroll
     for (int u = 0; u < C; ++u) {
-      x[u] = V{};
-      if (q0 + q(u) < a.nq && k0 + k() < a.nk)
-        x[u] = *(const V*)((const T*)a.bias + at(a, b, q0 + q(u), k0 + k()) + h0);
+      const uint32_t off = q0 + q(u) < a.nq && k0 + k() < a.nk
+                               ? (uint32_t)((q(u) * a.nk + k()) * a.h) * sizeof(T)
+                               : NOWHERE;
+      if constexpr (sizeof(T) == 2)
+        x[u] = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(rs, (int)off, 0, 0));
+      else
+        x[u] = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, 0, 0));
     }
   }
   __device__ inline void store(char* t) const {

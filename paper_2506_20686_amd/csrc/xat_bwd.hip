@@ -31,8 +31,7 @@ __device__ inline float weight(float s, float c, float m, float add) {
 // A row's statistics as weight() takes them: its maximum (with a bias), and the addend, -inf
 // for a row without keys (P = 0).
 template <bool BIAS>
-__device__ inline void row_stat(const XatArgs& a, int64_t R, float& m, float& add) {
-  const f32x2 x = *(const f32x2*)(a.stat + 2 * R);
+__device__ inline void row_stat(f32x2 x, float& m, float& add) {
   const bool none = x[0] == neg_inf();
   m = none ? 0.f : x[0];
   add = none ? neg_inf() : -LOG2E * (BIAS ? x[1] : x[0] + x[1]);
@@ -76,7 +75,7 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dq_kernel(X
     shift = wave_xor32_sum(L::dot_regs(dy, o));
   }
   float m, add;
-  row_stat<BIAS>(a, R, m, add);
+  row_stat<BIAS>(*(const f32x2*)(a.stat + 2 * R), m, add);
   const T* bias = nullptr;
   if (MODE == XB_PLANES) bias = (const T*)a.planes + ((bb * a.hk + w.kh) * rows + in) * a.nkp + 4 * g;
   const int nt = (a.nk + BK - 1) / BK;
@@ -86,22 +85,24 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dq_kernel(X
   f32x16 sk[DP / 32] = {}, pk[DP / 32] = {};
   float e = 0.f;
   int valid = 0;  // keys
-  St st;
-  Bt bt;
-  st.load(a, w.b, w.kh, t0 * BK);
-  if (HEADS) bt.load(a, bb, w.kh & ~3, first, t0 * BK);
-  for (int t = t0; t < t1; ++t) {
+  constexpr int D = xat_ahead(SW);  // loads run D tiles ahead
+  St st[D];
+  Bt bt[D];
+  auto load = [&](int d, int t) {
+    st[d].load(a, w.b, w.kh, t * BK);
+    if (HEADS) bt[d].load(a, bb, w.kh & ~3, first, t * BK);
+  };
+  auto step = [&](int d, int t) {
     char* tk = lds + ((t & 1) + (HEADS ? 2 * wave : 0)) * 2 * St::BYTES;
     char* tv = tk + St::BYTES;
     char* tb = blds + (HEADS ? (t & 1) * Bt::BYTES : 0);
-    const uint64_t ok = st.bits();
-    st.store(tk, tv, ok);
-    if (HEADS) bt.store(tb);
+    const uint64_t ok = st[d].bits();
+    st[d].store(tk, tv, ok);
+    if (HEADS) bt[d].store(tb);
     valid += __popcll(ok);
-    st.load(a, w.b, w.kh, (t + 1) * BK);
-    if (HEADS) bt.load(a, bb, w.kh & ~3, first, (t + 1) * BK);
+    load(d, t + D);
     __syncthreads();
-    if (ok == 0 || first >= rows) continue;
+    if (ok == 0 || first >= rows) return;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       f32x16 s = L::dot(tk, 32 * j, q, f32x16{});
@@ -135,6 +136,12 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dq_kernel(X
       e += sum16(dp);
       L::add2(tk, 32 * j, fs, sk, fp, pk);
     }
+  };
+#pragma unroll
+  for (int d = 0; d < D; ++d) load(d, t0 + d);
+  for (int t = t0; t < t1; t += D) {
+    step(0, t);
+    if (D == 2 && t + 1 < t1) step(D - 1, t + 1);
   }
   const bool single = a.splits == 1 && valid <= 1;
   if (w.tile == 0 && w.kh == 0 && w.split == 0 && threadIdx.x == 0) a.single[w.b] = single;
@@ -202,7 +209,9 @@ struct RowStage {
   using L = XTile<T, DP>;
   static constexpr int TILE = BQ * L::LINE, BYTES = 2 * TILE + 3 * BQ * 4;
   Chunk<T> q[S::C], dy[S::C];
-  float m, add, d;
+  f32x2 stat;
+  float d;
+  bool real;
   __device__ inline void load(const XatArgs& a, int64_t b, int kh, int r0) {
     const int rows = a.nq * a.group, q0 = row_query(a, r0 < rows ? r0 : 0);
     const int64_t at = ((b * a.nq + q0) * a.h + kh * a.group) * a.d;
@@ -218,13 +227,15 @@ struct RowStage {
       q[u] = load_chunk<T>(rq, off);
       dy[u] = load_chunk<T>(rd, off);
     }
-    const int id = threadIdx.x % (64 * NW), r = r0 + id;
-    m = 0.f, add = neg_inf(), d = 0.f;
-    if (id < BQ && r < rows) {
-      const int64_t R = row_at(a, b, kh, r, 1);
-      row_stat<BIAS>(a, R, m, add);
-      d = a.dsum[R];
-    }
+    const int id = threadIdx.x % (64 * NW), r = r0 + id, qi = row_query(a, r);
+    real = id < BQ && r < rows;
+    const int64_t R0 = (b * a.nq + q0) * a.h + kh * a.group;
+    const uint32_t i = (uint32_t)((qi - q0) * a.h + r - qi * a.group);
+    stat = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(
+                                         buf_rsrc_n(a.stat + 2 * R0, n), (int)(real ? 8 * i : NOWHERE), 0, 0));
+    d = __builtin_bit_cast(
+        float, __builtin_amdgcn_raw_buffer_load_b32(buf_rsrc_n(a.dsum + R0, n),
+                                                    (int)(real ? 4 * i : NOWHERE), 0, 0));
   }
   __device__ inline void store(char* t) const {
 #pragma unroll
@@ -234,6 +245,8 @@ struct RowStage {
     }
     const int id = threadIdx.x % (64 * NW);
     if (id < BQ) {
+      float m, add;
+      row_stat<BIAS>(real ? stat : f32x2{neg_inf(), 0.f}, m, add);
       float* p = (float*)(t + 2 * TILE) + id;
       p[0] = m;
       p[BQ] = add;
@@ -279,22 +292,26 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dkv_kernel(
   const float c = BIAS ? LOG2E : a.scale * LOG2E;
   f32x16 dv[DP / 32] = {}, dk[DP / 32] = {};
   const bool single = a.single[w.b] != 0;
-  St st;
-  Bt bt;
-  st.load(a, w.b, w.kh, t0 * BQ);
-  if (HEADS) bt.load(a, bb, w.kh & ~3, t0 * BQ, first);
-  for (int t = t0; t < t1; ++t) {
+  constexpr int D = HEADS ? 2 : 1;  // loads run D tiles ahead
+  St st[D];
+  Bt bt[D];
+  auto load = [&](int d, int t) {
+    st[d].load(a, w.b, w.kh, t * BQ);
+    if (HEADS) bt[d].load(a, bb, w.kh & ~3, t * BQ, first);
+  };
+  const bool any = __any(valid);  // the wave has a valid key
+  auto step = [&](int d, int t) {
     char* tq = lds + ((t & 1) + (HEADS ? 2 * wave : 0)) * St::BYTES;
     char* td = tq + St::TILE;
     char* tb = blds + (HEADS ? (t & 1) * Bt::BYTES : 0);
     char* ts = SAME ? tb : dlds + (HEADS ? (t & 1) * Dt::BYTES : 0);
     const float* stat = (const float*)(tq + 2 * St::TILE);
-    st.store(tq);
-    if (HEADS) bt.store(tb);
-    st.load(a, w.b, w.kh, (t + 1) * BQ);
-    if (HEADS) bt.load(a, bb, w.kh & ~3, (t + 1) * BQ, first);
+    st[d].store(tq);
+    if (HEADS) bt[d].store(tb);
+    load(d, t + D);
     __syncthreads();
-    if (first >= a.nk) continue;
+    if (!any && !BIAS) return;
+    if (first >= a.nk) return;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int r0 = t * BQ + 32 * j;
@@ -347,6 +364,15 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dkv_kernel(
       L::add(td, 32 * j, f, dv);
       acc_frags(dp, f);
       L::add(tq, 32 * j, f, dk);
+    }
+  };
+  // a workgroup whose keys are all masked has nothing to sum
+  if (BIAS || __syncthreads_or(valid)) {
+#pragma unroll
+    for (int d = 0; d < D; ++d) load(d, t0 + d);
+    for (int t = t0; t < t1; t += D) {
+      step(0, t);
+      if (D == 2 && t + 1 < t1) step(D - 1, t + 1);
     }
   }
   if (key >= a.nk) return;

@@ -17,7 +17,7 @@ namespace triattn {
 namespace {
 
 template <typename T, int DP, int NW, int MODE>
-__global__ __launch_bounds__(64 * NW, (xat_fwd_waves<T, DP, NW>())) void xat_fwd_kernel(XatArgs a, int tiles) {
+__global__ __launch_bounds__(64 * NW, (xat_fwd_waves<T, DP, NW, MODE>())) void xat_fwd_kernel(XatArgs a, int tiles) {
   constexpr bool BIAS = MODE != XB_NONE, HEADS = MODE == XB_HEADS;
   constexpr int SW = HEADS ? 1 : NW;  // waves that share a tile
   constexpr int BK = xat_keys<T, DP, SW>(), J = BK / 32;
@@ -43,22 +43,25 @@ __global__ __launch_bounds__(64 * NW, (xat_fwd_waves<T, DP, NW>())) void xat_fwd
   const float c = BIAS ? LOG2E : a.scale * LOG2E;
   float m = neg_inf(), l = 0.f;
   f32x16 o[DP / 32] = {};
-  St st;
-  Bt bt;
-  st.load(a, w.b, w.kh, t0 * BK);
-  if (HEADS) bt.load(a, bb, w.kh & ~3, first, t0 * BK);
-  for (int t = t0; t < t1; ++t) {
+  // loads run D tiles ahead; past the end they touch no memory
+  constexpr int D = xat_ahead(SW);
+  St st[D];
+  Bt bt[D];
+  auto load = [&](int d, int t) {
+    st[d].load(a, w.b, w.kh, t * BK);
+    if (HEADS) bt[d].load(a, bb, w.kh & ~3, first, t * BK);
+  };
+  auto step = [&](int d, int t) {
     char* tk = lds + ((t & 1) + (HEADS ? 2 * wave : 0)) * 2 * St::BYTES;
     char* tv = tk + St::BYTES;
     char* tb = blds + (HEADS ? (t & 1) * Bt::BYTES : 0);
-    const uint64_t ok = st.bits();
-    st.store(tk, tv, ok);
-    if (HEADS) bt.store(tb);
-    st.load(a, w.b, w.kh, (t + 1) * BK);
-    if (HEADS) bt.load(a, bb, w.kh & ~3, first, (t + 1) * BK);
+    const uint64_t ok = st[d].bits();
+    st[d].store(tk, tv, ok);
+    if (HEADS) bt[d].store(tb);
+    load(d, t + D);
     // this buffer was last read two steps ago, before the barrier of the last step
     __syncthreads();
-    if (ok == 0 || first >= rows) continue;
+    if (ok == 0 || first >= rows) return;
     f32x16 s[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
@@ -109,6 +112,12 @@ __global__ __launch_bounds__(64 * NW, (xat_fwd_waves<T, DP, NW>())) void xat_fwd
       acc_frags(s[j], p);
       L::add(tv, 32 * j, p, o);
     }
+  };
+#pragma unroll
+  for (int d = 0; d < D; ++d) load(d, t0 + d);
+  for (int t = t0; t < t1; t += D) {
+    step(0, t);
+    if (D == 2 && t + 1 < t1) step(D - 1, t + 1);
   }
   l = wave_xor32_sum(l);
   if (r >= rows) return;
@@ -142,29 +151,49 @@ __global__ __launch_bounds__(64 * NW, (xat_fwd_waves<T, DP, NW>())) void xat_fwd
   if (g == 0) *(f32x2*)(a.stat + 2 * R) = f32x2{m, l > 0.f ? __logf(l) : 0.f};
 }
 
-// Joins the splits: four channels of a row a thread.
+// Joins the splits: a wave a row, its lanes over channels (in fours) and over splits.
 template <typename T>
 __global__ __launch_bounds__(256) void xat_join_kernel(XatArgs a) {
-  const int64_t all = a.batch * a.nq * a.h, quads = a.d / 4;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= all * quads) return;
-  const int64_t R = i / quads;
-  const int ch = 4 * (int)(i % quads);
+  const int64_t all = a.batch * a.nq * a.h;
+  const int64_t R = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (R >= all) return;
+  const int lane = threadIdx.x & 63;
   const float* pm = a.part + (int64_t)a.splits * all * a.d;
+  // the weights of splits lane and lane + 64
+  static_assert(XAT_SPLITS <= 128, "two splits a lane");
+  f32x2 x[2];
   float m = neg_inf();
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, pm[((int64_t)s * all + R) * 2]);
-  const float base = m == neg_inf() ? 0.f : m;
-  float l = 0.f;
-  f32x4 o{};
-  for (int s = 0; s < a.splits; ++s) {
-    const f32x2 x = *(const f32x2*)(pm + ((int64_t)s * all + R) * 2);
-    const float f = __builtin_amdgcn_exp2f((x[0] - base) * LOG2E);
-    l = fmaf(x[1], f, l);
-    o += *(const f32x4*)(a.part + ((int64_t)s * all + R) * a.d + ch) * f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int s = lane + 64 * u;
+    x[u] = f32x2{neg_inf(), 0.f};
+    if (s < a.splits) x[u] = *(const f32x2*)(pm + ((int64_t)s * all + R) * 2);
+    m = fmaxf(m, x[u][0]);
   }
+  for (int i = 1; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i));
+  const float base = m == neg_inf() ? 0.f : m;
+  float f[2], l = 0.f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    f[u] = __builtin_amdgcn_exp2f((x[u][0] - base) * LOG2E);
+    l = fmaf(x[u][1], f[u], l);
+  }
+  for (int i = 1; i < 64; i *= 2) l += __shfl_xor(l, i);
+  const int per = a.d <= 32 ? 8 : a.d <= 64 ? 16 : 32, ch = 4 * (lane % per);
+  f32x4 o{};
+#pragma unroll 4
+  for (int s0 = 0; s0 < a.splits; s0 += 64 / per) {
+    const int s = s0 + lane / per;
+    const float w = __shfl(s < 64 ? f[0] : f[1], s & 63);
+    if (s < a.splits && ch < a.d)
+      o += *(const f32x4*)(a.part + ((int64_t)s * all + R) * a.d + ch) * w;
+  }
+  for (int i = per; i < 64; i *= 2)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], i);
   const float inv = l > 0.f ? 1.f / l : 0.f;
-  store4((T*)a.out + R * a.d + ch, o * inv);
-  if (ch == 0) *(f32x2*)(a.stat + 2 * R) = f32x2{m, l > 0.f ? __logf(l) : 0.f};
+  if (lane < per && ch < a.d) store4((T*)a.out + R * a.d + ch, o * inv);
+  if (lane == 0) *(f32x2*)(a.stat + 2 * R) = f32x2{m, l > 0.f ? __logf(l) : 0.f};
 }
 
 template <typename T, int DP, int NW>
@@ -200,8 +229,8 @@ hipError_t fwd(const XatArgs& a, hipStream_t s) {
   }
   if (a.splits > 1) {
     KernelTimer t(K_XAT_JOIN, s);
-    const int64_t n = a.batch * a.nq * a.h * (a.d / 4);
-    hipLaunchKernelGGL(xat_join_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a);
+    const int64_t n = a.batch * a.nq * a.h;
+    hipLaunchKernelGGL(xat_join_kernel<T>, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, s, a);
   }
   return hipGetLastError();
 }

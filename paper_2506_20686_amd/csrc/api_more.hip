@@ -250,7 +250,7 @@ int tri_gated_linear_bwd_workspace_bytes(int dtype, int64_t m, int64_t k, int64_
   const int st = glu_check(dtype, m, k, f, wider(k, f));
   if (st != TRIATTN_OK) return st;
   if (bytes == nullptr) return TRIATTN_ERR_INVALID_ARG;
-  *bytes = glu_ws(triattn::lin_made_plan(dtype, m, (int)k, (int)(2 * f)));
+  *bytes = glu_ws(triattn::glu_bwd_plan(dtype, m, (int)k, (int)f));
   return TRIATTN_OK;
 }
 
@@ -262,7 +262,7 @@ int tri_gated_linear_bwd(int dtype, int64_t m, int64_t k, int64_t f, int act, co
   if (bad_act(act) || bad_pointers({x, w, dout}, {bias, dx, dw, dbias}))
     return TRIATTN_ERR_INVALID_ARG;
   if (dx == nullptr && dw == nullptr && dbias == nullptr) return TRIATTN_ERR_INVALID_ARG;
-  const triattn::LinBwdPlan plan = triattn::lin_made_plan(dtype, m, (int)k, (int)(2 * f));
+  const triattn::LinBwdPlan plan = triattn::glu_bwd_plan(dtype, m, (int)k, (int)f);
   if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < glu_ws(plan))
     return TRIATTN_ERR_WORKSPACE;
   float* dz = (float*)((char*)workspace + round256(plan.part));
@@ -276,8 +276,6 @@ int tri_gated_linear_bwd(int dtype, int64_t m, int64_t k, int64_t f, int act, co
   a.bias = bias;
   a.dout = dout;
   a.dz = dz;
-  const hipError_t e = triattn::launch_glu_dz(dtype, a, (hipStream_t)stream);
-  if (e != hipSuccess) return TRIATTN_ERR_HIP;
   triattn::LinBwdArgs b{};
   b.m = m;
   b.k = (int)k;
@@ -290,7 +288,7 @@ int tri_gated_linear_bwd(int dtype, int64_t m, int64_t k, int64_t f, int act, co
   b.part = (float*)workspace;
   b.splits = plan.splits;
   b.dz = dz;
-  return launched(triattn::launch_lin_made(dtype, b, (hipStream_t)stream));
+  return launched(triattn::launch_glu_bwd(dtype, a, b, (hipStream_t)stream));
 }
 
 int tri_grad_norm_workspace_bytes(int64_t count, const int64_t* sizes, size_t* bytes) {

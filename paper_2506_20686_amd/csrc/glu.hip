@@ -93,6 +93,323 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void glu_kernel(GluArg
   });
 }
 
+// ---- narrow bf16 projections (k, f <= 128): the pair channels -----------------------------
+//
+// Rows of 128 + 128 channels move as many bytes as 4 f k operations take to multiply in a
+// fraction of the time, so a workgroup keeps W in registers, from the start to its last row,
+// and walks over blocks of 32 rows; nothing but x, dout, out and dx crosses memory.
+constexpr int GLU_ROWS = 32;
+
+// W to LDS as two squares (lines k, columns of a half each), zeros past the ends.
+template <int THREADS>
+__device__ inline void stage_w(const GluArgs& a, char* t) {
+  const Mat<bf16> w{(const bf16*)a.w, a.k, 2 * a.f};
+#pragma unroll
+  for (int u = 0; u < 2 * 128 * 16 / THREADS; ++u) {
+    const int id = (int)threadIdx.x + THREADS * u, half = id / 2048, line = id / 16 % 128;
+    const int c = id % 16;
+    const rsrc_t rs = buf_rsrc_n(w.p, (uint32_t)(a.k * 2 * a.f) * 2u);
+    const uint32_t off = line < a.k && 8 * c < a.f
+                             ? (uint32_t)((line * 2 + half) * a.f + 8 * c) * 2u
+                             : 0x80000000u;
+    *(u32x4*)(t + half * 128 * 256 + Square::chunk_at(line, c)) = __builtin_bit_cast(
+        u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, 0, 0));
+  }
+}
+
+// Four packed bf16 of an accumulator quad.
+__device__ inline u32x2 pack4(float a, float b, float c, float d) {
+  return __builtin_bit_cast(u32x2, bf16x4{(bf16)a, (bf16)b, (bf16)c, (bf16)d});
+}
+// Quads i (columns 8 i + 4 g ..) of a row's 32 results -> this lane's columns 16 g .. + 7 and
+// 16 g + 8 .. + 15, by exchanges between the two halves of the wave.
+__device__ inline void row_words(const u32x2 (&q)[4], u32x4 (&w)[2]) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const auto x = __builtin_amdgcn_permlane32_swap(q[u][0], q[u + 2][0], false, false);
+    const auto y = __builtin_amdgcn_permlane32_swap(q[u][1], q[u + 2][1], false, false);
+    w[u] = u32x4{x[0], y[0], x[1], y[1]};
+  }
+}
+
+// Forward: a wave has 32 columns of both halves.  Rows come straight into operand registers
+// (a lane a row), the next block's on their way meanwhile.
+template <int ACT>
+__global__ __launch_bounds__(256, 2) void glu_narrow_fwd_kernel(GluArgs a) {
+  __shared__ __attribute__((aligned(16))) char lds[2 * 128 * 256];
+  stage_w<256>(a, lds);
+  __syncthreads();
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
+  const int c0 = 32 * wave;
+  if (c0 >= a.f) return;
+  bf16x8 wa[8], wb[8];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    wa[t] = Square::across(lds, c0, 16 * t, lane);
+    wb[t] = Square::across(lds + 128 * 256, c0, 16 * t, lane);
+  }
+  f32x16 ba{}, bb{};
+  if (a.bias) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int c = c0 + acc_row(v, g);
+      if (c < a.f) {
+        ba[v] = (float)((const bf16*)a.bias)[c];
+        bb[v] = (float)((const bf16*)a.bias)[a.f + c];
+      }
+    }
+  }
+  bf16x8 x[8];
+  auto load = [&](int64_t r0) {
+    const int64_t left = a.m - r0;
+    const int rows = left < 0 ? 0 : left < GLU_ROWS ? (int)left : GLU_ROWS;
+    const rsrc_t rs = buf_rsrc_n((const bf16*)a.x + r0 * a.k, (uint32_t)(rows * a.k) * 2u);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const int c = 16 * t + 8 * g;
+      const uint32_t off = c < a.k ? (uint32_t)((lane & 31) * a.k + c) * 2u : 0x80000000u;
+      x[t] = __builtin_bit_cast(bf16x8,
+                                __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, 0, 0));
+    }
+  };
+  const int64_t step = (int64_t)gridDim.x * GLU_ROWS;
+  int64_t r0 = (int64_t)blockIdx.x * GLU_ROWS;
+  load(r0);
+  for (; r0 < a.m; r0 += step) {
+    f32x16 za = ba, zb = bb;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      za = Mma<bf16>::mma(wa[t], x[t], za);
+      zb = Mma<bf16>::mma(wb[t], x[t], zb);
+    }
+    load(r0 + step);
+    u32x2 q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = gate_value<bf16>(za[4 * i + e], ACT) * zb[4 * i + e];
+      q[i] = pack4(o[0], o[1], o[2], o[3]);
+    }
+    u32x4 w[2];
+    row_words(q, w);
+    const int64_t r = r0 + (lane & 31);
+    bf16* out = (bf16*)a.out + r * a.f + c0 + 16 * g;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (r < a.m && c0 + 16 * g + 8 * u < a.f) *(u32x4*)(out + 8 * u) = w[u];
+  }
+}
+
+// Backward: eight waves on a block of 32 rows.
+//   z    a wave has 16 columns of either half (one tile: rows 0 .. 15 a, 16 .. 31 b, so that a
+//        lane has a and b of the same output); dz goes to LDS in three planes;
+//   dW   32 columns of dz a wave, all of k, in registers to the end;
+//   dx   a tile of 32 of k and one half of dz's columns a wave; the halves meet in LDS.
+// 48 of a wave's 56 matrix instructions a block are the three planes' (24 bits of dz).
+constexpr int GLU_BWD_WG = 512;
+template <int ACT>
+__global__ __launch_bounds__(GLU_BWD_WG) void glu_narrow_bwd_kernel(GluArgs a, LinBwdArgs o) {
+  constexpr int LINES = GLU_ROWS * 256;  // bytes of 32 lines of 128 bf16
+  // W first; then x (two buffers), dz (three planes of two halves), the halves of dx
+  constexpr int X = 0, Z = 2 * LINES, P = Z + 6 * LINES;
+  __shared__ __attribute__((aligned(16))) char lds[P + 4 * 64 * 16 * 4];
+  static_assert(sizeof(lds) >= 2 * 128 * 256, "room for W");
+  stage_w<GLU_BWD_WG>(a, lds);
+  __syncthreads();
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
+  const int kt = 32 * (wave & 3), half = wave >> 2;  // of dx
+  bf16x8 wz[8], wx[8];
+  {
+    const char* mine = lds + (lane & 16 ? 128 * 256 : 0);
+    const int i = lane & 15, col = 16 * wave + 4 * (i & 3);
+    typedef TRIATTN_LDS s16x4* lds4;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const int line = 16 * t + 8 * g + (i >> 2);
+      const char* p = mine + Square::chunk_at(line, col >> 3) + (col & 4) * 2;
+      const char* q = mine + Square::chunk_at(line + 4, col >> 3) + (col & 4) * 2;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(uintptr_t)lds_addr(p));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(uintptr_t)lds_addr(q));
+      wz[t] = __builtin_bit_cast(bf16x8,
+                                 __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      wx[t] = Square::along(lds + half * 128 * 256, kt, 16 * t, lane);
+    }
+  }
+  f32x16 bias{};
+  if (a.bias) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int c = 16 * wave + acc_row(v & 7, g);
+      if (c < a.f) bias[v] = (float)((const bf16*)a.bias)[(v >> 3) * a.f + c];
+    }
+  }
+  // this thread's chunk of x, and its row's dout (columns of its part of dz)
+  const int line = threadIdx.x / 16, chunk = threadIdx.x % 16;
+  u32x4 x;
+  u32x2 dy[2];
+  auto load = [&](int64_t r0) {
+    const int64_t left = a.m - r0;
+    const int rows = left < 0 ? 0 : left < GLU_ROWS ? (int)left : GLU_ROWS;
+    const rsrc_t rx = buf_rsrc_n((const bf16*)a.x + r0 * a.k, (uint32_t)(rows * a.k) * 2u);
+    const uint32_t off = 8 * chunk < a.k ? (uint32_t)(line * a.k + 8 * chunk) * 2u : 0x80000000u;
+    x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, (int)off, 0, 0));
+    const rsrc_t rd = buf_rsrc_n((const bf16*)a.dout + r0 * a.f, (uint32_t)(rows * a.f) * 2u);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int c = 16 * wave + 8 * i + 4 * g;
+      const uint32_t at = c < a.f ? (uint32_t)((lane & 31) * a.f + c) * 2u : 0x80000000u;
+      dy[i] = __builtin_bit_cast(u32x2,
+                                 __builtin_amdgcn_raw_buffer_load_b64(rd, (int)at, 0, 0));
+    }
+  };
+  f32x16 gw[4] = {};
+  f32x16 col{};  // this lane's rows' sums of dz
+  const int64_t step = (int64_t)gridDim.x * GLU_ROWS;
+  int64_t r0 = (int64_t)blockIdx.x * GLU_ROWS;
+  load(r0);
+  __syncthreads();  // W has been read
+  int buf = 0;
+  for (; r0 < a.m; r0 += step, buf ^= 1) {
+    char* tx = lds + X + buf * LINES;
+    *(u32x4*)(tx + Square::chunk_at(line, chunk)) = x;
+    float d[8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const bf16x4 y = __builtin_bit_cast(bf16x4, dy[i]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) d[4 * i + e] = (float)y[e];
+    }
+    __syncthreads();
+    load(r0 + step);
+    f32x16 z = bias;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) z = Mma<bf16>::mma(wz[t], Square::along(tx, 0, 16 * t, lane), z);
+#pragma unroll
+    for (int v = 0; v < 8; ++v) {
+      float value, slope;
+      act_both<bf16>(z[v], ACT, value, slope);
+      z[v] = d[v] * z[v + 8] * slope;
+      z[v + 8] = d[v] * value;
+    }
+    col += z;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float f[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = z[8 * h + 4 * i + e];
+        char* to = lds + Z + h * LINES + Square::chunk_at(lane & 31, 2 * wave + i) + 8 * g;
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+          bf16x4 b;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            b[e] = (bf16)f[e];
+            if (p < 2) f[e] -= (float)b[e];
+          }
+          *(bf16x4*)(to + 2 * p * LINES) = b;
+        }
+      }
+    __syncthreads();
+    if (o.dw) {
+      // columns 32 (wave % 4) of half wave / 4
+#pragma unroll
+      for (int kk = 0; kk < GLU_ROWS; kk += 16) {
+        bf16x8 fx[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) fx[u] = Square::across(tx, 32 * u, kk, lane);
+#pragma unroll
+        for (int p = 2; p >= 0; --p) {
+          const bf16x8 fz = Square::across(lds + Z + (2 * p + half) * LINES, kt, kk, lane);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) gw[u] = Mma<bf16>::mma(fz, fx[u], gw[u]);
+        }
+      }
+    }
+    if (o.dx) {
+      f32x16 gx{};
+#pragma unroll
+      for (int p = 2; p >= 0; --p)
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+          gx = Mma<bf16>::mma(
+              wx[t], Square::along(lds + Z + (2 * p + half) * LINES, 0, 16 * t, lane), gx);
+      f32x4* part = (f32x4*)(lds + P) + ((wave & 3) * 64 + lane) * 4;
+      if (half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          part[i ^ (lane & 3)] =
+              f32x4{gx[4 * i], gx[4 * i + 1], gx[4 * i + 2], gx[4 * i + 3]};
+      }
+      __syncthreads();
+      if (!half) {
+        u32x2 q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 y = part[i ^ (lane & 3)];
+          q[i] = pack4(gx[4 * i] + y[0], gx[4 * i + 1] + y[1], gx[4 * i + 2] + y[2],
+                       gx[4 * i + 3] + y[3]);
+        }
+        u32x4 w[2];
+        row_words(q, w);
+        const int64_t r = r0 + (lane & 31);
+        bf16* dx = (bf16*)o.dx + r * a.k + kt + 16 * g;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          if (r < a.m && kt + 16 * g + 8 * u < a.k) *(u32x4*)(dx + 8 * u) = w[u];
+      }
+    }
+  }
+  const int n = 2 * a.f;
+  float* dw = o.splits > 1 ? o.part + blockIdx.x * slab_floats(a.k, n) : o.dw;
+  float* db = o.splits > 1 ? dw + (int64_t)a.k * n : o.dbias;
+  if (o.dw) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = 32 * u + (lane & 31);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int j = kt + 8 * q + 4 * g;
+        if (i < a.k && j < a.f)
+          *(f32x4*)(dw + (int64_t)i * n + half * a.f + j) =
+              f32x4{gw[u][4 * q], gw[u][4 * q + 1], gw[u][4 * q + 2], gw[u][4 * q + 3]};
+      }
+    }
+  }
+  if (o.dbias) {  // the 32 lanes of a half hold rows of the same columns
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      float s = col[v];
+      for (int i = 1; i < 32; i *= 2) s += __shfl_xor(s, i);
+      const int c = 16 * wave + acc_row(v & 7, g);
+      if ((lane & 31) == 0 && c < a.f) db[(v >> 3) * a.f + c] = s;
+    }
+  }
+}
+
+// f(constant) for the activation: one inside a row's loop would branch for every value.
+template <typename F>
+void with_act(int act, F f) {
+  switch (act) {
+    case TRIATTN_ACT_NONE: f(std::integral_constant<int, TRIATTN_ACT_NONE>()); break;
+    case TRIATTN_ACT_RELU: f(std::integral_constant<int, TRIATTN_ACT_RELU>()); break;
+    case TRIATTN_ACT_GELU: f(std::integral_constant<int, TRIATTN_ACT_GELU>()); break;
+    case TRIATTN_ACT_SILU: f(std::integral_constant<int, TRIATTN_ACT_SILU>()); break;
+    default: f(std::integral_constant<int, TRIATTN_ACT_SIGMOID>());
+  }
+}
+
+bool narrow(int dtype, int k, int f) {
+  return dtype == TRIATTN_BF16 && k <= 128 && f <= 128 && k % 8 == 0 && f % 8 == 0;
+}
+// Workgroups of the narrow kernels: one a CU backward, two forward, with blocks for all.
+int narrow_wgs(int64_t m, int most) {
+  const int64_t blocks = (m + GLU_ROWS - 1) / GLU_ROWS;
+  return (int)(blocks < most ? blocks : most);
+}
+
 template <typename T, bool DZ>
 hipError_t launch(const GluArgs& a, hipStream_t s) {
   KernelTimer t(DZ ? K_GLU_DZ : K_GLU_FWD, s);
@@ -112,10 +429,37 @@ hipError_t launch(const GluArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_glu_fwd(int dtype, const GluArgs& a, hipStream_t s) {
+  if (narrow(dtype, a.k, a.f)) {
+    KernelTimer t(K_GLU_FWD, s);
+    const dim3 grid(narrow_wgs(a.m, 512)), wg(256);
+    with_act(a.act, [&](auto act) {
+      hipLaunchKernelGGL((glu_narrow_fwd_kernel<decltype(act)::value>), grid, wg, 0, s, a);
+    });
+    return hipGetLastError();
+  }
   return dtype == TRIATTN_BF16 ? launch<bf16, false>(a, s) : launch<float, false>(a, s);
 }
-hipError_t launch_glu_dz(int dtype, const GluArgs& a, hipStream_t s) {
-  return dtype == TRIATTN_BF16 ? launch<bf16, true>(a, s) : launch<float, true>(a, s);
+
+LinBwdPlan glu_bwd_plan(int dtype, int64_t m, int k, int f) {
+  if (!narrow(dtype, k, f)) return lin_made_plan(dtype, m, k, 2 * f);
+  LinBwdPlan p{};
+  p.splits = narrow_wgs(m, 256);
+  if (p.splits > 1) p.part = lin_slab_bytes(k, 2 * f, p.splits);
+  return p;
+}
+hipError_t launch_glu_bwd(int dtype, const GluArgs& a, const LinBwdArgs& b, hipStream_t s) {
+  if (narrow(dtype, a.k, a.f)) {
+    {
+      KernelTimer t(K_GLU_DZ, s);
+      const dim3 grid(b.splits), wg(GLU_BWD_WG);
+      with_act(a.act, [&](auto act) {
+        hipLaunchKernelGGL((glu_narrow_bwd_kernel<decltype(act)::value>), grid, wg, 0, s, a, b);
+      });
+    }
+    return (b.dw || b.dbias) && b.splits > 1 ? launch_lin_reduce(b, s) : hipGetLastError();
+  }
+  const hipError_t e = dtype == TRIATTN_BF16 ? launch<bf16, true>(a, s) : launch<float, true>(a, s);
+  return e != hipSuccess ? e : launch_lin_made(dtype, b, s);
 }
 
 }  // namespace triattn

@@ -145,11 +145,6 @@ __host__ __device__ inline int64_t split_rows(int64_t m, int splits) {
   const int64_t per = (m + splits - 1) / splits;
   return (per + 63) / 64 * 64;
 }
-// Floats of one split's partial sums: dw, then dbias.
-__host__ __device__ inline int64_t slab_floats(int k, int n) {
-  return ((int64_t)k * n + n + 3) / 4 * 4;
-}
-
 // One split's dW tile and, in the first row of tiles, its dbias.  Without splits the
 // results themselves.  The rows are split so that the GPU is full although dW has few tiles.
 template <typename T, int R, int DZ, bool ALIGNED>
@@ -231,31 +226,6 @@ __global__ __launch_bounds__(256) void lin_bwd_both_kernel(LinBwdArgs a, int ndx
 // of ragged rows would not fit the registers beside two times 128 rows.
 // 589,824 x 128 x 128: 85 us (5.3 TB/s of x, dout and dx) and 6 for the sums of 256 slabs, where
 // the two kernels above and their sums take 143.
-struct Square {  // lines of 128 bf16, read along and across
-  // Both reads are free of bank conflicts: s differs between any 16 consecutive lines
-  // (its low three bits between 8) for 16-byte reads down the lines, and its bits 3, 2 as
-  // well as its bits 2, 1 between the four lines of a transposing read.
-  __device__ static inline int chunk_at(int line, int c) {
-    const int e = line & 3, s = ((e ^ (e << 1)) << 1) ^ ((line >> 2) & 3);
-    return (line * 16 + (c ^ s)) * 16;
-  }
-  // lines r0 .. + 31 as rows, columns k0 .. + 15 as indices
-  __device__ static inline bf16x8 along(const char* t, int r0, int k0, int lane) {
-    return *(const bf16x8*)(t + chunk_at(r0 + (lane & 31), (k0 >> 3) + (lane >> 5)));
-  }
-  // columns r0 .. + 31 as rows, lines k0 .. + 15 as indices
-  __device__ static inline bf16x8 across(const char* t, int r0, int k0, int lane) {
-    const int i = lane & 15, col = r0 + (lane & 16) + 4 * (i & 3);
-    const int line = k0 + 8 * (lane >> 5) + (i >> 2);
-    typedef TRIATTN_LDS s16x4* lds4;
-    const char* a = t + chunk_at(line, col >> 3) + (col & 4) * 2;
-    const char* b = t + chunk_at(line + 4, col >> 3) + (col & 4) * 2;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(uintptr_t)lds_addr(a));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(uintptr_t)lds_addr(b));
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-  }
-};
-
 constexpr int NARROW_WG = 512;
 constexpr int narrow_rows(int dz, bool aligned) {
   return dz == DZ_ACT || !aligned ? 64 : 128;
@@ -623,6 +593,10 @@ LinBwdPlan lin_bwd_plan(int dtype, int64_t m, int k, int n, int act) {
   return p;
 }
 
+hipError_t launch_lin_reduce(const LinBwdArgs& a, hipStream_t s) { return reduce(a, s); }
+size_t lin_slab_bytes(int k, int n, int splits) {
+  return (size_t)splits * (size_t)slab_floats(k, n) * sizeof(float);
+}
 LinBwdPlan lin_made_plan(int dtype, int64_t m, int k, int n) {
   LinBwdPlan p{};
   p.splits = dtype == TRIATTN_BF16 ? dw_splits<bf16>(m, k, n, TRIATTN_ACT_SILU)

@@ -603,5 +603,35 @@ constexpr int planes() {
   return sizeof(T) == 2 ? 1 : 3;
 }
 
+// Floats of one split's partial sums: dw, then dbias.
+__host__ __device__ inline int64_t slab_floats(int k, int n) {
+  return ((int64_t)k * n + n + 3) / 4 * 4;
+}
+
+struct Square {  // lines of 128 bf16, read along and across
+  // Both reads are free of bank conflicts: s differs between any 16 consecutive lines
+  // (its low three bits between 8) for 16-byte reads down the lines, and its bits 3, 2 as
+  // well as its bits 2, 1 between the four lines of a transposing read.
+  __device__ static inline int chunk_at(int line, int c) {
+    const int e = line & 3, s = ((e ^ (e << 1)) << 1) ^ ((line >> 2) & 3);
+    return (line * 16 + (c ^ s)) * 16;
+  }
+  // lines r0 .. + 31 as rows, columns k0 .. + 15 as indices
+  __device__ static inline bf16x8 along(const char* t, int r0, int k0, int lane) {
+    return *(const bf16x8*)(t + chunk_at(r0 + (lane & 31), (k0 >> 3) + (lane >> 5)));
+  }
+  // columns r0 .. + 31 as rows, lines k0 .. + 15 as indices
+  __device__ static inline bf16x8 across(const char* t, int r0, int k0, int lane) {
+    const int i = lane & 15, col = r0 + (lane & 16) + 4 * (i & 3);
+    const int line = k0 + 8 * (lane >> 5) + (i >> 2);
+    typedef TRIATTN_LDS s16x4* lds4;
+    const char* a = t + chunk_at(line, col >> 3) + (col & 4) * 2;
+    const char* b = t + chunk_at(line + 4, col >> 3) + (col & 4) * 2;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(uintptr_t)lds_addr(a));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(uintptr_t)lds_addr(b));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
 }  // namespace
 }  // namespace triattn

@@ -70,6 +70,9 @@ hipError_t launch_lin_bwd(int dtype, const LinBwdArgs& a, hipStream_t s);
 // The products of a backward whose dz [m][n] is made already (a.dz; act, z and dout unused).
 LinBwdPlan lin_made_plan(int dtype, int64_t m, int k, int n);
 hipError_t launch_lin_made(int dtype, const LinBwdArgs& a, hipStream_t s);
+// Slabs of partial sums (dw, then dbias) and their sum.
+size_t lin_slab_bytes(int k, int n, int splits);
+hipError_t launch_lin_reduce(const LinBwdArgs& a, hipStream_t s);
 
 // ---- gated linear projection (glu.hip) -------------------------------------------------------
 constexpr int GLU_MAX_F = 4096;
@@ -84,7 +87,9 @@ struct GluArgs {
   float* dz;                    // backward, workspace: [m][2 f]
 };
 hipError_t launch_glu_fwd(int dtype, const GluArgs& a, hipStream_t s);
-hipError_t launch_glu_dz(int dtype, const GluArgs& a, hipStream_t s);
+// The backward: b holds its results (n = 2 f), slabs and dz, as the plan sizes them.
+LinBwdPlan glu_bwd_plan(int dtype, int64_t m, int k, int f);
+hipError_t launch_glu_bwd(int dtype, const GluArgs& a, const LinBwdArgs& b, hipStream_t s);
 
 // ---- norm and clipping of gradients (grad.hip) ------------------------------------------------
 // Tensors of a launch: their addresses and sizes travel in its arguments.

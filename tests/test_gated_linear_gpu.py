@@ -41,7 +41,8 @@ def both(m, k, f, act, dtype, seed=0, bias=True):
 # outputs), halves that are no whole 16-byte words of rows that are; few and many rows
 SIZES = [(1, 1, 1), (1, 384, 1024), (3, 7, 5), (64, 64, 32), (65, 33, 33), (130, 128, 128),
          (777, 129, 211), (100, 40, 4), (100, 40, 12), (50, 300, 1), (37, 8, 500), (4100, 96, 64),
-         (2000, 24, 150), (20000, 16, 8), (9, 1000, 65), (33000, 128, 64), (256, 256, 20)]
+         (2000, 24, 150), (20000, 16, 8), (9, 1000, 65), (33000, 128, 64), (256, 256, 20),
+         (1000, 128, 128), (33, 8, 8), (70001, 64, 24), (31, 120, 104), (40, 16, 128)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F4])
@@ -59,7 +60,8 @@ def test_activations(size, act, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F4])
-@pytest.mark.parametrize("size", [(70, 64, 40), (129, 33, 37), (5000, 128, 64)], ids=str)
+@pytest.mark.parametrize("size", [(70, 64, 40), (129, 33, 37), (5000, 128, 64), (9000, 128, 128),
+                                  (300, 136, 72)], ids=str)
 def test_nothing_outside_the_outputs_is_written(size, dtype):
     m, k, f = size
     x, w, b, dy = (dev(t) for t in inputs(m, k, f, dtype, 1))

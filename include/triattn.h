@@ -469,7 +469,7 @@ int tri_cross_attn_bwd(int dtype, int64_t batch, int64_t nq, int64_t nk, int64_t
 int tri_gated_linear_fwd(int dtype, int64_t m, int64_t k, int64_t f, int act, const void* x,
                          const void* w, const void* bias, void* out, void* stream);
 
-/* Bytes of device workspace tri_gated_linear_bwd needs for these sizes (8 m f for dz in fp32,
+/* Bytes of device workspace tri_gated_linear_bwd needs for these sizes (12 m f for dz,
  * and partial sums). */
 int tri_gated_linear_bwd_workspace_bytes(int dtype, int64_t m, int64_t k, int64_t f,
                                          size_t* bytes);

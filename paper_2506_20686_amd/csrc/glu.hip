@@ -4,7 +4,8 @@
 // halves, 8 and 8 in turn, so that a thread ends with a and b of the same outputs and neither is
 // written.  The backward forms them again, with
 //   da = dout b act'(a),  db = dout act(a)
-// in the product's epilogue, as dz = [da | db] in fp32; dx = dz W^T, dW = x^T dz and the sums of
+// in the product's epilogue, as dz = [da | db] in 24 bits, three planes of bf16 where rows are
+// whole words (6 bytes an element moved, but a tile that reads dz need not split it), else fp32; dx = dz W^T, dW = x^T dz and the sums of
 // dz are the linear projection's products.
 #include "lin_tile.h"
 #include "timing.h"
@@ -38,6 +39,25 @@ __device__ inline float gate_value(float z, int act) {
   float p, q;
   sigmoid<sizeof(T) == 4>(z, p, q);
   return p;
+}
+
+// The first `have` (whole words) of 8 values as three planes of bf16, `plane` elements apart.
+__device__ inline void put_planes(bf16* p, int64_t plane, int have, float (&f)[8]) {
+#pragma unroll
+  for (int u = 0; u < 3; ++u) {
+    struct B {
+      bf16 e[8];
+    } b;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      b.e[e] = (bf16)f[e];
+      if (u < 2) f[e] -= (float)b.e[e];
+    }
+    const u32x4 w = __builtin_bit_cast(u32x4, b);
+    // (fp32's whole words are 4 elements: half a word here, and the second half may start there)
+    if (have >= 8) ((Any16*)(p + u * plane))->v = w;
+    else if (have > 0) *(u32x2*)(p + u * plane) = u32x2{w[0], w[1]};
+  }
 }
 
 template <typename T, int R, bool ALIGNED, bool DZ>
@@ -82,9 +102,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void glu_kernel(GluArg
         za[e] = d[e] * zb[e] * slope;
         zb[e] = d[e] * value;
       }
-      float* dz = a.dz + i * 2 * a.f + j;
-      put8<float, ALIGNED>(dz, have, za);
-      put8<float, ALIGNED>(dz + a.f, have, zb);
+      const int64_t at = i * 2 * a.f + j;
+      if constexpr (ALIGNED) {
+        bf16* dz = (bf16*)a.dz + at;
+        put_planes(dz, a.m * 2 * a.f, have, za);
+        put_planes(dz + a.f, a.m * 2 * a.f, have, zb);
+      } else {
+        put8<float, false>(a.dz + at, have, za);
+        put8<float, false>(a.dz + at + a.f, have, zb);
+      }
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) za[e] = gate_value<T>(za[e], a.act) * zb[e];
@@ -133,7 +159,7 @@ __device__ inline void row_words(const u32x2 (&q)[4], u32x4 (&w)[2]) {
 }
 
 // Forward: a wave has 32 columns of both halves.  Rows come straight into operand registers
-// (a lane a row), the next block's on their way meanwhile.
+// (a lane a row), those of the next two blocks on their way meanwhile.
 template <int ACT>
 __global__ __launch_bounds__(256, 2) void glu_narrow_fwd_kernel(GluArgs a) {
   __shared__ __attribute__((aligned(16))) char lds[2 * 128 * 256];
@@ -159,8 +185,8 @@ __global__ __launch_bounds__(256, 2) void glu_narrow_fwd_kernel(GluArgs a) {
       }
     }
   }
-  bf16x8 x[8];
-  auto load = [&](int64_t r0) {
+  bf16x8 x[2][8];
+  auto load = [&](int d, int64_t r0) {
     const int64_t left = a.m - r0;
     const int rows = left < 0 ? 0 : left < GLU_ROWS ? (int)left : GLU_ROWS;
     const rsrc_t rs = buf_rsrc_n((const bf16*)a.x + r0 * a.k, (uint32_t)(rows * a.k) * 2u);
@@ -168,21 +194,19 @@ __global__ __launch_bounds__(256, 2) void glu_narrow_fwd_kernel(GluArgs a) {
     for (int t = 0; t < 8; ++t) {
       const int c = 16 * t + 8 * g;
       const uint32_t off = c < a.k ? (uint32_t)((lane & 31) * a.k + c) * 2u : 0x80000000u;
-      x[t] = __builtin_bit_cast(bf16x8,
+      x[d][t] = __builtin_bit_cast(bf16x8,
                                 __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, 0, 0));
     }
   };
   const int64_t step = (int64_t)gridDim.x * GLU_ROWS;
-  int64_t r0 = (int64_t)blockIdx.x * GLU_ROWS;
-  load(r0);
-  for (; r0 < a.m; r0 += step) {
+  auto block = [&](int d, int64_t r0) {
     f32x16 za = ba, zb = bb;
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
-      za = Mma<bf16>::mma(wa[t], x[t], za);
-      zb = Mma<bf16>::mma(wb[t], x[t], zb);
+      za = Mma<bf16>::mma(wa[t], x[d][t], za);
+      zb = Mma<bf16>::mma(wb[t], x[d][t], zb);
     }
-    load(r0 + step);
+    load(d, r0 + 2 * step);
     u32x2 q[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -198,6 +222,13 @@ __global__ __launch_bounds__(256, 2) void glu_narrow_fwd_kernel(GluArgs a) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
       if (r < a.m && c0 + 16 * g + 8 * u < a.f) *(u32x4*)(out + 8 * u) = w[u];
+  };
+  const int64_t r1 = (int64_t)blockIdx.x * GLU_ROWS;
+  load(0, r1);
+  load(1, r1 + step);
+  for (int64_t r0 = r1; r0 < a.m; r0 += 2 * step) {
+    block(0, r0);
+    if (r0 + step < a.m) block(1, r0 + step);
   }
 }
 
@@ -410,10 +441,16 @@ int narrow_wgs(int64_t m, int most) {
   return (int)(blocks < most ? blocks : most);
 }
 
+// Rows of every tensor, and the halves of W's, are whole 16-byte words.
+bool whole(int dtype, int k, int f) {
+  const int word = dtype == TRIATTN_BF16 ? WORD<bf16> : WORD<float>;
+  return k % word == 0 && f % word == 0;
+}
+
 template <typename T, bool DZ>
 hipError_t launch(const GluArgs& a, hipStream_t s) {
   KernelTimer t(DZ ? K_GLU_DZ : K_GLU_FWD, s);
-  const bool al = a.k % WORD<T> == 0 && a.f % WORD<T> == 0;
+  const bool al = whole(sizeof(T) == 2 ? TRIATTN_BF16 : TRIATTN_F32, a.k, a.f);
   // 128-wide tiles where there are enough of them for the 256 CUs, as in the linear projection
   const bool big = (al || sizeof(T) == 2) && a.f > 32 &&
                    (a.m + 127) / 128 * ((a.f + 63) / 64) >= 256 && (sizeof(T) == 2 || a.k >= 256);
@@ -441,7 +478,7 @@ hipError_t launch_glu_fwd(int dtype, const GluArgs& a, hipStream_t s) {
 }
 
 LinBwdPlan glu_bwd_plan(int dtype, int64_t m, int k, int f) {
-  if (!narrow(dtype, k, f)) return lin_made_plan(dtype, m, k, 2 * f);
+  if (!narrow(dtype, k, f)) return lin_made_plan(dtype, m, k, 2 * f, whole(dtype, k, f));
   LinBwdPlan p{};
   p.splits = narrow_wgs(m, 256);
   if (p.splits > 1) p.part = lin_slab_bytes(k, 2 * f, p.splits);
@@ -459,7 +496,7 @@ hipError_t launch_glu_bwd(int dtype, const GluArgs& a, const LinBwdArgs& b, hipS
     return (b.dw || b.dbias) && b.splits > 1 ? launch_lin_reduce(b, s) : hipGetLastError();
   }
   const hipError_t e = dtype == TRIATTN_BF16 ? launch<bf16, true>(a, s) : launch<float, true>(a, s);
-  return e != hipSuccess ? e : launch_lin_made(dtype, b, s);
+  return e != hipSuccess ? e : launch_lin_made(dtype, b, whole(dtype, a.k, a.f), s);
 }
 
 }  // namespace triattn

@@ -93,6 +93,12 @@ struct DzSource<T, DZ_MADE> {
   static constexpr int STAGE = DZ_X, P = 3;
 };
 
+template <typename T>
+struct DzSource<T, DZ_PLANES> {
+  using E = bf16;
+  static constexpr int STAGE = DZ_PLANES, P = 3;
+};
+
 // dz = dout act'(z) in fp32, where several column tiles of dx and dW would each form it again from
 // the two tensors (an exponential an element).  Bound by memory and a launch: 1500 x 1536 in 8.5
 // us; 1500 x 384 x 1536 backward with it 41 us, without 71; 16,384 x 512 x 2048 with it 271,
@@ -128,7 +134,7 @@ __device__ inline void dx_tile(const LinBwdArgs& a, char* lds, int wg) {
   const int nj = (a.k + R - 1) / R;
   const int64_t i0 = (int64_t)(wg / nj) * R;
   const int j0 = (wg % nj) * R;
-  const E* src = DZ == DZ_MADE ? (const E*)a.dz : (const E*)a.dout;
+  const E* src = DZ >= DZ_MADE ? (const E*)a.dz : (const E*)a.dout;
   f32x16 acc[G::NT][G::NT];
   float none[8];
   G::run(lds, Mat<E>{src, a.m, a.n}, (const E*)a.z, Mat<T>{(const T*)a.w, a.k, a.n}, nullptr,
@@ -165,7 +171,7 @@ __device__ inline void dw_tile(const LinBwdArgs& a, char* lds, int wg) {
   float* db = a.splits > 1 ? dw + (int64_t)a.k * a.n : a.dbias;
   f32x16 acc[G::NT][G::NT];
   float col[8] = {};
-  const E* src = DZ == DZ_MADE ? (const E*)a.dz : (const E*)a.dout;
+  const E* src = DZ >= DZ_MADE ? (const E*)a.dz : (const E*)a.dout;
   G::run(lds, Mat<T>{(const T*)a.x, a.m, a.k}, nullptr, Mat<E>{src, a.m, a.n}, (const E*)a.z,
          a.act, i0, j0, k0, k1, sum, col, acc);
   const int j = j0 + G::piece_col(), have = a.n - j;
@@ -545,8 +551,9 @@ hipError_t bwd_narrow(const LinBwdArgs& a, hipStream_t s) {
 
 // The products with a dz that is in the workspace.
 template <typename T>
-hipError_t bwd_made(const LinBwdArgs& a, hipStream_t s) {
-  bwd_align<T, DZ_MADE>(a, s);
+hipError_t bwd_made(const LinBwdArgs& a, bool planes, hipStream_t s) {
+  if (planes) bwd_launch<T, DZ_PLANES, true>(a, s);
+  else bwd_launch<T, DZ_MADE, false>(a, s);
   return (a.dw || a.dbias) && a.splits > 1 ? reduce(a, s) : hipGetLastError();
 }
 
@@ -597,12 +604,12 @@ hipError_t launch_lin_reduce(const LinBwdArgs& a, hipStream_t s) { return reduce
 size_t lin_slab_bytes(int k, int n, int splits) {
   return (size_t)splits * (size_t)slab_floats(k, n) * sizeof(float);
 }
-LinBwdPlan lin_made_plan(int dtype, int64_t m, int k, int n) {
+LinBwdPlan lin_made_plan(int dtype, int64_t m, int k, int n, bool planes) {
   LinBwdPlan p{};
   p.splits = dtype == TRIATTN_BF16 ? dw_splits<bf16>(m, k, n, TRIATTN_ACT_SILU)
                                    : dw_splits<float>(m, k, n, TRIATTN_ACT_SILU);
   if (p.splits > 1) p.part = (size_t)p.splits * (size_t)slab_floats(k, n) * sizeof(float);
-  p.dz = (size_t)m * n * sizeof(float);
+  p.dz = (size_t)m * n * (planes ? 3 * sizeof(bf16) : sizeof(float));
   return p;
 }
 
@@ -612,8 +619,8 @@ hipError_t launch_lin_fwd(int dtype, const LinArgs& a, hipStream_t s) {
 hipError_t launch_lin_bwd(int dtype, const LinBwdArgs& a, hipStream_t s) {
   return dtype == TRIATTN_BF16 ? bwd<bf16>(a, s) : bwd<float>(a, s);
 }
-hipError_t launch_lin_made(int dtype, const LinBwdArgs& a, hipStream_t s) {
-  return dtype == TRIATTN_BF16 ? bwd_made<bf16>(a, s) : bwd_made<float>(a, s);
+hipError_t launch_lin_made(int dtype, const LinBwdArgs& a, bool planes, hipStream_t s) {
+  return dtype == TRIATTN_BF16 ? bwd_made<bf16>(a, planes, s) : bwd_made<float>(a, planes, s);
 }
 
 }  // namespace triattn

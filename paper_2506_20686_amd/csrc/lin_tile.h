@@ -289,9 +289,10 @@ struct Tile {
   }
 };
 
-// What dz is made of in the staging: the tensor itself; dout where z > 0; dout act'(z); and
-// (not in the staging) dz made beforehand.
-enum Dz { DZ_X, DZ_RELU, DZ_ACT, DZ_MADE };
+// What dz is made of in the staging: the tensor itself; dout where z > 0; dout act'(z); (not in
+// the staging) dz made beforehand; or made and split beforehand, its planes of bf16 one after
+// the other.
+enum Dz { DZ_X, DZ_RELU, DZ_ACT, DZ_MADE, DZ_PLANES };
 
 // Staging of one operand: this thread's chunks of a tile, from memory to LDS.  GATED: the
 // matrix is two side by side (cols / 2 columns each), and a tile holds R / 2 columns of both, 8
@@ -300,7 +301,9 @@ template <typename T, int R, int BK, bool KM, int P, int DZ, bool ALIGNED, bool 
 struct Stage {
   using L = Tile<R, BK, KM, P>;
   static constexpr int N = R * BK / 8 / 256;  // chunks a thread
-  Raw8<T> x[N], z[DZ == DZ_X ? 1 : N];
+  static constexpr bool SPLIT = DZ == DZ_PLANES, WITH_Z = DZ == DZ_RELU || DZ == DZ_ACT;
+  static_assert(!SPLIT || ALIGNED, "planes of whole words");
+  Raw8<T> x[SPLIT ? P * N : N], z[WITH_Z ? N : 1];
   int info[ALIGNED ? 1 : N];
 
   // Tile at rows i0, indices k0 (of k1): lines are rows (K major) or indices.
@@ -314,14 +317,19 @@ struct Stage {
       const int c = GATED ? 8 * (ch >> 1) + (ch & 1) * half : 8 * ch;
       const int64_t r0 = KM ? i0 : k0;
       const int c0 = (int)(KM ? k0 : i0);
-      if constexpr (ALIGNED) {
+      if constexpr (SPLIT) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+          x[P * u + p] = fetch<T>(Mat<T>{m.p + p * m.rows * m.cols, w.rows, w.cols}, r0, c0,
+                                  KM ? R : BK, line, c);
+      } else if constexpr (ALIGNED) {
         x[u] = fetch<T>(w, r0, c0, KM ? R : BK, line, c);
-        if constexpr (DZ != DZ_X)
+        if constexpr (WITH_Z)
           z[u] = fetch<T>(Mat<T>{zp, w.rows, w.cols}, r0, c0, KM ? R : BK, line, c);
       } else {
         const int lim = KM ? R : (int)(k1 - k0 < BK ? k1 - k0 : BK);
         x[u] = fetch_any<T>(w, r0, c0, lim, line, c, info[u], half);
-        if constexpr (DZ != DZ_X) {
+        if constexpr (WITH_Z) {
           int same;
           z[u] = fetch_any<T>(Mat<T>{zp, w.rows, w.cols}, r0, c0, lim, line, c, same);
         }
@@ -334,8 +342,16 @@ struct Stage {
   }
   // The values of chunk u.
   __device__ inline void values(int u, int act, float (&f)[8]) const {
-    unpack(raw(x[u], u), f);
-    if constexpr (DZ != DZ_X) {
+    unpack(raw(x[SPLIT ? P * u : u], u), f);
+    if constexpr (SPLIT) {  // the smaller planes together first
+      float g[8], h[8];
+      static_assert(P == 3, "planes");
+      unpack(x[P * u + 1], g);
+      unpack(x[P * u + 2], h);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] += g[e] + h[e];
+    }
+    if constexpr (WITH_Z) {
       float g[8];
       unpack(raw(z[u], u), g);
 #pragma unroll
@@ -352,12 +368,15 @@ struct Stage {
       const int id = (int)threadIdx.x + 256 * u;
       char* d = tile + L::chunk_at(id / L::LINE, id % L::LINE);
       float f[8];
-      if (P > 1 || DZ != DZ_X || SUM) values(u, act, f);
+      if ((!SPLIT && (P > 1 || WITH_Z)) || SUM) values(u, act, f);
       if (SUM && sum) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) col[e] += f[e];
       }
-      if constexpr (P == 1 && DZ == DZ_X) {
+      if constexpr (SPLIT) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) *(u32x4*)(d + p * L::PLANE) = x[P * u + p].v[0];
+      } else if constexpr (P == 1 && DZ == DZ_X) {
         *(u32x4*)d = raw(x[u], u).v[0];
       } else {
 #pragma unroll

@@ -67,9 +67,10 @@ LinBwdPlan lin_bwd_plan(int dtype, int64_t m, int k, int n, int act);
 hipError_t launch_lin_fwd(int dtype, const LinArgs& a, hipStream_t s);
 hipError_t launch_lin_bwd(int dtype, const LinBwdArgs& a, hipStream_t s);
 
-// The products of a backward whose dz [m][n] is made already (a.dz; act, z and dout unused).
-LinBwdPlan lin_made_plan(int dtype, int64_t m, int k, int n);
-hipError_t launch_lin_made(int dtype, const LinBwdArgs& a, hipStream_t s);
+// The products of a backward whose dz [m][n] is made already (a.dz; act, z and dout unused), in
+// fp32 or, for rows of whole 16-byte words, as three planes of bf16 one after the other.
+LinBwdPlan lin_made_plan(int dtype, int64_t m, int k, int n, bool planes);
+hipError_t launch_lin_made(int dtype, const LinBwdArgs& a, bool planes, hipStream_t s);
 // Slabs of partial sums (dw, then dbias) and their sum.
 size_t lin_slab_bytes(int k, int n, int splits);
 hipError_t launch_lin_reduce(const LinBwdArgs& a, hipStream_t s);

@@ -42,7 +42,8 @@ def both(m, k, f, act, dtype, seed=0, bias=True):
 SIZES = [(1, 1, 1), (1, 384, 1024), (3, 7, 5), (64, 64, 32), (65, 33, 33), (130, 128, 128),
          (777, 129, 211), (100, 40, 4), (100, 40, 12), (50, 300, 1), (37, 8, 500), (4100, 96, 64),
          (2000, 24, 150), (20000, 16, 8), (9, 1000, 65), (33000, 128, 64), (256, 256, 20),
-         (1000, 128, 128), (33, 8, 8), (70001, 64, 24), (31, 120, 104), (40, 16, 128)]
+         (1000, 128, 128), (33, 8, 8), (70001, 64, 24), (31, 120, 104), (40, 16, 128),
+         (200, 136, 28), (90, 20, 36), (600, 200, 4)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F4])

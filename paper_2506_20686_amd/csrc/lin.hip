@@ -207,13 +207,13 @@ __global__ __launch_bounds__(256) void lin_bwd_w_kernel(LinBwdArgs a) {
 }
 // Both in one launch, where dx does not fill the GPU: the first ndx workgroups make dx, the others
 // dW (in tiles of RW).  1500 x 384 x 1536 with GELU: 28 us, where the two take 27 and 20.
-template <typename T, int RW, int DZ, bool ALIGNED>
+template <typename T, int RW, int DZ, bool ALIGNED, int RX = 64>
 __global__ __launch_bounds__(256) void lin_bwd_both_kernel(LinBwdArgs a, int ndx) {
-  constexpr int LX = DxProduct<T, 64, DZ, ALIGNED>::LDS, LW = DwProduct<T, RW, DZ, ALIGNED>::LDS;
+  constexpr int LX = DxProduct<T, RX, DZ, ALIGNED>::LDS, LW = DwProduct<T, RW, DZ, ALIGNED>::LDS;
   __shared__ __attribute__((aligned(16))) char lds[LX > LW ? LX : LW];
   const int wg = blockIdx.x, ndw = (int)gridDim.x - ndx;
   if (wg < ndx)
-    dx_tile<T, 64, DZ, ALIGNED>(a, lds, xcd_swizzle(wg, ndx));
+    dx_tile<T, RX, DZ, ALIGNED>(a, lds, xcd_swizzle(wg, ndx));
   else
     dw_tile<T, RW, DZ, ALIGNED>(a, lds, xcd_swizzle(wg - ndx, ndw));
 }
@@ -474,10 +474,22 @@ bool wide_w(int64_t m, int k, int n) {
 template <typename T, int DZ, bool AL>
 void bwd_launch(const LinBwdArgs& a, hipStream_t s) {
   const bool weights = a.dw || a.dbias, ww = wide_w(a.m, a.k, a.n);
-  const bool wx = wide<T>(a.m, a.k, a.n);
+  // with planes, 128-wide tiles of dx beside those of dW where they make up half the CUs'
+  // work: tiles of 64 read LDS as often as the matrix cores multiply
+  constexpr bool PLANES = DZ == DZ_PLANES && sizeof(T) == 2;
+  const bool beside = PLANES && ww && a.dx && weights && a.k > 64 &&
+                      tiles_of(a.m, a.k, 128) >= 96 && tiles_of(a.m, a.k, 128) < 256;
+  const bool wx = beside || wide<T>(a.m, a.k, a.n);
   const unsigned ndx = (unsigned)tiles_of(a.m, a.k, wx ? 128 : 64);
   const unsigned ndw = (unsigned)(tiles_of(a.k, a.n, ww ? 128 : 64) * a.splits);
   const dim3 wg(256), both(ndx + ndw);
+  if constexpr (PLANES) {
+    if (beside) {
+      KernelTimer t(K_LIN_BWD_BOTH, s);
+      hipLaunchKernelGGL((lin_bwd_both_kernel<T, 128, DZ, AL, 128>), both, wg, 0, s, a, (int)ndx);
+      return;
+    }
+  }
   // (and a launch holds fewer than 2^32 threads)
   if (a.dx && weights && !wx && ndx < (1u << 20)) {
     KernelTimer t(K_LIN_BWD_BOTH, s);

@@ -158,8 +158,8 @@ __device__ inline void row_words(const u32x2 (&q)[4], u32x4 (&w)[2]) {
   }
 }
 
-// Forward: a wave has 32 columns of both halves.  Rows come straight into operand registers
-// (a lane a row), those of the next two blocks on their way meanwhile.
+// Forward: a wave has 32 columns of both halves; blocks of 64 rows through LDS, the next one's on
+// their way meanwhile.
 template <int ACT>
 __global__ __launch_bounds__(256, 2) void glu_narrow_fwd_kernel(GluArgs a) {
   __shared__ __attribute__((aligned(16))) char lds[2 * 128 * 256];
@@ -167,7 +167,6 @@ __global__ __launch_bounds__(256, 2) void glu_narrow_fwd_kernel(GluArgs a) {
   __syncthreads();
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
   const int c0 = 32 * wave;
-  if (c0 >= a.f) return;
   bf16x8 wa[8], wb[8];
 #pragma unroll
   for (int t = 0; t < 8; ++t) {
@@ -185,50 +184,61 @@ __global__ __launch_bounds__(256, 2) void glu_narrow_fwd_kernel(GluArgs a) {
       }
     }
   }
-  bf16x8 x[2][8];
-  auto load = [&](int d, int64_t r0) {
+  // chunks of 64 rows, a row's 16 by 16 consecutive threads
+  constexpr int M = 2 * GLU_ROWS, N = M * 16 / 256;
+  const int chunk = threadIdx.x % 16;
+  u32x4 x[N];
+  auto load = [&](int64_t r0) {
     const int64_t left = a.m - r0;
-    const int rows = left < 0 ? 0 : left < GLU_ROWS ? (int)left : GLU_ROWS;
+    const int rows = left < 0 ? 0 : left < M ? (int)left : M;
     const rsrc_t rs = buf_rsrc_n((const bf16*)a.x + r0 * a.k, (uint32_t)(rows * a.k) * 2u);
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      const int c = 16 * t + 8 * g;
-      const uint32_t off = c < a.k ? (uint32_t)((lane & 31) * a.k + c) * 2u : 0x80000000u;
-      x[d][t] = __builtin_bit_cast(bf16x8,
-                                __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, 0, 0));
+    for (int u = 0; u < N; ++u) {
+      const int line = threadIdx.x / 16 + 16 * u;
+      const uint32_t off = 8 * chunk < a.k ? (uint32_t)(line * a.k + 8 * chunk) * 2u : 0x80000000u;
+      x[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, 0, 0));
     }
   };
-  const int64_t step = (int64_t)gridDim.x * GLU_ROWS;
-  auto block = [&](int d, int64_t r0) {
-    f32x16 za = ba, zb = bb;
+  const int64_t step = (int64_t)gridDim.x * M;
+  int64_t r0 = (int64_t)blockIdx.x * M;
+  load(r0);
+  __syncthreads();  // W has been read
+  int buf = 0;
+  for (; r0 < a.m; r0 += step, buf ^= 1) {
+    char* tx = lds + buf * M * 256;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      za = Mma<bf16>::mma(wa[t], x[d][t], za);
-      zb = Mma<bf16>::mma(wb[t], x[d][t], zb);
+    for (int u = 0; u < N; ++u)
+      *(u32x4*)(tx + Square::chunk_at(threadIdx.x / 16 + 16 * u, chunk)) = x[u];
+    load(r0 + step);
+    // this buffer was last read two blocks ago, before the barrier of the last block
+    __syncthreads();
+    if (c0 >= a.f) continue;
+#pragma unroll
+    for (int j = 0; j < M; j += 32) {
+      f32x16 za = ba, zb = bb;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const bf16x8 fx = Square::along(tx, j, 16 * t, lane);
+        za = Mma<bf16>::mma(wa[t], fx, za);
+        zb = Mma<bf16>::mma(wb[t], fx, zb);
+      }
+      u32x2 q[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          o[e] = gate_value<bf16>(za[4 * i + e], ACT) * zb[4 * i + e];
+        q[i] = pack4(o[0], o[1], o[2], o[3]);
+      }
+      u32x4 w[2];
+      row_words(q, w);
+      const int64_t r = r0 + j + (lane & 31);
+      bf16* out = (bf16*)a.out + r * a.f + c0 + 16 * g;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (r < a.m && c0 + 16 * g + 8 * u < a.f) *(u32x4*)(out + 8 * u) = w[u];
     }
-    load(d, r0 + 2 * step);
-    u32x2 q[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float o[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = gate_value<bf16>(za[4 * i + e], ACT) * zb[4 * i + e];
-      q[i] = pack4(o[0], o[1], o[2], o[3]);
-    }
-    u32x4 w[2];
-    row_words(q, w);
-    const int64_t r = r0 + (lane & 31);
-    bf16* out = (bf16*)a.out + r * a.f + c0 + 16 * g;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-      if (r < a.m && c0 + 16 * g + 8 * u < a.f) *(u32x4*)(out + 8 * u) = w[u];
-  };
-  const int64_t r1 = (int64_t)blockIdx.x * GLU_ROWS;
-  load(0, r1);
-  load(1, r1 + step);
-  for (int64_t r0 = r1; r0 < a.m; r0 += 2 * step) {
-    block(0, r0);
-    if (r0 + step < a.m) block(1, r0 + step);
   }
 }
 
@@ -468,7 +478,7 @@ hipError_t launch(const GluArgs& a, hipStream_t s) {
 hipError_t launch_glu_fwd(int dtype, const GluArgs& a, hipStream_t s) {
   if (narrow(dtype, a.k, a.f)) {
     KernelTimer t(K_GLU_FWD, s);
-    const dim3 grid(narrow_wgs(a.m, 512)), wg(256);
+    const dim3 grid(narrow_wgs((a.m + 1) / 2, 512)), wg(256);
     with_act(a.act, [&](auto act) {
       hipLaunchKernelGGL((glu_narrow_fwd_kernel<decltype(act)::value>), grid, wg, 0, s, a);
     });

@@ -259,6 +259,12 @@ struct KvStage {
   }
 };
 
+// Where the bias comes from: none; planes of it, a head each, that a launch before made; or, for
+// four heads at a time, as it lies (heads fastest).  In the last case a workgroup's four waves
+// take four heads of the same 32 rows (or keys): each stages its own head's tiles, and they
+// share the bias tile of 32 queries x 32 keys x 4 heads, whose 4 heads are one load.
+enum XatBias { XB_NONE, XB_PLANES, XB_HEADS };
+
 // Keys of a tile: 64 for workgroups of four waves where the two buffers leave room for several
 // on a CU, else 32.
 template <typename T, int DP, int NW>
@@ -268,8 +274,14 @@ constexpr int xat_keys() {
 
 // Waves of a workgroup that share staged tiles: 32 rows each.  Few rows take a wave to
 // themselves, which needs no barrier.
-inline int xat_row_waves(const XatArgs& a) { return (int64_t)a.nq * a.group <= 32 ? 1 : 4; }
-inline int xat_key_waves(const XatArgs& a) { return a.nk <= 32 ? 1 : 4; }
+// (fp32 rows of more than 64 channels would take it too many registers.)
+inline int xat_waves_for(int dtype, const XatArgs& a, int64_t rows) {
+  return rows <= 32 && (dtype == TRIATTN_BF16 || a.d <= 64) ? 1 : 4;
+}
+inline int xat_row_waves(int dtype, const XatArgs& a) {
+  return xat_waves_for(dtype, a, (int64_t)a.nq * a.group);
+}
+inline int xat_key_waves(int dtype, const XatArgs& a) { return xat_waves_for(dtype, a, a.nk); }
 // (with the heads side by side, a wave has 32 rows or keys and a workgroup's others the same)
 inline int xat_row_tiles(const XatArgs& a, int nw) {
   return (int)(((int64_t)a.nq * a.group + 32 * nw - 1) / (32 * nw));
@@ -278,8 +290,12 @@ inline int xat_key_tiles(const XatArgs& a, int nw) { return (a.nk + 32 * nw - 1)
 
 constexpr int XAT_SPLITS = 128;
 
-// Tiles whose loads are in flight: two where a wave stages for itself.
-constexpr int xat_ahead(int sharing) { return sharing == 1 ? 2 : 1; }
+// Tiles whose loads are in flight: two where a wave stages for itself rows of at most `most`
+// bytes (for its registers: 128 forward, 64 backward).
+template <typename T, int DP>
+constexpr int xat_ahead(int sharing, int most) {
+  return sharing == 1 && DP * (int)sizeof(T) <= most ? 2 : 1;
+}
 
 // Splits of a long loop: so that the workgroups (of nw waves) fill the GPU, each of at least
 // `least` steps.
@@ -293,34 +309,56 @@ inline int xat_splits(int64_t wgs, int nw, int64_t steps, int64_t least) {
 // Whether a bias is taken as it lies, four heads a workgroup: the heads' tiles and the bias tile fit LDS, and 4 heads a load.
 inline bool xat_by_heads(int dtype, const XatArgs& a) {
   const int64_t e = dtype == TRIATTN_BF16 ? 2 : 4;
-  return a.bias_batch > 0 && a.group == 1 && a.h % 4 == 0 && a.d <= (e == 2 ? 64 : 32) &&
+  return a.bias_batch > 0 && a.group == 1 && a.h % 4 == 0 && a.d <= (e == 2 ? 128 : 64) &&
          32 * e * a.nk * a.h < (int64_t)1 << 31;  // offsets within a tile
 }
 
+// Groups of waves of a workgroup that take the tiles of its loop in turn (and join their sums in
+// LDS), where few workgroups have long loops.  Four where a wave stages for itself.  With four
+// heads side by side two, for 256 registers a lane, and one where the tiles would not fit LDS.
+inline bool xat_groups(int64_t wgs, int64_t steps) { return wgs < 512 && steps >= 8; }
+template <typename T, int DP, int NW, int MODE>
+constexpr int xat_most_groups() {
+  return NW == 1 ? 4 : MODE == XB_HEADS && DP <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1;
+}
+inline int xat_most_groups(int dtype, const XatArgs& a, int nw) {
+  if (xat_by_heads(dtype, a)) return a.d <= (dtype == TRIATTN_BF16 ? 64 : 32) ? 2 : 1;
+  return nw == 1 ? 4 : 1;
+}
+
+// Splits of a loop over `steps` tiles of 32 by `wgs` workgroups of nw waves.
+inline int xat_loop_splits(int dtype, const XatArgs& a, int64_t wgs, int nw, int64_t steps) {
+  const int groups = xat_groups(wgs, steps) ? xat_most_groups(dtype, a, nw) : 1;
+  if (xat_by_heads(dtype, a)) return xat_splits(wgs * groups * 2, 4, steps, 6 * groups);
+  return xat_splits(wgs * groups, nw, steps, 8 * groups);
+}
+inline int64_t xat_row_wgs(int dtype, const XatArgs& a) {
+  if (xat_by_heads(dtype, a)) return a.batch * (a.h / 4) * xat_row_tiles(a, 1);
+  return a.batch * a.hk * xat_row_tiles(a, xat_row_waves(dtype, a));
+}
+inline int64_t xat_key_wgs(int dtype, const XatArgs& a) {
+  if (xat_by_heads(dtype, a)) return a.batch * (a.h / 4) * xat_key_tiles(a, 1);
+  return a.batch * a.hk * xat_key_tiles(a, xat_key_waves(dtype, a));
+}
+inline int64_t xat_key_steps(const XatArgs& a) { return (a.nk + 31) / 32; }
+inline int64_t xat_row_steps(const XatArgs& a) { return ((int64_t)a.nq * a.group + 31) / 32; }
 inline int xat_key_splits(int dtype, const XatArgs& a) {
-  if (xat_by_heads(dtype, a))
-    return xat_splits(a.batch * (a.h / 4) * xat_row_tiles(a, 1), 4, (a.nk + 31) / 32, 6);
-  const int nw = xat_row_waves(a);
-  return xat_splits(a.batch * a.hk * xat_row_tiles(a, nw), nw, (a.nk + 63) / 64, 4);
+  return xat_loop_splits(dtype, a, xat_row_wgs(dtype, a), xat_row_waves(dtype, a), xat_key_steps(a));
 }
 inline int xat_row_splits(int dtype, const XatArgs& a) {
-  if (xat_by_heads(dtype, a))
-    return xat_splits(a.batch * (a.h / 4) * xat_key_tiles(a, 1), 4, (a.nq + 31) / 32, 6);
-  const int nw = xat_key_waves(a);
-  return xat_splits(a.batch * a.hk * xat_key_tiles(a, nw), nw,
-                    ((int64_t)a.nq * a.group + 63) / 64, 4);
+  return xat_loop_splits(dtype, a, xat_key_wgs(dtype, a), xat_key_waves(dtype, a), xat_row_steps(a));
 }
 
-// Waves a SIMD that a backward kernel's registers have to leave room for.
+
+// Waves a SIMD that a kernel's registers have to leave room for: backward, forward.
 template <typename T, int DP>
 constexpr int xat_waves() {
-  return sizeof(T) == 2 && DP <= 64 ? 2 : 1;
+  return DP <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1;
 }
-
 template <typename T, int DP, int NW, int MODE>
 constexpr int xat_fwd_waves() {
   const int most = DP == 32 ? 4 : DP == 64 ? 3 : 2;  // without a bias, tiles shared
-  return sizeof(T) == 4 ? 1 : NW == 1 || MODE != 0 ? most - 1 : most;
+  return sizeof(T) == 4 ? 1 : NW == 1 || MODE != XB_NONE ? most - 1 : most;
 }
 
 // The logits' (or weights') values of a tile's masked keys set to `value`, for the few tiles that
@@ -336,12 +374,6 @@ __device__ inline void mask_tile(f32x16& s, uint32_t bits, int g, float value) {
     if (!((b >> (8 * (v >> 2) + (v & 3))) & 1u)) s[v] = value;
 }
 
-// Where the bias comes from: none; planes of it, a head each, that a launch before made; or, for
-// four heads at a time, as it lies (heads fastest).  In the last case a workgroup's four waves
-// take four heads of the same 32 rows (or keys): each stages its own head's tiles, and they
-// share the bias tile of 32 queries x 32 keys x 4 heads, whose 4 heads are one load.
-enum XatBias { XB_NONE, XB_PLANES, XB_HEADS };
-
 template <typename T>
 struct BiasTile {
   typedef T V __attribute__((__vector_size__(4 * sizeof(T))));
@@ -350,7 +382,7 @@ struct BiasTile {
   static constexpr int LINE = 32 * 4 * (int)sizeof(T) + 4 * (int)sizeof(T), BYTES = 32 * LINE;
   static constexpr int C = 4;  // entries of a thread
   V x[C];
-  __device__ static inline int q(int u) { return (int)threadIdx.x / 32 + 8 * u; }
+  __device__ static inline int q(int u) { return (int)(threadIdx.x & 255) / 32 + 8 * u; }
   __device__ static inline int k() { return threadIdx.x % 32; }
   __device__ static inline int64_t at(const XatArgs& a, int64_t b, int q, int k) {
     return ((b * a.nq + q) * a.nk + k) * a.h;
@@ -407,13 +439,48 @@ __device__ inline Item item_of(const XatArgs& a, int wg, int tiles, int splits) 
 __device__ inline Item heads_item(const XatArgs& a, int wg, int tiles, int splits) {
   Item t;
   const int quads = a.h / 4;
-  t.kh = 4 * (wg % quads) + (threadIdx.x >> 6);
+  t.kh = 4 * (wg % quads) + ((threadIdx.x >> 6) & 3);
   wg /= quads;
   t.split = wg % splits;
   wg /= splits;
   t.tile = wg % tiles;
   t.b = wg / tiles;
   return t;
+}
+
+// Adds the groups' accumulators to the first group's, in order, through the waves' places in LDS
+// (`bytes` each); for all waves of a workgroup.
+template <int DP, int NW, int KW>
+__device__ inline void add_groups(char* lds, int bytes, f32x16 (&acc)[DP / 32]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __syncthreads();
+  if (wave >= NW) {
+    f32x4* p = (f32x4*)(lds + wave * bytes) + lane;
+#pragma unroll
+    for (int i = 0; i < DP / 8; ++i)
+      p[64 * i] = f32x4{acc[i / 4][i % 4 * 4], acc[i / 4][i % 4 * 4 + 1], acc[i / 4][i % 4 * 4 + 2],
+                        acc[i / 4][i % 4 * 4 + 3]};
+  }
+  __syncthreads();
+  if (wave < NW) {
+#pragma unroll
+    for (int k = 1; k < KW; ++k) {
+      const f32x4* p = (const f32x4*)(lds + (wave + NW * k) * bytes) + lane;
+#pragma unroll
+      for (int i = 0; i < DP / 8; ++i) {
+        const f32x4 x = p[64 * i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i / 4][i % 4 * 4 + e] += x[e];
+      }
+    }
+  }
+}
+
+// Waits for a wave's own LDS stores (others' where a tile is shared).
+template <bool SHARED>
+__device__ inline void tile_barrier() {
+  if (SHARED) __syncthreads();
+  else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
 }  // namespace triattn

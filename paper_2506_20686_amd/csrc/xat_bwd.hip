@@ -47,8 +47,9 @@ __device__ inline float* part_e(const XatArgs& a, int split, int64_t R) {
   return a.part + (int64_t)a.splits * all * 2 * a.d + (int64_t)split * all + R;
 }
 
-template <typename T, int DP, int NW, int MODE>
-__global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dq_kernel(XatArgs a, int tiles) {
+template <typename T, int DP, int NW, int MODE, int KW>
+__global__ __launch_bounds__(64 * NW * KW, (xat_waves<T, DP>())) void xat_dq_kernel(XatArgs a,
+                                                                                   int tiles) {
   constexpr bool BIAS = MODE != XB_NONE, HEADS = MODE == XB_HEADS;
   constexpr int SW = HEADS ? 1 : NW;  // waves that share a tile
   constexpr int BK = xat_keys<T, DP, SW>(), J = BK / 32;
@@ -56,12 +57,13 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dq_kernel(X
   using St = KvStage<T, DP, BK, SW>;
   using Bt = BiasTile<T>;
   using L = XTile<T, DP>;
-  __shared__ __attribute__((aligned(16))) char lds[2 * 2 * St::BYTES * (NW / SW)];
-  __shared__ __attribute__((aligned(16))) char blds[HEADS ? 2 * Bt::BYTES : 16];
+  __shared__ __attribute__((aligned(16))) char lds[2 * St::BYTES * (SW == 1 ? NW * KW : 2)];
+  __shared__ __attribute__((aligned(16))) char blds[HEADS ? 2 * KW * Bt::BYTES : 16];
   const int wg = xcd_swizzle(blockIdx.x, gridDim.x);
   const Item w = HEADS ? heads_item(a, wg, tiles, a.splits) : item_of(a, wg, tiles, a.splits);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
-  const int rows = a.nq * a.group, first = (w.tile * SW + (HEADS ? 0 : wave)) * 32;
+  const int head = wave % NW, group = wave / NW;  // head: or the tile of rows (keys)
+  const int rows = a.nq * a.group, first = (w.tile * SW + (HEADS ? 0 : head)) * 32;
   const int64_t bb = a.bias_batch == 1 ? 0 : w.b;
   const int r = first + (lane & 31), in = r < rows ? r : rows - 1;
   const int64_t R = row_at(a, w.b, w.kh, in, 1);
@@ -85,23 +87,26 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dq_kernel(X
   f32x16 sk[DP / 32] = {}, pk[DP / 32] = {};
   float e = 0.f;
   int valid = 0;  // keys
-  constexpr int D = xat_ahead(SW);  // loads run D tiles ahead
+  constexpr int D = xat_ahead<T, DP>(SW, 64);  // loads run D tiles ahead
   St st[D];
   Bt bt[D];
-  auto load = [&](int d, int t) {
-    st[d].load(a, w.b, w.kh, t * BK);
-    if (HEADS) bt[d].load(a, bb, w.kh & ~3, first, t * BK);
+  const int n = (t1 - t0 + KW - 1) / KW;  // steps, in each the next KW tiles
+  auto load = [&](int d, int i) {
+    const int t = t0 + i * KW + group, k0 = t < t1 ? t * BK : nt * BK;
+    st[d].load(a, w.b, w.kh, k0);
+    if (HEADS) bt[d].load(a, bb, w.kh & ~3, first, k0);
   };
-  auto step = [&](int d, int t) {
-    char* tk = lds + ((t & 1) + (HEADS ? 2 * wave : 0)) * 2 * St::BYTES;
+  auto step = [&](int d, int i) {
+    const int t = t0 + i * KW + group;
+    char* tk = lds + (SW == 1 ? wave : i & 1) * 2 * St::BYTES;
     char* tv = tk + St::BYTES;
-    char* tb = blds + (HEADS ? (t & 1) * Bt::BYTES : 0);
+    char* tb = blds + (HEADS ? (2 * group + (i & 1)) * Bt::BYTES : 0);
     const uint64_t ok = st[d].bits();
     st[d].store(tk, tv, ok);
     if (HEADS) bt[d].store(tb);
     valid += __popcll(ok);
-    load(d, t + D);
-    __syncthreads();
+    load(d, i + D);
+    tile_barrier<(SW > 1 || HEADS)>();
     if (ok == 0 || first >= rows) return;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
@@ -114,7 +119,7 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dq_kernel(X
           if constexpr (HEADS) {
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-              x[u] = (float)*Bt::entry(tb, lane & 31, 8 * i + 4 * g + u, wave);
+              x[u] = (float)*Bt::entry(tb, lane & 31, 8 * i + 4 * g + u, head);
           } else {
             x = load4(bias + (int64_t)t * BK + 32 * j + 8 * i);
           }
@@ -138,15 +143,29 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dq_kernel(X
     }
   };
 #pragma unroll
-  for (int d = 0; d < D; ++d) load(d, t0 + d);
-  for (int t = t0; t < t1; t += D) {
-    step(0, t);
-    if (D == 2 && t + 1 < t1) step(D - 1, t + 1);
+  for (int d = 0; d < D; ++d) load(d, d);
+  for (int i = 0; i < n; i += D) {
+    step(0, i);
+    if (D == 2 && i + 1 < n) step(D - 1, i + 1);
+  }
+  float sum = wave_xor32_sum(e);
+  if constexpr (KW > 1) {
+    __shared__ float part[NW * KW][32];
+    __shared__ int count[NW * KW];
+    if (g == 0) part[wave][lane] = sum;
+    if (lane == 0) count[wave] = valid;
+    add_groups<DP, NW, KW>(lds, 2 * St::BYTES, sk);
+    add_groups<DP, NW, KW>(lds, 2 * St::BYTES, pk);
+    if (group > 0) return;
+#pragma unroll
+    for (int k = 1; k < KW; ++k) {
+      sum += part[head + NW * k][lane & 31];
+      valid += count[head + NW * k];
+    }
   }
   const bool single = a.splits == 1 && valid <= 1;
   if (w.tile == 0 && w.kh == 0 && w.split == 0 && threadIdx.x == 0) a.single[w.b] = single;
   if (r >= rows) return;
-  const float sum = wave_xor32_sum(e);
   if (a.splits > 1) {
     float *ps = part_ab(a, w.split, R, 0), *pp = part_ab(a, w.split, R, 1);
 #pragma unroll
@@ -255,8 +274,9 @@ struct RowStage {
   }
 };
 
-template <typename T, int DP, int NW, int MODE, typename DS = float>
-__global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dkv_kernel(XatArgs a, int tiles) {
+template <typename T, int DP, int NW, int MODE, int KW, typename DS = float>
+__global__ __launch_bounds__(64 * NW * KW, (xat_waves<T, DP>())) void xat_dkv_kernel(XatArgs a,
+                                                                                    int tiles) {
   constexpr bool BIAS = MODE != XB_NONE, HEADS = MODE == XB_HEADS;
   constexpr int SW = HEADS ? 1 : NW;  // waves that share a tile
   constexpr int BQ = xat_keys<T, DP, SW>(), J = BQ / 32;
@@ -266,13 +286,14 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dkv_kernel(
   using L = XTile<T, DP>;
   // dS of the four heads leaves through LDS: in the bias's place where it has the bias's type
   constexpr bool SAME = sizeof(T) == sizeof(DS);
-  __shared__ __attribute__((aligned(16))) char lds[2 * St::BYTES * (NW / SW)];
-  __shared__ __attribute__((aligned(16))) char blds[HEADS ? 2 * Bt::BYTES : 16];
-  __shared__ __attribute__((aligned(16))) char dlds[HEADS && !SAME ? 2 * Dt::BYTES : 16];
+  __shared__ __attribute__((aligned(16))) char lds[St::BYTES * (SW == 1 ? NW * KW : 2)];
+  __shared__ __attribute__((aligned(16))) char blds[HEADS ? 2 * KW * Bt::BYTES : 16];
+  __shared__ __attribute__((aligned(16))) char dlds[HEADS && !SAME ? 2 * KW * Dt::BYTES : 16];
   const int wg = xcd_swizzle(blockIdx.x, gridDim.x);
   const Item w = HEADS ? heads_item(a, wg, tiles, a.splits_q) : item_of(a, wg, tiles, a.splits_q);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
-  const int rows = a.nq * a.group, first = (w.tile * SW + (HEADS ? 0 : wave)) * 32;
+  const int head = wave % NW, group = wave / NW;  // head: or the tile of rows (keys)
+  const int rows = a.nq * a.group, first = (w.tile * SW + (HEADS ? 0 : head)) * 32;
   const int key = first + (lane & 31);
   const int64_t bb = a.bias_batch == 1 ? 0 : w.b;
   const bool valid = key < a.nk && (a.mask == nullptr || a.mask[w.b * a.nk + key] != 0);
@@ -292,36 +313,41 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dkv_kernel(
   const float c = BIAS ? LOG2E : a.scale * LOG2E;
   f32x16 dv[DP / 32] = {}, dk[DP / 32] = {};
   const bool single = a.single[w.b] != 0;
-  constexpr int D = HEADS ? 2 : 1;  // loads run D tiles ahead
+  constexpr int D = HEADS ? xat_ahead<T, DP>(SW, 64) : 1;  // loads run D tiles ahead
   St st[D];
   Bt bt[D];
-  auto load = [&](int d, int t) {
-    st[d].load(a, w.b, w.kh, t * BQ);
-    if (HEADS) bt[d].load(a, bb, w.kh & ~3, t * BQ, first);
+  const int n = (t1 - t0 + KW - 1) / KW;  // steps, in each the next KW tiles
+  auto load = [&](int d, int i) {
+    const int t = t0 + i * KW + group, r0 = t < t1 ? t * BQ : nt * BQ;
+    st[d].load(a, w.b, w.kh, r0);
+    if (HEADS) bt[d].load(a, bb, w.kh & ~3, r0, first);
   };
   const bool any = __any(valid);  // the wave has a valid key
-  auto step = [&](int d, int t) {
-    char* tq = lds + ((t & 1) + (HEADS ? 2 * wave : 0)) * St::BYTES;
+  auto step = [&](int d, int i) {
+    const int t = t0 + i * KW + group;
+    char* tq = lds + (SW == 1 ? wave : i & 1) * St::BYTES;
     char* td = tq + St::TILE;
-    char* tb = blds + (HEADS ? (t & 1) * Bt::BYTES : 0);
-    char* ts = SAME ? tb : dlds + (HEADS ? (t & 1) * Dt::BYTES : 0);
+    char* tb = blds + (HEADS ? (2 * group + (i & 1)) * Bt::BYTES : 0);
+    char* ts = SAME ? tb : dlds + (HEADS ? (2 * group + (i & 1)) * Dt::BYTES : 0);
     const float* stat = (const float*)(tq + 2 * St::TILE);
     st[d].store(tq);
     if (HEADS) bt[d].store(tb);
-    load(d, t + D);
-    __syncthreads();
+    load(d, i + D);
+    tile_barrier<(SW > 1 || HEADS)>();
     if (!any && !BIAS) return;
     if (first >= a.nk) return;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int r0 = t * BQ + 32 * j;
-      if (r0 >= rows) break;
+      // (with the heads side by side every wave comes to the barrier below: a tile past the
+      // group's last is zeros, and its dS go nowhere)
+      if (!HEADS && (t >= t1 || r0 >= rows)) break;
       float x[16];
       if constexpr (BIAS) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           const int r = r0 + acc_row(v, g);
-          if (HEADS) x[v] = (float)*Bt::entry(tb, acc_row(v, g), lane & 31, wave);
+          if (HEADS) x[v] = (float)*Bt::entry(tb, acc_row(v, g), lane & 31, head);
           else x[v] = key < a.nk && r < rows ? (float)bias[(int64_t)r * a.nkp] : 0.f;
         }
       }
@@ -347,10 +373,10 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dkv_kernel(
         // a wave writes where it alone has read; all four before the entries leave
 #pragma unroll
         for (int v = 0; v < 16; ++v)
-          *Dt::entry(ts, acc_row(v, g), lane & 31, wave) = (DS)(valid ? dp[v] : 0.f);
+          *Dt::entry(ts, acc_row(v, g), lane & 31, head) = (DS)(valid ? dp[v] : 0.f);
         __syncthreads();
-        Dt::write(a, a.bias_batch == a.batch ? (DS*)a.dbias : (DS*)a.dplanes, w.b, w.kh & ~3, r0,
-                  first, ts);
+        Dt::write(a, a.bias_batch == a.batch ? (DS*)a.dbias : (DS*)a.dplanes, w.b, w.kh & ~3,
+                  t < t1 ? r0 : rows, first, ts);
       }
       if (MODE == XB_PLANES && ds) {
 #pragma unroll
@@ -369,11 +395,16 @@ __global__ __launch_bounds__(64 * NW, (xat_waves<T, DP>())) void xat_dkv_kernel(
   // a workgroup whose keys are all masked has nothing to sum
   if (BIAS || __syncthreads_or(valid)) {
 #pragma unroll
-    for (int d = 0; d < D; ++d) load(d, t0 + d);
-    for (int t = t0; t < t1; t += D) {
-      step(0, t);
-      if (D == 2 && t + 1 < t1) step(D - 1, t + 1);
+    for (int d = 0; d < D; ++d) load(d, d);
+    for (int i = 0; i < n; i += D) {
+      step(0, i);
+      if (D == 2 && i + 1 < n) step(D - 1, i + 1);
     }
+  }
+  if constexpr (KW > 1) {
+    add_groups<DP, NW, KW>(lds, St::BYTES, dv);
+    add_groups<DP, NW, KW>(lds, St::BYTES, dk);
+    if (group > 0) return;
   }
   if (key >= a.nk) return;
   // whatever the column of a masked key holds, its gradients are zeros
@@ -415,35 +446,54 @@ __global__ __launch_bounds__(256) void xat_dkv_join_kernel(XatArgs a) {
   store4((T*)a.dv + i, y);
 }
 
-template <typename T, int DP, int NW>
+template <typename T, int DP, int NW, int MODE>
 void dq_launch(const XatArgs& a, hipStream_t s) {
-  const int tiles = xat_row_tiles(a, NW);
-  const dim3 grid((unsigned)(a.batch * a.hk * tiles * a.splits)), wg(64 * NW);
-  if (a.bias) hipLaunchKernelGGL((xat_dq_kernel<T, DP, NW, XB_PLANES>), grid, wg, 0, s, a, tiles);
-  else hipLaunchKernelGGL((xat_dq_kernel<T, DP, NW, XB_NONE>), grid, wg, 0, s, a, tiles);
-}
-template <typename T, int DP>
-void dq_heads(const XatArgs& a, hipStream_t s) {
-  const int tiles = xat_row_tiles(a, 1);
-  const dim3 grid((unsigned)(a.batch * (a.h / 4) * tiles * a.splits)), wg(256);
-  hipLaunchKernelGGL((xat_dq_kernel<T, DP, 4, XB_HEADS>), grid, wg, 0, s, a, tiles);
-}
-template <typename T, int DP>
-void dkv_heads(const XatArgs& a, hipStream_t s) {
-  const int tiles = xat_key_tiles(a, 1);
-  const dim3 grid((unsigned)(a.batch * (a.h / 4) * tiles * a.splits_q)), wg(256);
-  // samples that share a bias: dS in fp32, to be summed over them
-  if (a.bias_batch == a.batch)
-    hipLaunchKernelGGL((xat_dkv_kernel<T, DP, 4, XB_HEADS, T>), grid, wg, 0, s, a, tiles);
+  constexpr int KW = xat_most_groups<T, DP, NW, MODE>();
+  const int tiles = xat_row_tiles(a, MODE == XB_HEADS ? 1 : NW);
+  const int64_t wgs = xat_row_wgs(sizeof(T) == 2 ? TRIATTN_BF16 : TRIATTN_F32, a);
+  const dim3 grid((unsigned)(wgs * a.splits));
+  if (KW > 1 && xat_groups(wgs, xat_key_steps(a)))
+    hipLaunchKernelGGL((xat_dq_kernel<T, DP, NW, MODE, KW>), grid, dim3(64 * NW * KW), 0, s, a,
+                       tiles);
   else
-    hipLaunchKernelGGL((xat_dkv_kernel<T, DP, 4, XB_HEADS, float>), grid, wg, 0, s, a, tiles);
+    hipLaunchKernelGGL((xat_dq_kernel<T, DP, NW, MODE, 1>), grid, dim3(64 * NW), 0, s, a, tiles);
 }
-template <typename T, int DP, int NW>
+// DS: dbias as it leaves the kernel, the tensors' type, or fp32 to be summed over the samples.
+template <typename T, int DP, int NW, int MODE, typename DS = float>
 void dkv_launch(const XatArgs& a, hipStream_t s) {
-  const int tiles = xat_key_tiles(a, NW);
-  const dim3 grid((unsigned)(a.batch * a.hk * tiles * a.splits_q)), wg(64 * NW);
-  if (a.bias) hipLaunchKernelGGL((xat_dkv_kernel<T, DP, NW, XB_PLANES>), grid, wg, 0, s, a, tiles);
-  else hipLaunchKernelGGL((xat_dkv_kernel<T, DP, NW, XB_NONE>), grid, wg, 0, s, a, tiles);
+  constexpr int KW = xat_most_groups<T, DP, NW, MODE>();
+  // (fp32 tiles of dS beside bf16 ones of the bias leave no room for two groups of 64 channels)
+  constexpr int GROUPS = MODE == XB_HEADS && sizeof(DS) > sizeof(T) && DP == 64 ? 1 : KW;
+  const int tiles = xat_key_tiles(a, MODE == XB_HEADS ? 1 : NW);
+  const int64_t wgs = xat_key_wgs(sizeof(T) == 2 ? TRIATTN_BF16 : TRIATTN_F32, a);
+  const dim3 grid((unsigned)(wgs * a.splits_q));
+  if (GROUPS > 1 && xat_groups(wgs, xat_row_steps(a)))
+    hipLaunchKernelGGL((xat_dkv_kernel<T, DP, NW, MODE, GROUPS, DS>), grid, dim3(64 * NW * GROUPS),
+                       0, s, a, tiles);
+  else
+    hipLaunchKernelGGL((xat_dkv_kernel<T, DP, NW, MODE, 1, DS>), grid, dim3(64 * NW), 0, s, a,
+                       tiles);
+}
+template <typename T, int DP>
+void dq_width(const XatArgs& a, bool heads, hipStream_t s) {
+  constexpr int ONE = sizeof(T) == 2 || DP <= 64 ? 1 : 4;
+  const int nw = xat_row_waves(sizeof(T) == 2 ? TRIATTN_BF16 : TRIATTN_F32, a);
+  if constexpr (sizeof(T) == 2 || DP <= 64)
+    if (heads) return dq_launch<T, DP, 4, XB_HEADS>(a, s);
+  if (a.bias) nw == 1 ? dq_launch<T, DP, ONE, XB_PLANES>(a, s) : dq_launch<T, DP, 4, XB_PLANES>(a, s);
+  else nw == 1 ? dq_launch<T, DP, ONE, XB_NONE>(a, s) : dq_launch<T, DP, 4, XB_NONE>(a, s);
+}
+template <typename T, int DP>
+void dkv_width(const XatArgs& a, bool heads, hipStream_t s) {
+  constexpr int ONE = sizeof(T) == 2 || DP <= 64 ? 1 : 4;
+  const int nw = xat_key_waves(sizeof(T) == 2 ? TRIATTN_BF16 : TRIATTN_F32, a);
+  if constexpr (sizeof(T) == 2 || DP <= 64) {
+    if (heads && a.bias_batch == a.batch) return dkv_launch<T, DP, 4, XB_HEADS, T>(a, s);
+    if (heads) return dkv_launch<T, DP, 4, XB_HEADS, float>(a, s);
+  }
+  if (a.bias)
+    nw == 1 ? dkv_launch<T, DP, ONE, XB_PLANES>(a, s) : dkv_launch<T, DP, 4, XB_PLANES>(a, s);
+  else nw == 1 ? dkv_launch<T, DP, ONE, XB_NONE>(a, s) : dkv_launch<T, DP, 4, XB_NONE>(a, s);
 }
 
 template <typename T>
@@ -456,12 +506,9 @@ hipError_t bwd(const XatArgs& a, hipStream_t s) {
   }
   {
     KernelTimer t(K_XAT_DQ, s);
-    const int nw = xat_row_waves(a);
-    if (heads && a.d <= 32) dq_heads<T, 32>(a, s);
-    else if (heads) dq_heads<bf16, 64>(a, s);
-    else if (a.d <= 32) nw == 1 ? dq_launch<T, 32, 1>(a, s) : dq_launch<T, 32, 4>(a, s);
-    else if (a.d <= 64) nw == 1 ? dq_launch<T, 64, 1>(a, s) : dq_launch<T, 64, 4>(a, s);
-    else nw == 1 ? dq_launch<T, 128, 1>(a, s) : dq_launch<T, 128, 4>(a, s);
+    if (a.d <= 32) dq_width<T, 32>(a, heads, s);
+    else if (a.d <= 64) dq_width<T, 64>(a, heads, s);
+    else dq_width<T, 128>(a, heads, s);
   }
   if (a.splits > 1) {
     KernelTimer t(K_XAT_JOIN, s);
@@ -470,12 +517,9 @@ hipError_t bwd(const XatArgs& a, hipStream_t s) {
   }
   {
     KernelTimer t(K_XAT_DKV, s);
-    const int nw = xat_key_waves(a);
-    if (heads && a.d <= 32) dkv_heads<T, 32>(a, s);
-    else if (heads) dkv_heads<bf16, 64>(a, s);
-    else if (a.d <= 32) nw == 1 ? dkv_launch<T, 32, 1>(a, s) : dkv_launch<T, 32, 4>(a, s);
-    else if (a.d <= 64) nw == 1 ? dkv_launch<T, 64, 1>(a, s) : dkv_launch<T, 64, 4>(a, s);
-    else nw == 1 ? dkv_launch<T, 128, 1>(a, s) : dkv_launch<T, 128, 4>(a, s);
+    if (a.d <= 32) dkv_width<T, 32>(a, heads, s);
+    else if (a.d <= 64) dkv_width<T, 64>(a, heads, s);
+    else dkv_width<T, 128>(a, heads, s);
   }
   if (a.splits_q > 1) {
     KernelTimer t(K_XAT_JOIN, s);

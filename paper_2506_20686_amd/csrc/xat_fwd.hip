@@ -16,8 +16,9 @@
 namespace triattn {
 namespace {
 
-template <typename T, int DP, int NW, int MODE>
-__global__ __launch_bounds__(64 * NW, (xat_fwd_waves<T, DP, NW, MODE>())) void xat_fwd_kernel(XatArgs a, int tiles) {
+template <typename T, int DP, int NW, int MODE, int KW>
+__global__ __launch_bounds__(64 * NW * KW, (xat_fwd_waves<T, DP, NW, MODE>())) void xat_fwd_kernel(
+    XatArgs a, int tiles) {
   constexpr bool BIAS = MODE != XB_NONE, HEADS = MODE == XB_HEADS;
   constexpr int SW = HEADS ? 1 : NW;  // waves that share a tile
   constexpr int BK = xat_keys<T, DP, SW>(), J = BK / 32;
@@ -25,12 +26,14 @@ __global__ __launch_bounds__(64 * NW, (xat_fwd_waves<T, DP, NW, MODE>())) void x
   using St = KvStage<T, DP, BK, SW>;
   using Bt = BiasTile<T>;
   using L = XTile<T, DP>;
-  __shared__ __attribute__((aligned(16))) char lds[2 * 2 * St::BYTES * (NW / SW)];
-  __shared__ __attribute__((aligned(16))) char blds[HEADS ? 2 * Bt::BYTES : 16];
+  // K and V of each wave, or two buffers of all waves'; the groups' bias tiles, two buffers each
+  __shared__ __attribute__((aligned(16))) char lds[2 * St::BYTES * (SW == 1 ? NW * KW : 2)];
+  __shared__ __attribute__((aligned(16))) char blds[HEADS ? 2 * KW * Bt::BYTES : 16];
   const int wg = xcd_swizzle(blockIdx.x, gridDim.x);
   const Item w = HEADS ? heads_item(a, wg, tiles, a.splits) : item_of(a, wg, tiles, a.splits);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
-  const int rows = a.nq * a.group, first = (w.tile * SW + (HEADS ? 0 : wave)) * 32;
+  const int head = wave % NW, group = wave / NW;  // head: or the tile of rows
+  const int rows = a.nq * a.group, first = (w.tile * SW + (HEADS ? 0 : head)) * 32;
   const int r = first + (lane & 31), in = r < rows ? r : rows - 1;
   const int64_t bb = a.bias_batch == 1 ? 0 : w.b;
   typename L::Row q;
@@ -44,23 +47,26 @@ __global__ __launch_bounds__(64 * NW, (xat_fwd_waves<T, DP, NW, MODE>())) void x
   float m = neg_inf(), l = 0.f;
   f32x16 o[DP / 32] = {};
   // loads run D tiles ahead; past the end they touch no memory
-  constexpr int D = xat_ahead(SW);
+  constexpr int D = xat_ahead<T, DP>(SW, 128);
   St st[D];
   Bt bt[D];
-  auto load = [&](int d, int t) {
-    st[d].load(a, w.b, w.kh, t * BK);
-    if (HEADS) bt[d].load(a, bb, w.kh & ~3, first, t * BK);
+  const int n = (t1 - t0 + KW - 1) / KW;  // steps, in each the next KW tiles
+  auto load = [&](int d, int i) {
+    const int t = t0 + i * KW + group, k0 = t < t1 ? t * BK : nt * BK;
+    st[d].load(a, w.b, w.kh, k0);
+    if (HEADS) bt[d].load(a, bb, w.kh & ~3, first, k0);
   };
-  auto step = [&](int d, int t) {
-    char* tk = lds + ((t & 1) + (HEADS ? 2 * wave : 0)) * 2 * St::BYTES;
+  auto step = [&](int d, int i) {
+    const int t = t0 + i * KW + group;
+    char* tk = lds + (SW == 1 ? wave : i & 1) * 2 * St::BYTES;
     char* tv = tk + St::BYTES;
-    char* tb = blds + (HEADS ? (t & 1) * Bt::BYTES : 0);
+    char* tb = blds + (HEADS ? (2 * group + (i & 1)) * Bt::BYTES : 0);
     const uint64_t ok = st[d].bits();
     st[d].store(tk, tv, ok);
     if (HEADS) bt[d].store(tb);
-    load(d, t + D);
-    // this buffer was last read two steps ago, before the barrier of the last step
-    __syncthreads();
+    load(d, i + D);
+    // what waves share was last read two steps ago, before the barrier of the last step
+    tile_barrier<(SW > 1 || HEADS)>();
     if (ok == 0 || first >= rows) return;
     f32x16 s[J];
 #pragma unroll
@@ -73,7 +79,7 @@ __global__ __launch_bounds__(64 * NW, (xat_fwd_waves<T, DP, NW, MODE>())) void x
           if constexpr (HEADS) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              x[e] = (float)*Bt::entry(tb, lane & 31, 8 * i + 4 * g + e, wave);
+              x[e] = (float)*Bt::entry(tb, lane & 31, 8 * i + 4 * g + e, head);
           } else {
             x = load4(bias + (int64_t)t * BK + 32 * j + 8 * i);
           }
@@ -114,12 +120,34 @@ __global__ __launch_bounds__(64 * NW, (xat_fwd_waves<T, DP, NW, MODE>())) void x
     }
   };
 #pragma unroll
-  for (int d = 0; d < D; ++d) load(d, t0 + d);
-  for (int t = t0; t < t1; t += D) {
-    step(0, t);
-    if (D == 2 && t + 1 < t1) step(D - 1, t + 1);
+  for (int d = 0; d < D; ++d) load(d, d);
+  for (int i = 0; i < n; i += D) {
+    step(0, i);
+    if (D == 2 && i + 1 < n) step(D - 1, i + 1);
   }
   l = wave_xor32_sum(l);
+  if constexpr (KW > 1) {  // all groups to the maximum of theirs, then their sums
+    __shared__ f32x2 ml[NW * KW][32];
+    if (g == 0) ml[wave][lane] = f32x2{m, l};
+    __syncthreads();
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) top = fmaxf(top, ml[head + NW * k][lane & 31][0]);
+    const float f = top > m ? __builtin_amdgcn_exp2f((m - top) * c) : 1.f;
+#pragma unroll
+    for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) o[n][v] *= f;
+    l = 0.f;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) {
+      const f32x2 x = ml[head + NW * k][lane & 31];
+      l = fmaf(x[1], top > x[0] ? __builtin_amdgcn_exp2f((x[0] - top) * c) : 1.f, l);
+    }
+    m = top;
+    add_groups<DP, NW, KW>(lds, 2 * St::BYTES, o);
+    if (group > 0) return;
+  }
   if (r >= rows) return;
   if (!BIAS) m *= a.scale;  // scale > 0: -inf stays
   const int64_t R = row_at(a, w.b, w.kh, r, 1);
@@ -196,18 +224,26 @@ __global__ __launch_bounds__(256) void xat_join_kernel(XatArgs a) {
   if (lane == 0) *(f32x2*)(a.stat + 2 * R) = f32x2{m, l > 0.f ? __logf(l) : 0.f};
 }
 
-template <typename T, int DP, int NW>
+template <typename T, int DP, int NW, int MODE>
 void fwd_launch(const XatArgs& a, hipStream_t s) {
-  const int tiles = xat_row_tiles(a, NW);
-  const dim3 grid((unsigned)(a.batch * a.hk * tiles * a.splits)), wg(64 * NW);
-  if (a.bias) hipLaunchKernelGGL((xat_fwd_kernel<T, DP, NW, XB_PLANES>), grid, wg, 0, s, a, tiles);
-  else hipLaunchKernelGGL((xat_fwd_kernel<T, DP, NW, XB_NONE>), grid, wg, 0, s, a, tiles);
+  constexpr int KW = xat_most_groups<T, DP, NW, MODE>();
+  const int tiles = xat_row_tiles(a, MODE == XB_HEADS ? 1 : NW);
+  const int64_t wgs = xat_row_wgs(sizeof(T) == 2 ? TRIATTN_BF16 : TRIATTN_F32, a);
+  const dim3 grid((unsigned)(wgs * a.splits));
+  if (KW > 1 && xat_groups(wgs, xat_key_steps(a)))
+    hipLaunchKernelGGL((xat_fwd_kernel<T, DP, NW, MODE, KW>), grid, dim3(64 * NW * KW), 0, s, a,
+                       tiles);
+  else
+    hipLaunchKernelGGL((xat_fwd_kernel<T, DP, NW, MODE, 1>), grid, dim3(64 * NW), 0, s, a, tiles);
 }
 template <typename T, int DP>
-void fwd_heads(const XatArgs& a, hipStream_t s) {
-  const int tiles = xat_row_tiles(a, 1);
-  const dim3 grid((unsigned)(a.batch * (a.h / 4) * tiles * a.splits)), wg(256);
-  hipLaunchKernelGGL((xat_fwd_kernel<T, DP, 4, XB_HEADS>), grid, wg, 0, s, a, tiles);
+void fwd_width(const XatArgs& a, bool heads, hipStream_t s) {
+  constexpr int ONE = sizeof(T) == 2 || DP <= 64 ? 1 : 4;
+  const int nw = xat_row_waves(sizeof(T) == 2 ? TRIATTN_BF16 : TRIATTN_F32, a);
+  if constexpr (sizeof(T) == 2 || DP <= 64)
+    if (heads) return fwd_launch<T, DP, 4, XB_HEADS>(a, s);
+  if (a.bias) nw == 1 ? fwd_launch<T, DP, ONE, XB_PLANES>(a, s) : fwd_launch<T, DP, 4, XB_PLANES>(a, s);
+  else nw == 1 ? fwd_launch<T, DP, ONE, XB_NONE>(a, s) : fwd_launch<T, DP, 4, XB_NONE>(a, s);
 }
 
 template <typename T>
@@ -220,12 +256,9 @@ hipError_t fwd(const XatArgs& a, hipStream_t s) {
   }
   {
     KernelTimer t(K_XAT_FWD, s);
-    const int nw = xat_row_waves(a);
-    if (heads && a.d <= 32) fwd_heads<T, 32>(a, s);
-    else if (heads) fwd_heads<bf16, 64>(a, s);
-    else if (a.d <= 32) nw == 1 ? fwd_launch<T, 32, 1>(a, s) : fwd_launch<T, 32, 4>(a, s);
-    else if (a.d <= 64) nw == 1 ? fwd_launch<T, 64, 1>(a, s) : fwd_launch<T, 64, 4>(a, s);
-    else nw == 1 ? fwd_launch<T, 128, 1>(a, s) : fwd_launch<T, 128, 4>(a, s);
+    if (a.d <= 32) fwd_width<T, 32>(a, heads, s);
+    else if (a.d <= 64) fwd_width<T, 64>(a, heads, s);
+    else fwd_width<T, 128>(a, heads, s);
   }
   if (a.splits > 1) {
     KernelTimer t(K_XAT_JOIN, s);

@@ -58,7 +58,8 @@ SIZES = [(1, 1, 1, 1, 1, 8), (1, 1, 1, 2, 1, 16), (2, 7, 33, 4, 4, 32), (1, 33, 
          (1, 40, 100, 2, 2, 96), (1, 700, 90, 1, 1, 72), (5, 32, 128, 4, 4, 32),
          (2, 11, 32, 6, 2, 8), (1, 1500, 3, 2, 2, 32), (1, 3, 1500, 1, 1, 128),
          (2, 1, 130, 7, 1, 56), (1, 97, 640, 5, 5, 24), (1, 45, 70, 16, 16, 24),
-         (3, 50, 40, 8, 8, 64), (1, 1, 1, 4, 4, 8)]
+         (3, 50, 40, 8, 8, 64), (1, 1, 1, 4, 4, 8), (1, 300, 420, 4, 4, 32),
+         (2, 70, 500, 4, 4, 56), (1, 290, 33, 4, 4, 128), (1, 20, 9000, 2, 2, 32)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F4])
@@ -186,7 +187,7 @@ def test_sharp_weights():
 
 @pytest.mark.parametrize("dtype", [BF, F4])
 @pytest.mark.parametrize("size", [(2, 37, 70, 4, 2, 24), (1, 3, 900, 4, 1, 64), (1, 900, 5, 2, 2, 8),
-                                  (2, 37, 70, 8, 8, 24)],
+                                  (2, 37, 70, 8, 8, 24), (1, 300, 420, 4, 4, 32)],
                          ids=str)
 def test_nothing_outside_the_outputs_is_written(size, dtype):
     b, nq, nk, h, hk, d = size

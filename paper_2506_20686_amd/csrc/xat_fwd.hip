@@ -31,7 +31,7 @@ __global__ __launch_bounds__(64 * NW * KW, (xat_fwd_waves<T, DP, NW, MODE>())) v
   __shared__ __attribute__((aligned(16))) char blds[HEADS ? 2 * KW * Bt::BYTES : 16];
   const int wg = xcd_swizzle(blockIdx.x, gridDim.x);
   const Item w = HEADS ? heads_item(a, wg, tiles, a.splits) : item_of(a, wg, tiles, a.splits);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = wave_id(), g = lane >> 5;
   const int head = wave % NW, group = wave / NW;  // head: or the tile of rows
   const int rows = a.nq * a.group, first = (w.tile * SW + (HEADS ? 0 : head)) * 32;
   const int r = first + (lane & 31), in = r < rows ? r : rows - 1;

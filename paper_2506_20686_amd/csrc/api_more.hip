@@ -91,21 +91,26 @@ size_t glu_ws(const triattn::LinBwdPlan& p) { return round256(p.part) + round256
 
 // ---- norm and clipping of gradients -----------------------------------------------------------
 
-int64_t grad_wgs(int64_t size) {
-  return (size + triattn::GRAD_SPAN - 1) / triattn::GRAD_SPAN;
-}
-int grad_sizes(int64_t count, const int64_t* sizes, int64_t* wgs) {
+struct GradPlan {
+  int64_t span, wgs;
+};
+int64_t grad_wgs(int64_t size, int64_t span) { return (size + span - 1) / span; }
+// A workgroup's elements: 32768 (8 or 16 words of 16 bytes a thread, four at a time), fewer where
+// that leaves CUs idle, down to 2048 (130,000 elements of 14 tensors: one round of words).
+int grad_plan(int64_t count, const int64_t* sizes, GradPlan* p) {
   if (count < 1 || count > ((int64_t)1 << 20) || sizes == nullptr) return TRIATTN_ERR_INVALID_ARG;
   int64_t total = 0;
-  *wgs = 0;
   for (int64_t i = 0; i < count; ++i) {
     if (sizes[i] < 0) return TRIATTN_ERR_INVALID_ARG;
     const int64_t room = ((int64_t)1 << 39) - 1 - total;
     if (sizes[i] > room) return TRIATTN_ERR_UNSUPPORTED;
     total += sizes[i];
-    *wgs += grad_wgs(sizes[i]);
   }
-  return *wgs >= MAX_WGS ? TRIATTN_ERR_UNSUPPORTED : TRIATTN_OK;
+  p->span = 2048;
+  while (p->span < 32768 && total / p->span > 2048) p->span *= 2;
+  p->wgs = 0;
+  for (int64_t i = 0; i < count; ++i) p->wgs += grad_wgs(sizes[i], p->span);
+  return p->wgs >= MAX_WGS ? TRIATTN_ERR_UNSUPPORTED : TRIATTN_OK;
 }
 int grad_list(int64_t count, const int32_t* dtypes, const int64_t* sizes,
               const void* const* list) {
@@ -133,7 +138,7 @@ int grad_each(int64_t count, const int32_t* dtypes, const int64_t* sizes,
       a.dst[n] = outs ? outs[i] : nullptr;
       a.size[n] = sizes[i];
       a.dtype[n] = (uint8_t)dtypes[i];
-      a.first[n + 1] = a.first[n] + (int)grad_wgs(sizes[i]);
+      a.first[n + 1] = a.first[n] + (int)grad_wgs(sizes[i], a.span);
     }
     if (a.count == 0) break;
     if (launch(a) != hipSuccess) return TRIATTN_ERR_HIP;
@@ -292,38 +297,39 @@ int tri_gated_linear_bwd(int dtype, int64_t m, int64_t k, int64_t f, int act, co
 }
 
 int tri_grad_norm_workspace_bytes(int64_t count, const int64_t* sizes, size_t* bytes) {
-  int64_t wgs;
-  const int st = grad_sizes(count, sizes, &wgs);
+  GradPlan plan;
+  const int st = grad_plan(count, sizes, &plan);
   if (st != TRIATTN_OK) return st;
   if (bytes == nullptr) return TRIATTN_ERR_INVALID_ARG;
-  *bytes = grad_ws(wgs);
+  *bytes = grad_ws(plan.wgs);
   return TRIATTN_OK;
 }
 
 int tri_grad_norm(int64_t count, const int32_t* dtypes, const int64_t* sizes,
                   const void* const* grads, float* norm, void* workspace, size_t workspace_bytes,
                   void* stream) {
-  int64_t wgs;
-  int st = grad_sizes(count, sizes, &wgs);
+  GradPlan plan;
+  int st = grad_plan(count, sizes, &plan);
   if (st == TRIATTN_OK) st = grad_list(count, dtypes, sizes, grads);
   if (st != TRIATTN_OK) return st;
   if (norm == nullptr || ((uintptr_t)norm & 3u) != 0) return TRIATTN_ERR_INVALID_ARG;
-  if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < grad_ws(wgs))
+  if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < grad_ws(plan.wgs))
     return TRIATTN_ERR_WORKSPACE;
   triattn::GradArgs a{};
   a.part = (double*)workspace;
+  a.span = plan.span;
   const hipStream_t s = (hipStream_t)stream;
   st = grad_each(count, dtypes, sizes, grads, nullptr, a,
                  [&](const triattn::GradArgs& x) { return triattn::launch_grad_squares(x, s); });
   if (st != TRIATTN_OK) return st;
-  return launched(triattn::launch_grad_root(a.part, wgs, norm, s));
+  return launched(triattn::launch_grad_root(a.part, plan.wgs, norm, s));
 }
 
 int tri_grad_clip(int64_t count, const int32_t* dtypes, const int64_t* sizes,
                   const void* const* grads, const float* norm, float max_norm,
                   void* const* outs, void* stream) {
-  int64_t wgs;
-  int st = grad_sizes(count, sizes, &wgs);
+  GradPlan plan;
+  int st = grad_plan(count, sizes, &plan);
   if (st == TRIATTN_OK) st = grad_list(count, dtypes, sizes, grads);
   if (st == TRIATTN_OK) st = grad_list(count, dtypes, sizes, outs);
   if (st != TRIATTN_OK) return st;
@@ -331,6 +337,7 @@ int tri_grad_clip(int64_t count, const int32_t* dtypes, const int64_t* sizes,
   if (!(isfinite(max_norm) && max_norm > 0.f)) return TRIATTN_ERR_INVALID_ARG;
   triattn::GradArgs a{};
   a.norm = norm;
+  a.span = plan.span;
   a.limit = max_norm;
   const hipStream_t s = (hipStream_t)stream;
   return grad_each(count, dtypes, sizes, grads, outs, a,

@@ -71,8 +71,8 @@ __device__ inline double group_sum(double s) {
 
 __global__ __launch_bounds__(256) void grad_squares_kernel(GradArgs a) {
   const int wg = blockIdx.x, t = tensor_of(a, wg);
-  const int64_t at = (int64_t)(wg - a.first[t]) * GRAD_SPAN;
-  const int64_t n = a.size[t] - at < GRAD_SPAN ? a.size[t] - at : GRAD_SPAN;
+  const int64_t at = (int64_t)(wg - a.first[t]) * a.span;
+  const int64_t n = a.size[t] - at < a.span ? a.size[t] - at : a.span;
   double s = a.dtype[t] == TRIATTN_BF16 ? squares((const bf16*)a.src[t] + at, n)
                                         : squares((const float*)a.src[t] + at, n);
   s = group_sum(s);
@@ -82,25 +82,38 @@ __global__ __launch_bounds__(256) void grad_squares_kernel(GradArgs a) {
 __global__ __launch_bounds__(256) void grad_root_kernel(const double* part, int64_t count,
                                                         float* norm) {
   double s = 0.;
+#pragma unroll 8
   for (int64_t i = threadIdx.x; i < count; i += 256) s += part[i];
   s = group_sum(s);
   if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
 template <typename T>
-__device__ inline void scale(const T* p, T* o, int64_t n, float f) {
+__device__ inline u32x4 scaled(u32x4 v, float f) {
   constexpr int W = 16 / (int)sizeof(T);
   struct E {
     T x[W];
   };
-  const int64_t words = n / W;
-  for (int64_t i = threadIdx.x; i < words; i += 256) {
-    E e = __builtin_bit_cast(E, ((const u32x4*)p)[i]);
+  E e = __builtin_bit_cast(E, v);
 #pragma unroll
-    for (int k = 0; k < W; ++k) e.x[k] = (T)((float)e.x[k] * f);
-    ((u32x4*)o)[i] = __builtin_bit_cast(u32x4, e);
+  for (int k = 0; k < W; ++k) e.x[k] = (T)((float)e.x[k] * f);
+  return __builtin_bit_cast(u32x4, e);
+}
+template <typename T>
+__device__ inline void scale(const T* p, T* o, int64_t n, float f) {
+  constexpr int W = 16 / (int)sizeof(T);
+  const int64_t words = n / W;
+  int64_t i = threadIdx.x;
+  for (; i + 3 * 256 < words; i += 4 * 256) {
+    u32x4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = ((const u32x4*)p)[i + 256 * u];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      __builtin_nontemporal_store(scaled<T>(v[u], f), (u32x4*)o + i + 256 * u);
   }
-  const int64_t i = words * W + threadIdx.x;
+  for (; i < words; i += 256) ((u32x4*)o)[i] = scaled<T>(((const u32x4*)p)[i], f);
+  i = words * W + threadIdx.x;
   if (i < n) o[i] = (T)((float)p[i] * f);
 }
 
@@ -111,8 +124,8 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(GradArgs a) {
   const bool finite = (__float_as_uint(norm) & 0x7f800000u) != 0x7f800000u;
   const float f = finite && norm > a.limit ? a.limit / norm : 1.f;
   if (f == 1.f && a.src[t] == a.dst[t]) return;
-  const int64_t at = (int64_t)(wg - a.first[t]) * GRAD_SPAN;
-  const int64_t n = a.size[t] - at < GRAD_SPAN ? a.size[t] - at : GRAD_SPAN;
+  const int64_t at = (int64_t)(wg - a.first[t]) * a.span;
+  const int64_t n = a.size[t] - at < a.span ? a.size[t] - at : a.span;
   if (a.dtype[t] == TRIATTN_BF16) scale((const bf16*)a.src[t] + at, (bf16*)a.dst[t] + at, n, f);
   else scale((const float*)a.src[t] + at, (float*)a.dst[t] + at, n, f);
 }

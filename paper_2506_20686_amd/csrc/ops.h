@@ -107,8 +107,8 @@ struct GradArgs {
   int wg0;                      // workgroups of earlier launches
   const float* norm;
   float limit;
+  int64_t span;                 // elements of a workgroup
 };
-constexpr int64_t GRAD_SPAN = 1 << 15;  // elements of a workgroup
 hipError_t launch_grad_squares(const GradArgs& a, hipStream_t s);
 hipError_t launch_grad_root(const double* part, int64_t count, float* norm, hipStream_t s);
 hipError_t launch_grad_scale(const GradArgs& a, hipStream_t s);

@@ -574,6 +574,9 @@ void fwd_dma_kernel(FwdArgs<bf16> a) {
       };
 #pragma unroll
       for (int i = 0; i < FO_QT; ++i) {
+        // wait states the compiler misses where the branch around the mask follows the products
+        // at once: it counts those of the longer path
+        asm volatile("s_nop 3" : "+v"(s[i]));
         if (wb != 0xffffffffu) mask_rows(s[i], wb, g);
         weights(i);
         if (__any(!(t0[i] + t1[i] <= WEIGHT_LIMIT))) {
@@ -586,6 +589,8 @@ void fwd_dma_kernel(FwdArgs<bf16> a) {
           }
 #pragma unroll
           for (int t = 0; t < KC; ++t) s[i] = M::mma(kfrag(S * L::KS, t), qf[i][t], s[i]);
+          // likewise
+          asm volatile("s_nop 3" : "+v"(s[i]));
           if (wb != 0xffffffffu) mask_rows(s[i], wb, g);
           const float mx = wave_xor32_max(max16(s[i])) * c1;
           const float mnew = fmaxf(m[i], mx);

@@ -20,7 +20,7 @@ import pytest
 from paper_2506_20686_amd import build as hipbuild
 
 HIPCC = hipbuild.HIPCC
-SOURCES = ("xat_fwd.hip", "xat_bwd.hip", "glu.hip")
+SOURCES = ("fwd.hip", "xat_fwd.hip", "xat_bwd.hip", "glu.hip")
 needs_hipcc = pytest.mark.skipif(not (os.path.exists(HIPCC) or shutil.which("hipcc")),
                                  reason="hipcc not available")
 
@@ -148,7 +148,8 @@ def test_scanner_finds_a_planted_hazard():
 @pytest.mark.parametrize("src", SOURCES)
 def test_results_are_waited_for_on_every_path(tmp_path, src):
     out = tmp_path / (src + ".s")
-    cmd = [HIPCC, *hipbuild.FLAGS, "--cuda-device-only", "-S",
+    ilp = hipbuild.ILP_FLAGS if src in hipbuild.MAX_ILP else []
+    cmd = [HIPCC, *hipbuild.FLAGS, *ilp, "--cuda-device-only", "-S",
            "-I", os.path.join(hipbuild.ROOT, "include"), "-I", hipbuild.CSRC,
            os.path.join(hipbuild.CSRC, src), "-o", str(out)]
     res = subprocess.run(cmd, capture_output=True, text=True)

@@ -423,8 +423,8 @@ int tri_rel_bias_bwd(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges
  *   d a multiple of 8, at most 128 (TRIATTN_ERR_UNSUPPORTED else); heads a multiple of
  *   key_heads, at most 256 (TRIATTN_ERR_UNSUPPORTED above); 1 <= nq, nk <= 2^22;
  *   1 <= batch <= 2^20; scale finite and positive; with g = heads / key_heads, (nq g + 256) g
- *   < 2^32, and fewer than 2^24 workgroups and at most 2^34 elements in q, in k and in a map of
- *   the bias (TRIATTN_ERR_UNSUPPORTED).
+ *   < 2^32, and fewer than 2^24 workgroups and at most 2^34 elements in q and in k, and fewer
+ *   in a map of the bias with 64 keys more (TRIATTN_ERR_UNSUPPORTED).
  *   bias entries may be -inf (the key is excluded) or as low as the type goes.  Masked keys
  *   have no effect whatever they, or their bias entries, hold (NaN and infinities too), and
  *   zero gradients.  A query without a valid key gets out = 0 and no gradient.  Everything
@@ -492,7 +492,8 @@ int tri_gated_linear_bwd(int dtype, int64_t m, int64_t k, int64_t f, int act, co
  * count tensors, grads[i] of sizes[i] elements of dtypes[i] (TRIATTN_F32 or TRIATTN_BF16, mixed
  * as they come), contiguous, 16-byte aligned (a tensor of no elements may be NULL).  dtypes,
  * sizes, grads and outs are HOST arrays, read during the call.  outs[i] may be grads[i] (then
- * nothing is written where nothing is scaled); no other overlap.
+ * nothing is written where nothing is scaled); no other overlap, of outs among themselves
+ * either.
  *   The squares are summed in 64 bits in a fixed order (bitwise reproducible).  Elements may
  * hold anything: NaN and infinities show in norm.  tri_grad_clip takes norm from device memory,
  * so that it may be the norm over several GPUs; a norm that is not finite scales nothing.

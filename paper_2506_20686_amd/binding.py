@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import functools
 import math
 import os
 from typing import Optional
@@ -1018,8 +1019,10 @@ def rel_bias_bwd(pos, edges, dout, chain=None, workspace: Optional[torch.Tensor]
 
 # ---- cross attention, gated linear projection, clipping of gradients --------------------------
 
+@functools.lru_cache(maxsize=1024)
 def _sized(name, *args) -> int:
-    """What a *_workspace_bytes function of the library says."""
+    """What a *_workspace_bytes function of the library says: a function of the sizes
+    alone (kept, since asking takes as long as a small call's other arguments)."""
     n = _sz(0)
     st = getattr(lib(), name)(*args, ctypes.byref(n))
     if st != OK:
@@ -1030,22 +1033,26 @@ def _sized(name, *args) -> int:
 def _cross_common(q, k, v, bias, mask):
     """Checks; returns the sizes as the library takes them, the device, the shapes of
     the statistics."""
-    for name, t in (("q", q), ("k", k)):
-        if not isinstance(t, torch.Tensor):
-            raise TypeError(f"{name} must be a torch.Tensor")
-    if q.dim() not in (3, 4) or k.dim() != q.dim():
+    if not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor):
+        raise TypeError("q and k must be torch.Tensors")
+    shape, kshape, dtype, dev = q.shape, k.shape, q.dtype, q.device
+    if len(shape) == 4 and len(kshape) == 4:
+        batch, nq, h, d = shape
+        nk, hk = kshape[1], kshape[2]
+        lead = (batch,)
+    elif len(shape) == 3 and len(kshape) == 3:
+        nq, h, d = shape
+        nk, hk = kshape[0], kshape[1]
+        batch, lead = 1, ()
+    else:
         raise ValueError("q must be [nq, h, d] and k [nk, hk, d], or both with a batch axis")
-    dt = _DTYPES.get(q.dtype)
+    dt = _DTYPES.get(dtype)
     if dt is None:
-        raise ValueError(f"unsupported dtype {q.dtype}")
-    dev, dtype = q.device, q.dtype
-    lead = tuple(q.shape[:-3])
-    nq, h, d = q.shape[-3:]
-    nk, hk = k.shape[-3:-1]
-    _check("q", q, q.shape, dtype, dev)
+        raise ValueError(f"unsupported dtype {dtype}")
+    _check("q", q, shape, dtype, dev)
     _check("k", k, lead + (nk, hk, d), dtype, dev)
-    _check("v", v, k.shape, dtype, dev)
-    batch, bias_batch = lead[0] if lead else 1, 0
+    _check("v", v, kshape, dtype, dev)
+    bias_batch = 0
     if bias is not None:
         if not isinstance(bias, torch.Tensor):
             raise TypeError("bias must be a torch.Tensor")
@@ -1147,7 +1154,7 @@ def gated_linear_bwd(x, w, dout, bias=None, act: int = ACT_SILU,
 class GradList:
     """A list of gradients (fp32 and bf16 tensors of one GPU, of any shapes, contiguous),
     checked once, for programs that clip the same ones step after step.  A call
-    looks up the tensors' addresses anew."""
+    looks up the tensors' addresses anew.  A tensor may be there once only."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
@@ -1162,18 +1169,26 @@ class GradList:
             if t.dtype not in _DTYPES:
                 raise ValueError(f"tensors[{i}]: unsupported dtype {t.dtype}")
             _check(f"tensors[{i}]", t, t.shape, t.dtype, self.device)
+        at = [t.data_ptr() for t in self.tensors if t.numel()]
+        if len(set(at)) != len(at):
+            raise ValueError("a tensor is in the list twice")
         self.count = len(self.tensors)
         self.shapes = [t.shape for t in self.tensors]
         self.dtypes = array.array("i", [_DTYPES[t.dtype] for t in self.tensors])
         self.sizes = array.array("q", [t.numel() for t in self.tensors])
-        self.workspace_bytes = _sized("tri_grad_norm_workspace_bytes", self.count,
-                                      self.sizes.buffer_info()[0])
+        need = _sz(0)
+        st = lib().tri_grad_norm_workspace_bytes(self.count, self.sizes.buffer_info()[0],
+                                                 ctypes.byref(need))
+        if st != OK:
+            raise TriAttnError(st, "tri_grad_norm_workspace_bytes")
+        self.workspace_bytes = need.value
 
     def addresses(self):
-        """The tensors' addresses now; ValueError if one is not what was checked."""
-        for t, shape in zip(self.tensors, self.shapes):
-            if t.shape != shape or not t.is_contiguous():
-                raise ValueError(f"a tensor of the list has changed (was {tuple(shape)})")
+        """The tensors' addresses now; ValueError if one is not of the size that was
+        checked, or not contiguous."""
+        for t, n in zip(self.tensors, self.sizes):
+            if t.numel() != n or not t.is_contiguous():
+                raise ValueError(f"a tensor of the list has changed (had {n} elements)")
         return array.array("Q", [t.data_ptr() for t in self.tensors])
 
 

@@ -42,7 +42,8 @@ int xat_sizes(int dtype, int64_t batch, int64_t nq, int64_t nk, int64_t h, int64
   // at most one workgroup for 32 rows, keys or a chunk of a bias row, times the splits of few
   if (batch * hk * ((nq * g + 31) / 32) >= MAX_WGS || batch * hk * ((nk + 31) / 32) >= MAX_WGS)
     return TRIATTN_ERR_UNSUPPORTED;
-  if (bias_batch * nq * ((nk + 63) / 64 * 4) >= MAX_WGS || (bias_batch > 0 && nq * nk > most / h))
+  if (bias_batch * nq * ((nk + 63) / 64 * 4) >= MAX_WGS || 
+      (bias_batch > 0 && nq * (nk + 64) >= most / h))
     return TRIATTN_ERR_UNSUPPORTED;
   a->batch = batch;
   a->nq = (int)nq;

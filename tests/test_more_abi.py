@@ -53,7 +53,8 @@ XAT_SIZES = [(dict(dtype=-1), INV), (dict(dtype=2), INV), (dict(b=0), INV),
              (dict(d=20), UNS), (dict(d=4), UNS), (dict(nq=1 << 22, h=64, hk=1), UNS),
              (dict(b=1 << 20, nq=1 << 10, h=16, hk=16, d=128, bb=1), UNS),
              (dict(b=1 << 20, nk=1 << 13, nq=1, h=1, hk=1, d=8, bb=1), UNS),
-             (dict(nq=1 << 21, nk=65, bb=1), UNS)]
+             (dict(nq=1 << 21, nk=65, bb=1), UNS),
+             (dict(nq=1 << 13, nk=(1 << 13) - 63, h=256, hk=256, d=8, bb=1), UNS)]
 XAT_ARGS = [(dict(scale=s), INV) for s in (0.0, -1.0, NAN, INF)] + [
     (dict([(k, v)]), INV) for k in ("q", "k", "v", "out", "stat") for v in (None, P + 8)] + [
     (dict(bias=None), INV), (dict(bias=P + 8), INV), (dict(bb=0), INV), (dict(ws=None), WS),
@@ -159,7 +160,9 @@ def test_workspace_sizes(lib):
             assert need >= 0 and need % 256 == 0
             assert call(lib.tri_gated_linear_bwd, GLU_BWD, GLU,
                         dict(dtype=dtype, m=m, k=k, f=f, wsb=need - 1)) == WS
-    need = B._sized("tri_grad_norm_workspace_bytes", 3, GRAD["sizes"])
+    z = ctypes.c_size_t(0)
+    assert lib.tri_grad_norm_workspace_bytes(3, GRAD["sizes"], ctypes.byref(z)) == B.OK
+    need = z.value
     assert need % 256 == 0 and call(lib.tri_grad_norm, GRAD_NORM, GRAD, dict(wsb=need - 1)) == WS
 
 

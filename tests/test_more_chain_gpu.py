@@ -212,7 +212,7 @@ def test_wrappers_refuse_what_the_library_cannot_take():
                  lambda: B.gated_linear_bwd(x, w, x), lambda: B.gated_linear_fwd(x.cpu(), w.cpu()),
                  lambda: B.grad_norm([x, w.cpu()]), lambda: B.grad_norm([x.t()]),
                  lambda: B.grad_clip([x], B.grad_norm([x]), 1.0, [w]),
-                 lambda: B.grad_clip([x], stat, 1.0),
+                 lambda: B.grad_clip([x], stat, 1.0), lambda: B.grad_norm([x, w, x]),
                  lambda: B.grad_clip([x], B.grad_norm([x]).double(), 1.0)):
         with pytest.raises(ValueError):
             call()

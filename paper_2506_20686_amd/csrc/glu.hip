@@ -41,22 +41,29 @@ __device__ inline float gate_value(float z, int act) {
   return p;
 }
 
+// Four packed bf16 of an accumulator quad.
+__device__ inline u32x2 pack4(float a, float b, float c, float d) {
+  return __builtin_bit_cast(u32x2, bf16x4{(bf16)a, (bf16)b, (bf16)c, (bf16)d});
+}
+// The four values' next plane of bf16, taken off them.
+__device__ inline u32x2 take_plane(float& a, float& b, float& c, float& d) {
+  const u32x2 w = pack4(a, b, c, d);
+  a -= __uint_as_float(w[0] << 16);
+  b -= __uint_as_float(w[0] & 0xffff0000u);
+  c -= __uint_as_float(w[1] << 16);
+  d -= __uint_as_float(w[1] & 0xffff0000u);
+  return w;
+}
+
 // The first `have` (whole words) of 8 values as three planes of bf16, `plane` elements apart.
 __device__ inline void put_planes(bf16* p, int64_t plane, int have, float (&f)[8]) {
 #pragma unroll
   for (int u = 0; u < 3; ++u) {
-    struct B {
-      bf16 e[8];
-    } b;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      b.e[e] = (bf16)f[e];
-      if (u < 2) f[e] -= (float)b.e[e];
-    }
-    const u32x4 w = __builtin_bit_cast(u32x4, b);
+    const u32x2 lo = take_plane(f[0], f[1], f[2], f[3]), hi = take_plane(f[4], f[5], f[6], f[7]);
+    const u32x4 w{lo[0], lo[1], hi[0], hi[1]};
     // (fp32's whole words are 4 elements: half a word here, and the second half may start there)
     if (have >= 8) ((Any16*)(p + u * plane))->v = w;
-    else if (have > 0) *(u32x2*)(p + u * plane) = u32x2{w[0], w[1]};
+    else if (have > 0) *(u32x2*)(p + u * plane) = lo;
   }
 }
 
@@ -143,10 +150,6 @@ __device__ inline void stage_w(const GluArgs& a, char* t) {
   }
 }
 
-// Four packed bf16 of an accumulator quad.
-__device__ inline u32x2 pack4(float a, float b, float c, float d) {
-  return __builtin_bit_cast(u32x2, bf16x4{(bf16)a, (bf16)b, (bf16)c, (bf16)d});
-}
 // Quads i (columns 8 i + 4 g ..) of a row's 32 results -> this lane's columns 16 g .. + 7 and
 // 16 g + 8 .. + 15, by exchanges between the two halves of the wave.
 __device__ inline void row_words(const u32x2 (&q)[4], u32x4 (&w)[2]) {
@@ -343,15 +346,8 @@ __global__ __launch_bounds__(GLU_BWD_WG) void glu_narrow_bwd_kernel(GluArgs a, L
         for (int e = 0; e < 4; ++e) f[e] = z[8 * h + 4 * i + e];
         char* to = lds + Z + h * LINES + Square::chunk_at(lane & 31, 2 * wave + i) + 8 * g;
 #pragma unroll
-        for (int p = 0; p < 3; ++p) {
-          bf16x4 b;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            b[e] = (bf16)f[e];
-            if (p < 2) f[e] -= (float)b[e];
-          }
-          *(bf16x4*)(to + 2 * p * LINES) = b;
-        }
+        for (int p = 0; p < 3; ++p)
+          *(u32x2*)(to + 2 * p * LINES) = take_plane(f[0], f[1], f[2], f[3]);
       }
     __syncthreads();
     if (o.dw) {
@@ -377,19 +373,18 @@ __global__ __launch_bounds__(GLU_BWD_WG) void glu_narrow_bwd_kernel(GluArgs a, L
         for (int t = 0; t < 8; ++t)
           gx = Mma<bf16>::mma(
               wx[t], Square::along(lds + Z + (2 * p + half) * LINES, 0, 16 * t, lane), gx);
-      f32x4* part = (f32x4*)(lds + P) + ((wave & 3) * 64 + lane) * 4;
+      f32x4* part = (f32x4*)(lds + P) + (wave & 3) * 256 + lane;
       if (half) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          part[i ^ (lane & 3)] =
-              f32x4{gx[4 * i], gx[4 * i + 1], gx[4 * i + 2], gx[4 * i + 3]};
+          part[64 * i] = f32x4{gx[4 * i], gx[4 * i + 1], gx[4 * i + 2], gx[4 * i + 3]};
       }
       __syncthreads();
       if (!half) {
         u32x2 q[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const f32x4 y = part[i ^ (lane & 3)];
+          const f32x4 y = part[64 * i];
           q[i] = pack4(gx[4 * i] + y[0], gx[4 * i + 1] + y[1], gx[4 * i + 2] + y[2],
                        gx[4 * i + 3] + y[3]);
         }

@@ -351,9 +351,9 @@ inline int xat_row_splits(int dtype, const XatArgs& a) {
 
 
 // Waves a SIMD that a kernel's registers have to leave room for: backward, forward.
-template <typename T, int DP>
+template <typename T, int DP, int NW>
 constexpr int xat_waves() {
-  return DP <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1;
+  return DP <= (sizeof(T) == 2 || NW == 4 ? 64 : 32) ? 2 : 1;
 }
 template <typename T, int DP, int NW, int MODE>
 constexpr int xat_fwd_waves() {

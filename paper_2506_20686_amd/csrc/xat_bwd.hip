@@ -48,7 +48,7 @@ __device__ inline float* part_e(const XatArgs& a, int split, int64_t R) {
 }
 
 template <typename T, int DP, int NW, int MODE, int KW>
-__global__ __launch_bounds__(64 * NW * KW, (xat_waves<T, DP>())) void xat_dq_kernel(XatArgs a,
+__global__ __launch_bounds__(64 * NW * KW, (xat_waves<T, DP, NW>())) void xat_dq_kernel(XatArgs a,
                                                                                    int tiles) {
   constexpr bool BIAS = MODE != XB_NONE, HEADS = MODE == XB_HEADS;
   constexpr int SW = HEADS ? 1 : NW;  // waves that share a tile
@@ -275,7 +275,7 @@ struct RowStage {
 };
 
 template <typename T, int DP, int NW, int MODE, int KW, typename DS = float>
-__global__ __launch_bounds__(64 * NW * KW, (xat_waves<T, DP>())) void xat_dkv_kernel(XatArgs a,
+__global__ __launch_bounds__(64 * NW * KW, (xat_waves<T, DP, NW>())) void xat_dkv_kernel(XatArgs a,
                                                                                     int tiles) {
   constexpr bool BIAS = MODE != XB_NONE, HEADS = MODE == XB_HEADS;
   constexpr int SW = HEADS ? 1 : NW;  // waves that share a tile

@@ -52,8 +52,8 @@ __global__ __launch_bounds__(256) void xat_dbias_kernel(XatArgs a, int chunks) {
 }
 
 // Sums over the samples of their maps ([batch][stride]): 4 columns a thread, or, of many samples
-// and few columns, 16 columns and 64 slices of the samples a workgroup.  To dbias itself, or (PLANES)
-// to the first sample's map, each column by the one workgroup that reads it.
+// and few columns, 16 columns and 64 slices of the samples a workgroup.  To dbias itself, or
+// (PLANES) to the first sample's map, each column by the one workgroup that reads it.
 template <typename T, bool PLANES>
 __global__ __launch_bounds__(256) void xat_sum_kernel(XatArgs a, int64_t cols) {
   const int64_t i = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
@@ -76,8 +76,8 @@ template <typename T, bool PLANES>
 void sum_launch(const XatArgs& a, int64_t cols, hipStream_t s) {
   // (the columns, a multiple of 4, make fewer than 2^24 workgroups either way)
   if (a.batch >= 16 && cols < (int64_t)1 << 20)
-    hipLaunchKernelGGL((xat_slab_sum_kernel<T, PLANES>), dim3(slab_grid(cols)), dim3(SLAB_WG), 0, s, a,
-                       cols);
+    hipLaunchKernelGGL((xat_slab_sum_kernel<T, PLANES>), dim3(slab_grid(cols)), dim3(SLAB_WG), 0, s,
+                       a, cols);
   else
     hipLaunchKernelGGL((xat_sum_kernel<T, PLANES>), dim3((unsigned)((cols / 4 + 255) / 256)),
                        dim3(256), 0, s, a, cols);

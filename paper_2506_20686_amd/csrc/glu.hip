@@ -255,8 +255,8 @@ __global__ __launch_bounds__(256, 2) void glu_narrow_fwd_kernel(GluArgs a) {
 //   dW   32 columns of dz a wave, all of k, in registers to the end;
 //   dx   a tile of 32 of k and one half of dz's columns a wave; the halves meet in LDS.
 // 48 of a wave's 56 matrix instructions a block are the three planes' (24 bits of dz).  589,824 x
-// 128 x 128: 346 us, 270 GFLOP of matrix instructions; the matrix cores are busy 44% of the time,
-// the vector units 33%, LDS 44%, in phases that follow each other.  (The general kernels: 598 us.
+// 128 x 128: 346 us, 270 GFLOP of matrix instructions; the matrix cores are busy 45% of the time,
+// the vector units 33%, LDS 32%, in phases that follow each other.  (The general kernels: 598 us.
 // The next block's z and dz beside this one's dW, with a barrier less: 380.)
 constexpr int GLU_BWD_WG = 512;
 template <int ACT>

@@ -13,7 +13,7 @@
 // Bound, with long loops, by vector issue: an exponential a logit (a quarter of the rate) and some
 // 100 other instructions a 32 x 32 tile, beside 8 matrix instructions of 64 channels.  2 x 2048 x
 // 4099, 16 heads of 64, a quarter of the keys masked: 107 us (640 TFLOP/s of all keys, 480 of the
-// valid ones; the vector units 62% busy at the two waves a SIMD that 512 workgroups make).  One
+// valid ones; the vector units 55% busy at the two waves a SIMD that 512 workgroups make).  One
 // query to 30,011 keys: 24 us, 3.8 TB/s.  737 windows of 32 x 128 with a bias: 20 us, 4.2 TB/s.
 #include "timing.h"
 #include "triattn.h"

@@ -59,7 +59,7 @@ int xat_sizes(int dtype, int64_t batch, int64_t nq, int64_t nk, int64_t h, int64
 
 size_t xat_ws(const triattn::XatPlan& p) {
   return round256(p.planes) + round256(p.part) + round256(p.part_q) + round256(p.dsum) +
-         round256(p.single) + round256(p.dplanes) + 256;
+         round256(p.single) + round256(p.valid) + round256(p.dplanes) + 256;
 }
 void xat_place(const triattn::XatPlan& p, void* workspace, triattn::XatArgs* a) {
   char* w = (char*)workspace;
@@ -76,6 +76,8 @@ void xat_place(const triattn::XatPlan& p, void* workspace, triattn::XatArgs* a) 
   w += round256(p.dsum);
   a->single = (int*)w;
   w += round256(p.single);
+  a->valid = (int*)w;
+  w += round256(p.valid);
   a->dplanes = (float*)w;
 }
 

@@ -166,12 +166,13 @@ struct XatArgs {
   float* part_q;              // and of the rows
   float* dsum;                // [batch][nq][h]
   int* single;                // [batch]: whether it has one valid key at most
+  int* valid;                 // [batch][splits]: a split's valid keys
   float* dplanes;             // dbias of every sample, [batch][hk][nq * group][nkp] or as dbias
 };
 
 struct XatPlan {
   int nkp, splits, splits_q;
-  size_t planes, part, part_q, dsum, single, dplanes;  // bytes of workspace, 0 for none
+  size_t planes, part, part_q, dsum, single, valid, dplanes;  // bytes of workspace, 0 for none
 };
 XatPlan xat_fwd_plan(int dtype, const XatArgs& a);
 XatPlan xat_bwd_plan(int dtype, const XatArgs& a);

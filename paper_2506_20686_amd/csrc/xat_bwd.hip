@@ -169,8 +169,12 @@ __global__ __launch_bounds__(64 * NW * KW, (xat_waves<T, DP, NW>())) void xat_dq
       valid += count[head + NW * k];
     }
   }
+  // (of split keys, the sample's are known to the join)
   const bool single = a.splits == 1 && valid <= 1;
-  if (w.tile == 0 && w.kh == 0 && w.split == 0 && threadIdx.x == 0) a.single[w.b] = single;
+  if (w.tile == 0 && w.kh == 0 && threadIdx.x == 0) {
+    if (a.splits > 1) a.valid[w.b * a.splits + w.split] = valid;
+    else a.single[w.b] = single;
+  }
   if (r >= rows) return;
   if (a.splits > 1) {
     float *ps = part_ab(a, w.split, R, 0), *pp = part_ab(a, w.split, R, 1);
@@ -214,18 +218,25 @@ __global__ __launch_bounds__(256) void xat_dq_join_kernel(XatArgs a) {
   if (i >= all * quads) return;
   const int64_t R = i / quads;
   const int ch = 4 * (int)(i % quads);
+  const int64_t rows = (int64_t)a.nq * a.h, b = R / rows;
   f32x4 sk{}, pk{};
   float e = 0.f;
+  int valid = 0;
   for (int s = 0; s < a.splits; ++s) {
     sk += *(const f32x4*)(part_ab(a, s, R, 0) + ch);
     pk += *(const f32x4*)(part_ab(a, s, R, 1) + ch);
     e += *part_e(a, s, R);
+    valid += a.valid[b * a.splits + s];
   }
+  const bool single = valid <= 1;
   f32x4 x;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) x[u] = a.scale * fmaf(-e, pk[u], sk[u]);
+  for (int u = 0; u < 4; ++u) x[u] = single ? 0.f : a.scale * fmaf(-e, pk[u], sk[u]);
   store4((T*)a.dq + R * a.d + ch, x);
-  if (ch == 0) a.dsum[R] += e;
+  if (ch == 0) {
+    a.dsum[R] += e;
+    if (R == b * rows) a.single[b] = single;
+  }
 }
 
 // Tiles of BQ rows of q and dout, and the rows' statistics.
@@ -560,6 +571,7 @@ XatPlan xat_bwd_plan(int dtype, const XatArgs& a) {
   }
   p.dsum = (size_t)all * sizeof(float);
   p.single = (size_t)a.batch * sizeof(int);
+  if (p.splits > 1) p.valid = (size_t)a.batch * p.splits * sizeof(int);
   if (p.splits > 1) p.part = (size_t)p.splits * all * (2 * a.d + 1) * sizeof(float);
   if (p.splits_q > 1) p.part_q = (size_t)p.splits_q * keys * 2 * a.d * sizeof(float);
   return p;

@@ -1,0 +1,44 @@
+"""Cross attention through the C ABI: one valid key in loops that are split (bounds in
+cross_ref.py)."""
+import pytest
+import torch
+
+import ops_ref as R
+from paper_2506_20686_amd import binding as B
+from test_cross_attn_gpu import DEV, BF, F4, both, dev, inputs
+
+pytestmark = pytest.mark.gpu
+
+
+# (queries, keys, heads, key heads): loops of 2 to 8 splits; tiles shared by four waves, a
+# wave's own in groups of four, and four heads side by side in groups of two
+@pytest.mark.parametrize("dtype", [BF, F4])
+@pytest.mark.parametrize("bias", ["none", "shared", "each"])
+@pytest.mark.parametrize("nq,nk,h,hk", [(50, 900, 4, 2), (50, 2100, 4, 2), (50, 2100, 4, 4),
+                                        (5, 2100, 4, 2), (3, 1500, 1, 1)])
+def test_one_valid_key_of_split_loops(nq, nk, h, hk, bias, dtype):
+    # samples of one valid key in the first, a middle and the last split; of two keys in
+    # different splits, which have gradients; of none
+    q, k, v, x, _, y = inputs(5, nq, nk, h, hk, 32, dtype, bias, seed=nk + nq)
+    one = (3, nk // 2 + 1, nk - 1)
+    m = torch.zeros(5, nk, dtype=torch.uint8)
+    for b, at in enumerate(one):
+        m[b, at] = 1
+    m[3, 1] = m[3, nk - 2] = 1
+    out, stat = B.cross_attn_fwd(dev(q), dev(k), dev(v), dev(x), dev(m))
+    # P is exp2 of the rounding of s c alone, 1 up to that, and out = (v P) (1 / P): the product
+    # by matrix instructions (2 U), the reciprocal and the product (U each), out's own rounding
+    for b, at in enumerate(one):
+        want = v[b, at].repeat_interleave(h // hk, dim=0)[None].expand(nq, -1, -1).double()
+        R.check("out", out[b], want, (R.HALF[dtype] + 4.1 * R.U) * want.abs())
+    dq, dk, dv, db = B.cross_attn_bwd(dev(q), dev(k), dev(v), out, stat, dev(y), dev(x), dev(m))
+    for b in (0, 1, 2, 4):
+        assert not bool(dq[b].any()) and not bool(dk[b].any())
+        if bias == "each":
+            assert not bool(db[b].any())
+    assert bool(dq[3].any()) and bool(dk[3].any()) and not bool(dv[4].any())
+    if bias == "shared":  # of the sample with two keys alone
+        keys = torch.arange(nk)
+        assert not bool(db[:, (keys != 1) & (keys != nk - 2)].any())
+    keep = slice(0, 4)  # the plain form has no row without a key
+    both(q[keep], k[keep], v[keep], x[keep] if bias == "each" else x, m[keep], y[keep])

@@ -12,6 +12,7 @@ import array
 import ctypes
 import functools
 import math
+import operator
 import os
 from typing import Optional
 
@@ -1151,6 +1152,9 @@ def gated_linear_bwd(x, w, dout, bias=None, act: int = ACT_SILU,
     return dx, dw, dbias
 
 
+_dtype_of = operator.attrgetter("dtype")
+
+
 class GradList:
     """A list of gradients (fp32 and bf16 tensors of one GPU, of any shapes, contiguous),
     checked once, for programs that clip the same ones step after step.  A call
@@ -1174,8 +1178,11 @@ class GradList:
             raise ValueError("a tensor is in the list twice")
         self.count = len(self.tensors)
         self.shapes = [t.shape for t in self.tensors]
-        self.dtypes = array.array("i", [_DTYPES[t.dtype] for t in self.tensors])
-        self.sizes = array.array("q", [t.numel() for t in self.tensors])
+        self._kinds = [t.dtype for t in self.tensors]
+        self._numels = [t.numel() for t in self.tensors]
+        self._places = [t.get_device() for t in self.tensors]  # -1 off the GPUs
+        self.dtypes = array.array("i", [_DTYPES[k] for k in self._kinds])
+        self.sizes = array.array("q", self._numels)
         need = _sz(0)
         st = lib().tri_grad_norm_workspace_bytes(self.count, self.sizes.buffer_info()[0],
                                                  ctypes.byref(need))
@@ -1184,12 +1191,16 @@ class GradList:
         self.workspace_bytes = need.value
 
     def addresses(self):
-        """The tensors' addresses now; ValueError if one is not of the size that was
-        checked, or not contiguous."""
-        for t, n in zip(self.tensors, self.sizes):
-            if t.numel() != n or not t.is_contiguous():
-                raise ValueError(f"a tensor of the list has changed (had {n} elements)")
-        return array.array("Q", [t.data_ptr() for t in self.tensors])
+        """The tensors' addresses now; ValueError if one is no longer of the size, the dtype
+        or the device that were checked, or not contiguous."""
+        t = self.tensors
+        if (list(map(_dtype_of, t)) != self._kinds
+                or list(map(torch.Tensor.numel, t)) != self._numels
+                or list(map(torch.Tensor.get_device, t)) != self._places
+                or not all(map(torch.Tensor.is_contiguous, t))):
+            raise ValueError("a tensor of the list has another dtype, size or device than when "
+                             "the list was made, or is not contiguous")
+        return array.array("Q", map(torch.Tensor.data_ptr, t))
 
 
 def _grad_list(grads):

@@ -31,3 +31,13 @@ def test_a_changed_dtype_is_refused(kept, was, now):
     t[1].data = torch.zeros(60, dtype=now)
     with pytest.raises(ValueError):
         g.addresses()
+
+
+@pytest.mark.parametrize("change", [lambda l: l.append(torch.zeros(3)), lambda l: l.pop(),
+                                    lambda l: l.clear(), lambda l: l.insert(0, torch.zeros(5))])
+def test_a_changed_number_of_tensors_is_refused(kept, change):
+    # the list is the one that grad_clip returns
+    g = kept(torch.zeros(5), torch.zeros(5))
+    change(g.tensors)
+    with pytest.raises(ValueError):
+        g.addresses()

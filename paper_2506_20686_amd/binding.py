@@ -1173,9 +1173,6 @@ class GradList:
             if t.dtype not in _DTYPES:
                 raise ValueError(f"tensors[{i}]: unsupported dtype {t.dtype}")
             _check(f"tensors[{i}]", t, t.shape, t.dtype, self.device)
-        at = [t.data_ptr() for t in self.tensors if t.numel()]
-        if len(set(at)) != len(at):
-            raise ValueError("a tensor is in the list twice")
         self.count = len(self.tensors)
         self.shapes = [t.shape for t in self.tensors]
         self._kinds = [t.dtype for t in self.tensors]
@@ -1189,10 +1186,13 @@ class GradList:
         if st != OK:
             raise TriAttnError(st, "tri_grad_norm_workspace_bytes")
         self.workspace_bytes = need.value
+        # different addresses: tensors of no elements have none (0)
+        self._apart = sum(n > 0 for n in self._numels) + (0 in self._numels)
+        self.addresses()
 
     def addresses(self):
         """The tensors' addresses now; ValueError if one is no longer of the size, the dtype
-        or the device that were checked, or not contiguous."""
+        or the device that were checked, not contiguous, or in the list twice."""
         t = self.tensors
         if (list(map(_dtype_of, t)) != self._kinds
                 or list(map(torch.Tensor.numel, t)) != self._numels
@@ -1200,7 +1200,10 @@ class GradList:
                 or not all(map(torch.Tensor.is_contiguous, t))):
             raise ValueError("a tensor of the list has another dtype, size or device than when "
                              "the list was made, or is not contiguous")
-        return array.array("Q", map(torch.Tensor.data_ptr, t))
+        at = array.array("Q", map(torch.Tensor.data_ptr, t))
+        if len(set(at)) != self._apart:
+            raise ValueError("a tensor is in the list twice")
+        return at
 
 
 def _grad_list(grads):

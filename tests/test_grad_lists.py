@@ -41,3 +41,14 @@ def test_a_changed_number_of_tensors_is_refused(kept, change):
     change(g.tensors)
     with pytest.raises(ValueError):
         g.addresses()
+
+
+def test_tensors_that_come_to_share_storage_are_refused(kept):
+    t = [torch.zeros(8), torch.zeros(0), torch.zeros(8), torch.zeros(0)]
+    g = kept(*t)
+    g.addresses()  # tensors of no elements share nothing
+    t[2].data = t[0].data
+    with pytest.raises(ValueError):
+        g.addresses()
+    t[2].data = torch.zeros(8)
+    g.addresses()

@@ -34,3 +34,15 @@ def test_a_changed_device_is_refused():
         B.grad_norm(g)
     with pytest.raises(ValueError):
         B.grad_clip(g, norm, 1.0)
+
+
+def test_tensors_that_come_to_share_storage_are_refused():
+    t = [torch.ones(64, device=DEV), torch.ones(64, device=DEV)]
+    g = B.GradList(t)
+    norm = B.grad_norm(g)
+    t[1].data = t[0].data
+    with pytest.raises(ValueError):
+        B.grad_norm(g)
+    with pytest.raises(ValueError):
+        B.grad_clip(g, norm, 1.0)
+    assert bool((t[0] == 1).all())

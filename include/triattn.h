@@ -492,8 +492,9 @@ int tri_gated_linear_bwd(int dtype, int64_t m, int64_t k, int64_t f, int act, co
  * count tensors, grads[i] of sizes[i] elements of dtypes[i] (TRIATTN_F32 or TRIATTN_BF16, mixed
  * as they come), contiguous, 16-byte aligned (a tensor of no elements may be NULL).  dtypes,
  * sizes, grads and outs are HOST arrays, read during the call.  outs[i] may be grads[i] (then
- * nothing is written where nothing is scaled); no other overlap, of outs among themselves
- * either.
+ * nothing is written where nothing is scaled); any other overlap, of outs among themselves
+ * too, is TRIATTN_ERR_INVALID_ARG (the check takes 16 bytes of host memory a tensor past 64
+ * tensors: TRIATTN_ERR_UNSUPPORTED without).
  *   The squares are summed in 64 bits in a fixed order (bitwise reproducible).  Elements may
  * hold anything: NaN and infinities show in norm.  tri_grad_clip takes norm from device memory,
  * so that it may be the norm over several GPUs; a norm that is not finite scales nothing.

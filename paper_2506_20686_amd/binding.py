@@ -1228,8 +1228,9 @@ def grad_norm(grads, workspace: Optional[torch.Tensor] = None):
 def grad_clip(grads, norm, max_norm: float, out=None):
     """Scales the gradients (a GradList or tensors) by max_norm / norm where norm, as
     grad_norm gives it, is above max_norm: into `out` (likewise, of the same
-    shapes and dtypes; the gradients themselves or no memory of theirs), in place
-    if None.  A norm that is not finite scales nothing.  Returns out's tensors."""
+    shapes and dtypes; the gradients themselves or no memory of theirs, which else is
+    refused), in place if None.  A norm that is not finite scales nothing.  Returns out's
+    tensors."""
     g = _grad_list(grads)
     o = g if out is None else _grad_list(out)
     if o is not g and (o.device != g.device or o.shapes != g.shapes or o.dtypes != g.dtypes):

@@ -3,6 +3,10 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include "ops.h"
 #include "triattn.h"
 
@@ -121,6 +125,35 @@ int grad_list(int64_t count, const int32_t* dtypes, const int64_t* sizes,
   for (int64_t i = 0; i < count; ++i)
     if (bad_dtype(dtypes[i]) || (sizes[i] > 0 && (list[i] == nullptr || !aligned16(list[i]))))
       return TRIATTN_ERR_INVALID_ARG;
+  return TRIATTN_OK;
+}
+// TRIATTN_OK if the results are apart from each other and from every gradient that is not
+// clipped in its place: workgroups would write what others have still to read.
+int grad_apart(int64_t count, const int32_t* dtypes, const int64_t* sizes,
+               const void* const* grads, void* const* outs) {
+  struct Span {
+    uintptr_t at, end;
+  };
+  Span few[64];
+  std::unique_ptr<Span[]> many;
+  if (count > 64) many.reset(new (std::nothrow) Span[count]);
+  Span* s = count > 64 ? many.get() : few;
+  if (s == nullptr) return TRIATTN_ERR_UNSUPPORTED;
+  auto bytes = [&](int64_t i) { return (uintptr_t)sizes[i] * (dtypes[i] == TRIATTN_BF16 ? 2 : 4); };
+  int64_t n = 0;
+  for (int64_t i = 0; i < count; ++i)
+    if (sizes[i] > 0) s[n++] = Span{(uintptr_t)outs[i], (uintptr_t)outs[i] + bytes(i)};
+  std::sort(s, s + n, [](const Span& a, const Span& b) { return a.at < b.at; });
+  for (int64_t i = 1; i < n; ++i)
+    if (s[i - 1].end > s[i].at) return TRIATTN_ERR_INVALID_ARG;
+  for (int64_t i = 0; i < count; ++i) {
+    if (sizes[i] == 0 || grads[i] == outs[i]) continue;
+    const uintptr_t at = (uintptr_t)grads[i];
+    // the first result that ends behind the gradient's start
+    const Span* x =
+        std::upper_bound(s, s + n, at, [](uintptr_t v, const Span& a) { return v < a.end; });
+    if (x != s + n && x->at < at + bytes(i)) return TRIATTN_ERR_INVALID_ARG;
+  }
   return TRIATTN_OK;
 }
 size_t grad_ws(int64_t wgs) { return round256((size_t)wgs * sizeof(double)) + 256; }
@@ -338,6 +371,8 @@ int tri_grad_clip(int64_t count, const int32_t* dtypes, const int64_t* sizes,
   if (st != TRIATTN_OK) return st;
   if (norm == nullptr || ((uintptr_t)norm & 3u) != 0) return TRIATTN_ERR_INVALID_ARG;
   if (!(isfinite(max_norm) && max_norm > 0.f)) return TRIATTN_ERR_INVALID_ARG;
+  st = grad_apart(count, dtypes, sizes, grads, outs);
+  if (st != TRIATTN_OK) return st;
   triattn::GradArgs a{};
   a.norm = norm;
   a.span = plan.span;

@@ -424,7 +424,10 @@ int tri_rel_bias_bwd(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges
  *   key_heads, at most 256 (TRIATTN_ERR_UNSUPPORTED above); 1 <= nq, nk <= 2^22;
  *   1 <= batch <= 2^20; scale finite and positive; with g = heads / key_heads, (nq g + 256) g
  *   < 2^32, and fewer than 2^24 workgroups and at most 2^34 elements in q and in k, and fewer
- *   in a map of the bias with 64 keys more (TRIATTN_ERR_UNSUPPORTED).
+ *   in a map of the bias with 64 keys more (TRIATTN_ERR_UNSUPPORTED).  Where the bias is turned
+ *   into planes first (heads not a multiple of 4 or sharing key heads, fp32 rows of more than 64
+ *   channels, 32 rows of a map past 2 GiB), it has fewer than 2^24 pieces of a row of 16 keys,
+ *   over all its maps.
  *   bias entries may be -inf (the key is excluded) or as low as the type goes.  Masked keys
  *   have no effect whatever they, or their bias entries, hold (NaN and infinities too), and
  *   zero gradients.  A query without a valid key gets out = 0 and no gradient.  Everything

@@ -43,12 +43,10 @@ int xat_sizes(int dtype, int64_t batch, int64_t nq, int64_t nk, int64_t h, int64
   if ((nq * g + 256) * g >= (int64_t)1 << 32) return TRIATTN_ERR_UNSUPPORTED;
   const int64_t most = (int64_t)1 << 34;
   if (batch * nq > most / (h * d) || batch * nk > most / (hk * d)) return TRIATTN_ERR_UNSUPPORTED;
-  // at most one workgroup for 32 rows, keys or a chunk of a bias row, times the splits of few
+  // at most one workgroup for 32 rows or keys, times the splits of few
   if (batch * hk * ((nq * g + 31) / 32) >= MAX_WGS || batch * hk * ((nk + 31) / 32) >= MAX_WGS)
     return TRIATTN_ERR_UNSUPPORTED;
-  if (bias_batch * nq * ((nk + 63) / 64 * 4) >= MAX_WGS || 
-      (bias_batch > 0 && nq * (nk + 64) >= most / h))
-    return TRIATTN_ERR_UNSUPPORTED;
+  if (bias_batch > 0 && nq * (nk + 64) >= most / h) return TRIATTN_ERR_UNSUPPORTED;
   a->batch = batch;
   a->nq = (int)nq;
   a->nk = (int)nk;
@@ -58,6 +56,9 @@ int xat_sizes(int dtype, int64_t batch, int64_t nq, int64_t nk, int64_t h, int64
   a->group = (int)g;
   a->inv_group = g == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + g - 1) / g);
   a->bias_batch = bias_batch;
+  // of a bias that is turned into planes, at most one for 16 keys of a row of its maps
+  if (triattn::xat_needs_planes(dtype, *a) && bias_batch * nq * ((nk + 63) / 64 * 4) >= MAX_WGS)
+    return TRIATTN_ERR_UNSUPPORTED;
   return TRIATTN_OK;
 }
 

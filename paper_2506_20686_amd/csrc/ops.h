@@ -174,6 +174,7 @@ struct XatPlan {
   int nkp, splits, splits_q;
   size_t planes, part, part_q, dsum, single, valid, dplanes;  // bytes of workspace, 0 for none
 };
+bool xat_needs_planes(int dtype, const XatArgs& a);  // of its bias
 XatPlan xat_fwd_plan(int dtype, const XatArgs& a);
 XatPlan xat_bwd_plan(int dtype, const XatArgs& a);
 hipError_t launch_xat_fwd(int dtype, const XatArgs& a, hipStream_t s);

@@ -278,13 +278,17 @@ hipError_t fwd(const XatArgs& a, hipStream_t s) {
 
 }  // namespace
 
+bool xat_needs_planes(int dtype, const XatArgs& a) {
+  return a.bias_batch > 0 && !xat_by_heads(dtype, a);
+}
+
 XatPlan xat_fwd_plan(int dtype, const XatArgs& a) {
   XatPlan p{};
   const int64_t all = a.batch * a.nq * a.h;
   p.nkp = (a.nk + 63) / 64 * 64;
   p.splits = xat_key_splits(dtype, a);
   const size_t e = dtype == TRIATTN_BF16 ? 2 : 4;
-  if (a.bias_batch && !xat_by_heads(dtype, a))
+  if (xat_needs_planes(dtype, a))
     p.planes = (size_t)a.bias_batch * a.h * a.nq * p.nkp * e;
   if (p.splits > 1) p.part = (size_t)p.splits * all * (a.d + 2) * sizeof(float);
   return p;

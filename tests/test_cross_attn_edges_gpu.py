@@ -1,8 +1,9 @@
-"""Cross attention through the C ABI: one valid key in loops that are split (bounds in
-cross_ref.py)."""
+"""Cross attention through the C ABI: one valid key in loops that are split, many samples with
+a bias map each (bounds in cross_ref.py)."""
 import pytest
 import torch
 
+import cross_ref as C
 import ops_ref as R
 from paper_2506_20686_amd import binding as B
 from test_cross_attn_gpu import DEV, BF, F4, both, dev, inputs
@@ -42,3 +43,26 @@ def test_one_valid_key_of_split_loops(nq, nk, h, hk, bias, dtype):
         assert not bool(db[:, (keys != 1) & (keys != nk - 2)].any())
     keep = slice(0, 4)  # the plain form has no row without a key
     both(q[keep], k[keep], v[keep], x[keep] if bias == "each" else x, m[keep], y[keep])
+
+
+def test_many_samples_with_a_map_each():
+    # 512 maps of 768 x 768 x 4 heads (2.4 GB), taken as they lie: the first and the last sample
+    b, n, h, d = 512, 768, 4, 8
+    g = torch.Generator(DEV).manual_seed(1)
+
+    def normal(*shape):
+        return torch.empty(shape, dtype=BF, device=DEV).normal_(generator=g)
+
+    q, k, v, y, x = *(normal(b, n, h, d) for _ in range(4)), normal(b, n, n, h)
+    m = (torch.rand(b, n, generator=g, device=DEV) < 0.7).to(torch.uint8)
+    m[:, 5] = 1
+    out, stat = B.cross_attn_fwd(q, k, v, x, m)
+    grads = B.cross_attn_bwd(q, k, v, out, stat, y, x, m)
+    for i in (0, b - 1):
+        at = slice(i, i + 1)
+        q1, k1, v1, y1, x1, m1 = (t[at].cpu() for t in (q, k, v, y, x, m))
+        for a, r, e in zip((out, stat), *C.attn_fwd(q1, k1, v1, x1, m1)):
+            R.check("forward", a[at], r, e)
+        for name, a, r, e in zip(("dq", "dk", "dv", "dbias"), grads,
+                                 *C.attn_bwd(q1, k1, v1, y1, x1, m1)):
+            R.check(name, a[at], r, e)

@@ -14,6 +14,17 @@
 namespace triattn {
 namespace {
 
+// sigmoid(z) and sigmoid(-z), neither taken from 1: a and b are sums in fp32, never rounded to
+// the tensors' 8 bits, and the derivative far out is the small side's.  The hardware's exponential
+// serves for bf16 tensors: it is off by twice |z| half steps, as z's own half step is by |z|.
+template <bool FULL>
+__device__ inline void both_sides(float z, float& s, float& other) {
+  if constexpr (FULL) return sigmoid<true>(z, s, other);
+  const float e = __expf(-fabsf(z)), big = fast_rcp(1.f + e), small = e * big;
+  s = z < 0.f ? small : big;
+  other = z < 0.f ? big : small;
+}
+
 // The activation of tensors of T and its derivative.
 template <typename T>
 __device__ inline void act_both(float z, int act, float& value, float& slope) {
@@ -29,7 +40,7 @@ __device__ inline void act_both(float z, int act, float& value, float& slope) {
     value = z;
     slope = 1.f;
   } else {
-    sigmoid<sizeof(T) == 4>(z, p, q);
+    both_sides<sizeof(T) == 4>(z, p, q);
     value = act == TRIATTN_ACT_SILU ? z * p : p;
     slope = act == TRIATTN_ACT_SILU ? p * (1.f + z * q) : p * q;
   }

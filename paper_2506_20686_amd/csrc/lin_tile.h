@@ -10,8 +10,9 @@ namespace {
 
 // Activations of fp32 tensors keep fp32's bits in the tails too: value and derivative are
 // good to 14 half steps of themselves (the derivative, of its two terms).  With bf16
-// tensors z is known to 8 bits, so the hardware's exponential and reciprocal serve as they
-// are: near 0 both are as good, and far out an exponential of a is off by |a| half steps.
+// tensors the linear projection's z is known to 8 bits, so the hardware's exponential and
+// reciprocal serve as they are: near 0 both are as good, and far out an exponential of a is off
+// by |a| half steps.
 // (In full they cost a bf16 forward of 589,824 x 128 x 128 15%: 100 -> 115 us with gelu.)
 
 // exp(a), and exp(a + b) with |b| below a's last place, for -2^20 < a <= 0: the hardware's

@@ -90,19 +90,19 @@ __global__ __launch_bounds__(256) void grad_root_kernel(const double* part, int6
   if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
-template <typename T>
-__device__ inline u32x4 scaled(u32x4 v, float f) {
+template <typename T, typename F>
+__device__ inline u32x4 scaled(u32x4 v, F f) {
   constexpr int W = 16 / (int)sizeof(T);
   struct E {
     T x[W];
   };
   E e = __builtin_bit_cast(E, v);
 #pragma unroll
-  for (int k = 0; k < W; ++k) e.x[k] = (T)((float)e.x[k] * f);
+  for (int k = 0; k < W; ++k) e.x[k] = (T)(float)((F)(float)e.x[k] * f);
   return __builtin_bit_cast(u32x4, e);
 }
-template <typename T>
-__device__ inline void scale(const T* p, T* o, int64_t n, float f) {
+template <typename T, typename F>
+__device__ inline void scale(const T* p, T* o, int64_t n, F f) {
   constexpr int W = 16 / (int)sizeof(T);
   const int64_t words = n / W;
   int64_t i = threadIdx.x;
@@ -116,7 +116,13 @@ __device__ inline void scale(const T* p, T* o, int64_t n, float f) {
   }
   for (; i < words; i += 256) ((u32x4*)o)[i] = scaled<T>(((const u32x4*)p)[i], f);
   i = words * W + threadIdx.x;
-  if (i < n) o[i] = (T)((float)p[i] * f);
+  if (i < n) o[i] = (T)(float)((F)(float)p[i] * f);
+}
+template <typename F>
+__device__ inline void scale_tensor(const GradArgs& a, int t, int64_t at, F f) {
+  const int64_t n = a.size[t] - at < a.span ? a.size[t] - at : a.span;
+  if (a.dtype[t] == TRIATTN_BF16) scale((const bf16*)a.src[t] + at, (bf16*)a.dst[t] + at, n, f);
+  else scale((const float*)a.src[t] + at, (float*)a.dst[t] + at, n, f);
 }
 
 __global__ __launch_bounds__(256) void grad_scale_kernel(GradArgs a) {
@@ -127,9 +133,9 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(GradArgs a) {
   const float f = finite && norm > a.limit ? a.limit / norm : 1.f;
   if (f == 1.f && a.src[t] == a.dst[t]) return;
   const int64_t at = (int64_t)(wg - a.first[t]) * a.span;
-  const int64_t n = a.size[t] - at < a.span ? a.size[t] - at : a.span;
-  if (a.dtype[t] == TRIATTN_BF16) scale((const bf16*)a.src[t] + at, (bf16*)a.dst[t] + at, n, f);
-  else scale((const float*)a.src[t] + at, (float*)a.dst[t] + at, n, f);
+  // a factor below fp32's normal numbers has lost bits, though its products need not be small
+  if (f >= 0x1p-126f) scale_tensor(a, t, at, f);
+  else scale_tensor(a, t, at, (double)a.limit / (double)norm);
 }
 
 }  // namespace

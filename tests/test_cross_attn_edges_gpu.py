@@ -1,5 +1,5 @@
-"""Cross attention through the C ABI: one valid key in loops that are split, many samples with
-a bias map each (bounds in cross_ref.py)."""
+"""Cross attention through the C ABI: one valid key in loops that are split; many samples with
+a bias map each, or one for all (bounds in cross_ref.py)."""
 import pytest
 import torch
 
@@ -66,3 +66,20 @@ def test_many_samples_with_a_map_each():
         for name, a, r, e in zip(("dq", "dk", "dv", "dbias"), grads,
                                  *C.attn_bwd(q1, k1, v1, y1, x1, m1)):
             R.check(name, a[at], r, e)
+
+
+# one map of many samples: sums of dS over them, by slabs of samples from 16 of them on (fewer
+# samples than slices, as many and more, and more than twice), of four heads side by side and
+# of planes (shared key heads, heads not in fours); and past 2^20 columns, four a thread
+@pytest.mark.parametrize("dtype", [BF, F4])
+@pytest.mark.parametrize("b,nq,nk,h,hk,d", [
+    (16, 9, 33, 4, 4, 16), (17, 31, 13, 8, 8, 24), (64, 5, 40, 4, 4, 8), (150, 7, 11, 4, 4, 8),
+    (16, 9, 33, 4, 2, 16), (17, 31, 13, 3, 3, 24), (70, 6, 65, 5, 5, 8), (150, 3, 11, 6, 2, 8),
+    (15, 20, 70, 4, 4, 32), (15, 20, 70, 2, 2, 32), (16, 1, 1, 4, 4, 8), (40, 1, 1, 1, 1, 8),
+    (16, 100, 660, 16, 16, 8), (16, 90, 650, 18, 18, 8)])
+def test_a_map_that_many_samples_share(b, nq, nk, h, hk, d, dtype):
+    q, k, v, x, m, y = inputs(b, nq, nk, h, hk, d, dtype, "shared", True, seed=b + nk)
+    got = both(q, k, v, x, m, y)
+    again = B.cross_attn_bwd(dev(q), dev(k), dev(v), *got[:2], dev(y), dev(x), dev(m))
+    for a, c in zip(again, got[2:]):  # in a fixed order
+        assert torch.equal(a, c)

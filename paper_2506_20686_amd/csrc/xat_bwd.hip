@@ -218,7 +218,7 @@ __global__ __launch_bounds__(256) void xat_dq_join_kernel(XatArgs a) {
   if (i >= all * quads) return;
   const int64_t R = i / quads;
   const int ch = 4 * (int)(i % quads);
-  const int64_t rows = (int64_t)a.nq * a.h, b = R / rows;
+  const uint32_t rows = (uint32_t)a.nq * a.h, b = (uint32_t)R / rows;  // (at most 2^31 rows)
   f32x4 sk{}, pk{};
   float e = 0.f;
   int valid = 0;
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(256) void xat_dq_join_kernel(XatArgs a) {
     sk += *(const f32x4*)(part_ab(a, s, R, 0) + ch);
     pk += *(const f32x4*)(part_ab(a, s, R, 1) + ch);
     e += *part_e(a, s, R);
-    valid += a.valid[b * a.splits + s];
+    valid += a.valid[(int64_t)b * a.splits + s];
   }
   const bool single = valid <= 1;
   f32x4 x;
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(256) void xat_dq_join_kernel(XatArgs a) {
   store4((T*)a.dq + R * a.d + ch, x);
   if (ch == 0) {
     a.dsum[R] += e;
-    if (R == b * rows) a.single[b] = single;
+    if ((uint32_t)R == b * rows) a.single[b] = single;
   }
 }
 

@@ -447,9 +447,10 @@ int tri_cross_attn_fwd(int dtype, int64_t batch, int64_t nq, int64_t nk, int64_t
  * and stat, and dout; with P the weights, dP = dout V^T and D = sum_j P dP,
  *   dS = P (dP - D),  dq = scale dS K,  dk = scale dS^T Q,  dv = P^T dout,  dbias = dS,
  * dk and dv summed over the heads that share a key head and dbias over the samples that
- * share a bias, in a fixed order (bitwise reproducible).  dbias may be NULL (not wanted).  The
- * workspace holds dS in fp32 where there is a bias (4 batch nq nk heads bytes).  Same rules as
- * the forward. */
+ * share a bias, in a fixed order (bitwise reproducible).  A sample with one valid key has dS = 0.
+ * dbias may be NULL (not wanted).  The workspace holds dS of every sample in fp32 (4 batch nq nk
+ * heads bytes, with or without dbias) where samples share a map or the bias is turned into
+ * planes.  Same rules as the forward. */
 int tri_cross_attn_bwd_workspace_bytes(int dtype, int64_t batch, int64_t nq, int64_t nk,
                                        int64_t heads, int64_t key_heads, int64_t d,
                                        int64_t bias_batch, size_t* bytes);
@@ -466,9 +467,10 @@ int tri_cross_attn_bwd(int dtype, int64_t batch, int64_t nq, int64_t nk, int64_t
  * x [m][k], W [k][2 f] (a = columns 0 .. f-1, b = columns f .. 2 f-1, as W1 of the transition
  * layer), bias [2 f] (NULL = zeros), out [m][f], all in dtype.  Neither a nor b is written.
  *   act: a triattn_act, TRIATTN_ACT_SIGMOID too.
- *   dtype: as tri_linear_fwd.  1 <= m <= 2^31, 1 <= k <= 8192, 1 <= f <= 4096
- *   (TRIATTN_ERR_UNSUPPORTED above), any parity, and fewer than 2^24 tiles of 64 x 32 outputs
- *   (TRIATTN_ERR_UNSUPPORTED).  No workspace.  Same stream, pointer and error rules as above. */
+ *   dtype: as tri_linear_fwd.  1 <= m <= 2^31, 1 <= k <= 8192, 1 <= f <= 4096 (2 f within the
+ *   linear projection's 8192 columns; TRIATTN_ERR_UNSUPPORTED above), any parity, and fewer than
+ *   2^24 tiles of 64 x 32 outputs (TRIATTN_ERR_UNSUPPORTED).  No workspace.  Same stream, pointer
+ *   and error rules as above. */
 int tri_gated_linear_fwd(int dtype, int64_t m, int64_t k, int64_t f, int act, const void* x,
                          const void* w, const void* bias, void* out, void* stream);
 

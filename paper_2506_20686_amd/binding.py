@@ -1158,7 +1158,13 @@ _dtype_of = operator.attrgetter("dtype")
 class GradList:
     """A list of gradients (fp32 and bf16 tensors of one GPU, of any shapes, contiguous),
     checked once, for programs that clip the same ones step after step.  A call
-    looks up the tensors' addresses anew.  A tensor may be there once only."""
+    looks up the tensors' addresses anew, and refuses what has another size, dtype or
+    device since.  A tensor may be there once only.
+
+    The list holds the tensors, not the parameters whose gradients they are: it serves
+    where gradients stay (zero_grad(set_to_none=False), or buffers that a backward adds
+    to).  Where each step makes new ones, as torch's zero_grad does by default, make a
+    new list each step too; a kept one would norm and scale the old ones."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)

@@ -103,8 +103,9 @@ struct GradPlan {
   int64_t span, wgs;
 };
 int64_t grad_wgs(int64_t size, int64_t span) { return (size + span - 1) / span; }
-// A workgroup's elements: 32768 (8 or 16 words of 16 bytes a thread, four at a time), fewer where
-// that leaves CUs idle, down to 2048 (130,000 elements of 14 tensors: one round of words).
+// A workgroup's elements: 32768 (16 words of 16 bytes a thread in bf16, 32 in fp32, four at a
+// time), fewer where that leaves CUs idle, down to 2048 (130,000 elements of 14 tensors: one or two
+// words a thread).
 int grad_plan(int64_t count, const int64_t* sizes, GradPlan* p) {
   if (count < 1 || count > ((int64_t)1 << 20) || sizes == nullptr) return TRIATTN_ERR_INVALID_ARG;
   int64_t total = 0;

@@ -85,8 +85,8 @@ __device__ inline void put_planes(bf16* p, int64_t plane, int have, float (&f)[8
   }
 }
 
-// 6001 x 512 x 2048 bf16: 50 us (500 TFLOP/s), with dz as its result 73; as the linear projection's
-// forward, LDS reads and staging beside the products.
+// 6001 x 512 x 2048 bf16: 45 us (560 TFLOP/s), with dz as its result 65 (50 and 73 in the first
+// passes); as the linear projection's forward, LDS reads and staging beside the products.
 template <typename T, int R, bool ALIGNED, bool DZ>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void glu_kernel(GluArgs a) {
   using G = Product<T, T, R, step_k(R, 2 * planes<T>()), true, false, planes<T>(), planes<T>(),
@@ -272,9 +272,10 @@ __global__ __launch_bounds__(256, 2) void glu_narrow_fwd_kernel(GluArgs a) {
 //   dW   32 columns of dz a wave, all of k, in registers to the end;
 //   dx   a tile of 32 of k and one half of dz's columns a wave; the halves meet in LDS.
 // 48 of a wave's 56 matrix instructions a block are the three planes' (24 bits of dz).  589,824 x
-// 128 x 128: 346 us, 270 GFLOP of matrix instructions; the matrix cores are busy 45% of the time,
-// the vector units 33%, LDS 32%, in phases that follow each other.  (The general kernels: 598 us.
-// The next block's z and dz beside this one's dW, with a barrier less: 380.)
+// 128 x 128: 312 us, 350 in the first passes; 270 GFLOP of matrix instructions; the matrix cores
+// are busy 44% of the time, the vector units 34%, LDS 31%, in phases that follow each other.
+// (First passes too: the general kernels 598 us; the next block's z and dz beside this one's dW,
+// with a barrier less, 380.)  All 256 registers are taken, and with an activation 2 to 6 spilled.
 constexpr int GLU_BWD_WG = 512;
 template <int ACT>
 __global__ __launch_bounds__(GLU_BWD_WG) void glu_narrow_bwd_kernel(GluArgs a, LinBwdArgs o) {

@@ -1,8 +1,9 @@
 // Norm of many gradients together, and their scaling.  Bound by memory: each is read once for
 // the norm; read again (from the last-level cache, as far as it holds them) and written once.
 //
-// Squares are summed in 64 bits: an fp32 square has 48, so a term is exact, and no sum of
-// fp32 squares overflows or loses small ones.  The workgroups' sums are added in a fixed order.
+// Squares are summed in 64 bits: an fp32 square has 48, so a term is exact, no sum of them
+// overflows, and what is lost are terms below 2^-53 of it.  The workgroups' sums are added in a
+// fixed order.
 // 150,000,001 bf16 elements: 55 us, 5.5 TB/s.  60 tensors, 64,000,000 elements in both types (162
 // MB): 31 us for the sum, 53 to scale them.
 #include "common.h"

@@ -474,8 +474,8 @@ bool wide_w(int64_t m, int k, int n) {
 template <typename T, int DZ, bool AL>
 void bwd_launch(const LinBwdArgs& a, hipStream_t s) {
   const bool weights = a.dw || a.dbias, ww = wide_w(a.m, a.k, a.n);
-  // with planes, 128-wide tiles of dx beside those of dW where they make up half the CUs'
-  // work: tiles of 64 read LDS as often as the matrix cores multiply
+  // with planes, 128-wide tiles of dx beside those of dW from 96 of them on, three eighths of the
+  // CUs: tiles of 64 read LDS as often as the matrix cores multiply
   constexpr bool PLANES = DZ == DZ_PLANES && sizeof(T) == 2;
   const bool beside = PLANES && ww && a.dx && weights && a.k > 64 &&
                       tiles_of(a.m, a.k, 128) >= 96 && tiles_of(a.m, a.k, 128) < 256;

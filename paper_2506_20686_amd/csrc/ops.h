@@ -76,7 +76,8 @@ size_t lin_slab_bytes(int k, int n, int splits);
 hipError_t launch_lin_reduce(const LinBwdArgs& a, hipStream_t s);
 
 // ---- gated linear projection (glu.hip) -------------------------------------------------------
-constexpr int GLU_MAX_F = 4096;
+constexpr int GLU_MAX_F = 4096;  // 2 f columns of W: the linear projection's 8192, whose products
+                                 // the backward runs
 
 struct GluArgs {
   int64_t m;

@@ -14,12 +14,17 @@
 //   dQ = scale (dS' K - e P K),  D = d + e,
 // one more product for an exact D, where a pass of its own over the keys would take two and the
 // exponentials again.  A sample with one valid key has P = 1 and dS = 0 whatever its logits, which
-// no rounded P and D give exactly: its dS are set to 0.
+// no rounded P and D give exactly: its dS are set to 0 (the keys are counted over all splits).
 //
-// dS and P are rounded to bf16 for the second products (bf16 tensors).  2 x 2048 x 4099, 16 heads
-// of 64, a quarter of the keys masked: dq 139 us, dkv 171 (750 and 600 TFLOP/s of the valid keys'
-// four products each), bound as the forward is, at two waves a SIMD for their registers.
-// 737 windows of 32 x 128: 22 and 43 us, 5 and 3.5 TB/s.
+// dS and P are rounded to bf16 for the second products (bf16 tensors), half a step of each: dq, dk
+// and dv are off by 2.4e-3 of their norms, where their own rounding alone makes 1.7e-3.  With what
+// the roundings leave as products of their own it is 1.7e-3, but 432 us for 315 at 2 x 2048 x 4099
+// (first passes; windows 71 for 66, 768 x 768 with 16 heads of 24 46 for 42).
+//
+// 2 x 2048 x 4099, 16 heads of 64, a quarter of the keys masked: dq 123 us, dkv 147 (840 and 700
+// TFLOP/s of the valid keys' four products each; 137 and 168 in the first passes), as the forward
+// with no unit busy all the time: two waves a SIMD for their registers, vector issue 53 and 46% of
+// the cycles, the matrix cores 41 and 36%.  737 windows of 32 x 128: 22 and 43 us, 5 and 3.5 TB/s.
 #include "timing.h"
 #include "triattn.h"
 #include "xat.h"

@@ -6,15 +6,17 @@
 // through registers into LDS, the next tile's loads in flight while one is multiplied.
 //
 // Logits stay in natural units where there is a bias: a bias of the type's lowest value would
-// overflow in base 2.  P is rounded to bf16 for its product (bf16 tensors): half a step of each
-// weight, as much as the output's own rounding, beside twice the matrix instructions for 16 bits
-// of it.
+// overflow in base 2.  P is rounded to bf16 for its product (bf16 tensors), half a step of each
+// weight: an output is off by 1.9e-3 to 2.3e-3 of its norm, where its own rounding alone makes
+// 1.7e-3.  With what the rounding leaves as a second product, 16 bits of P, it is 1.7e-3, but 137
+// us for 107 at 2 x 2048 x 4099 (first passes; windows 21.3 for 20.7).
 //
-// Bound, with long loops, by vector issue: an exponential a logit (a quarter of the rate) and some
-// 100 other instructions a 32 x 32 tile, beside 8 matrix instructions of 64 channels.  2 x 2048 x
-// 4099, 16 heads of 64, a quarter of the keys masked: 107 us (640 TFLOP/s of all keys, 480 of the
-// valid ones; the vector units 55% busy at the two waves a SIMD that 512 workgroups make).  One
-// query to 30,011 keys: 24 us, 3.8 TB/s.  737 windows of 32 x 128 with a bias: 20 us, 4.2 TB/s.
+// With long loops no unit is busy all the time: vector issue (an exponential a logit, a quarter of
+// the rate, and some 100 other instructions a 32 x 32 tile) takes 55% of the cycles, the matrix
+// cores 26%, LDS 21%, one after the other in each of the two waves a SIMD that 512 workgroups
+// make.  2 x 2048 x 4099, 16 heads of 64, a quarter of the keys masked: 89 us (770 TFLOP/s of all
+// keys, 580 of the valid ones; 105 us in the first passes, before the card has settled).  One
+// query to 30,011 keys: 22 us, 4.1 TB/s.  737 windows of 32 x 128 with a bias: 20 us, 4.3 TB/s.
 #include "timing.h"
 #include "triattn.h"
 #include "xat.h"

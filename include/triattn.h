@@ -420,6 +420,7 @@ int tri_rel_bias_bwd(int dtype, int64_t batch, int64_t n, int64_t h, int n_edges
  *                      type's lowest value); -inf and 0 for a query without a key
  *   dtype: TRIATTN_F32 (fp32 throughout) or TRIATTN_BF16 (fp32 sums and statistics; the
  *          weights P and their gradients dS rounded to bf16 for the second products).
+ *          Weights below 2^-126, fp32's least normal number, are 0.
  *   d a multiple of 8, at most 128 (TRIATTN_ERR_UNSUPPORTED else); heads a multiple of
  *   key_heads, at most 256 (TRIATTN_ERR_UNSUPPORTED above); 1 <= nq, nk <= 2^22;
  *   1 <= batch <= 2^20; scale finite and positive; with g = heads / key_heads, (nq g + 256) g
